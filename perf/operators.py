@@ -33,11 +33,11 @@ def listed():
         # a small fp32 network, 77 states with holes in the mask
         dict(cross, name="cross_f32_masked", batch=2, q_len=1000, kv_len=77, heads=16, kv_heads=16, head_dim=32, dtype="f32", masked=True),
         # the QKV projection of the full network: 17550 + 226 tokens
-        {"name": "linear_qkv_full", "kind": "linear", "rows": 17776, "k": 1920, "n_out": 5760, "act": 0, "dtype": "bf16", "out": "bf16"},
+        {"name": "linear_qkv_full", "kind": "linear", "rows": 17776, "k": 1920, "n_out": 5760, "act": 0, "dtype": "bf16"},
         # the second MLP projection of one block on 4290 + 226 tokens
-        {"name": "linear_fc2_block", "kind": "linear", "rows": 4516, "k": 7680, "n_out": 1920, "act": 0, "dtype": "bf16", "out": "bf16"},
+        {"name": "linear_fc2_block", "kind": "linear", "rows": 4516, "k": 7680, "n_out": 1920, "act": 0, "dtype": "bf16"},
         # the first MLP projection on the 112 tokens of a preview: weights are what is read
-        {"name": "linear_fc1_few", "kind": "linear", "rows": 112, "k": 1920, "n_out": 7680, "act": 1, "dtype": "bf16", "out": "bf16"},
+        {"name": "linear_fc1_few", "kind": "linear", "rows": 112, "k": 1920, "n_out": 7680, "act": 1, "dtype": "bf16"},
         # the MLP's activations of the full network
         {"name": "quantize_mlp_full", "kind": "quantize", "rows": 17776, "k": 7680, "dtype": "bf16"},
         # ragged fp32 rows that end inside a block
@@ -68,7 +68,7 @@ def draw(rng):
                 return c
         elif kind == "linear":
             c = {"kind": kind, "rows": _log(rng, 1, 17776), "k": _log(rng, 64, 7680), "n_out": 4 * _log(rng, 8, 1920), "act": rng.choice([0, 0, 1]),
-                 "dtype": rng.choice(["bf16", "bf16", "f32"]), "out": rng.choice(["bf16", "bf16", "f32"])}
+                 "dtype": rng.choice(["bf16", "bf16", "f32"])}
             if work(c)["flops"] <= 3.9e11:
                 return c
         elif kind == "quantize":
@@ -96,7 +96,7 @@ def work(case):
                 "flops": 4.0 * c["batch"] * c["heads"] * c["q_len"] * keys * c["head_dim"]}
     if c["kind"] == "linear":
         return {"bytes": c["rows"] * c["k"] * (4.0 if c["dtype"] == "f32" else 2.0) + 1.0 * c["n_out"] * c["k"] +
-                c["rows"] * c["n_out"] * (4.0 if c["out"] == "f32" else 2.0), "flops": 2.0 * c["rows"] * c["k"] * c["n_out"]}
+                c["rows"] * c["n_out"] * 2.0, "flops": 2.0 * c["rows"] * c["k"] * c["n_out"]}
     if c["kind"] == "quantize":
         return {"bytes": c["rows"] * c["k"] * ((4.0 if c["dtype"] == "f32" else 2.0) + 1.0), "flops": 3.0 * c["rows"] * c["k"]}
     n = c["batch"] * c["positions"] * c["channels"]
@@ -213,7 +213,7 @@ def run(state):
             return B.fp8_quantize(s["x"])
         if kind == "linear":
             a, a_scale = B.fp8_quantize(s["x"])
-            return B.dit_linear_fp8(a, a_scale, s["w"], s["w_scale"], s["bias"], act=s["act"], out_dtype=_type(s["out"]))
+            return B.dit_linear_fp8(a, a_scale, s["w"], s["w_scale"], s["bias"], act=s["act"])
         return B.group_norm(s["x"], s["groups"], s["gamma"], s["beta"], eps=1e-5, act=s["act"])
     if kind == "cross":
         return _cross_plain(s)
@@ -221,7 +221,7 @@ def run(state):
         return _quantize_plain(s["x"])
     if kind == "linear":
         y = torch.matmul(_widen(*_quantize_plain(s["x"])), _widen(s["w"], s["w_scale"]).t()) + s["bias"]
-        return _activate(y, s["act"]).to(_type(s["out"]))
+        return _activate(y, s["act"]).to(torch.bfloat16)
     return _gnorm_plain(s)
 
 
