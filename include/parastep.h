@@ -35,6 +35,7 @@
  * with K % 64 == 0 and at least 64 outputs and fp32 with K % 32 == 0 (projections, outputs
  * a multiple of 4) and every attention shape (bf16 products at head_dim 64, fp32 otherwise);
  * every other accepted projection runs on a generic fp32-FMA kernel.
+ * (The operators of a conditioned predictor block name their own limits.)
  */
 #ifndef PARASTEP_H
 #define PARASTEP_H
@@ -180,6 +181,69 @@ PS_API int attn3d(const void* q, const void* k, const void* v, void* o,
 PS_API size_t dit_linear_workspace_bytes(int m, int n_out, int k, int dtype, int kernel_path);
 PS_API int dit_linear(const void* a, const void* w, const float* bias, void* out, int m, int n_out, int k,
                int act, int dtype, int kernel_path, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------- operators of a conditioned predictor block
+ * What a block that is conditioned on an encoder's states runs beside the entry points above (Preliminaries: eps_theta takes the
+ * condition c): attention to those states, projections in 8-bit floating point, and the group norm in front of them.
+ *
+ * Cross attention.  For every sample, query token and head,
+ *   o = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q . k_j - max),
+ * over the sample's keys that count: j < kv_lens[b] (kv_lens DEVICE int32 [batch], clamped to 0 .. kv_len; NULL: kv_len) and
+ * key_mask[b * mask_batch + j] != 0 (DEVICE bytes; NULL: all).  A row without any such key is zero, and what lies in k and v at keys
+ * that do not count is never used, NaN and infinity included (rows 0 .. kv_len-1 must be readable).  q and o hold heads heads,
+ * k and v kv_heads (a divisor): query heads h * (heads / kv_heads) .. share key head h.  head_dim in {16, 32, 64, 128}, its
+ * elements contiguous; every other stride is free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0 to repeat
+ * an operand; of an extent of 1 they are ignored), so k and v may be the halves of one projection.  Pointers 16-byte aligned; o
+ * must not overlap the inputs.  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).  Scores times scale * log2(e) must be
+ * finite in fp32.  bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32;
+ * fp32: everything in fp32.
+ * workspace: DEVICE, 256-byte aligned, >= cross_attn_workspace_bytes(...) (may be NULL when that is 0): where the rows of a sample
+ * do not fill the chip its keys are divided among workgroups, and their partial sums pass through it. */
+typedef struct {
+    int batch, q_len, kv_len, heads, kv_heads, head_dim;
+    int dtype;                                   /* ps_dtype of q, k, v and o */
+    float scale;
+    int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, o_batch, o_token, o_head;
+    int64_t mask_batch;                          /* bytes from one sample's mask to the next; 0: one mask for all */
+} cross_attn_shape;
+PS_API size_t cross_attn_workspace_bytes(const cross_attn_shape* shape);
+PS_API int cross_attn(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* o,
+               const cross_attn_shape* shape, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* 8-bit floating point with a power-of-two scale for each block of 128 columns of a row: x[r, c] = q[r, c] * 2^(s - 127) with
+ * s = scale[c / 128][r].
+ *   q      DEVICE e4m3 bytes [rows][kp], kp = cols rounded up to a multiple of 128, filled up with zeros
+ *   scale  DEVICE e8m0 bytes [kp / 128][pitch], pitch = rows rounded up to a multiple of 16, filled up with 0
+ * fp8_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment, 16 bytes are fastest).  A block's scale is the
+ * least power of two >= 2^-127 under which its largest finite |x| is at most 448; values are rounded once, to nearest even; NaN and
+ * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^31 blocks. */
+PS_API int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream);
+
+/* out[m, n_out] = act(a * w^T + bias) for operands in the format above, a of m rows and w of n_out rows, both of k columns; out DEVICE bf16, row-major; act 0 none, 1 tanh-GELU.  bias DEVICE fp32 [n_out].  All pointers
+ * 16-byte aligned; out must not overlap the operands; m may be 0; k <= 2^22.  Products are summed 8 at a time as the matrix
+ * instruction does it, which cuts off what lies below 2^-13 of the largest of the 8 (in the mean 1e-5 of the result's norm), and from
+ * there on in fp32: that is why out is bf16 only.
+ * workspace: DEVICE, 256-byte aligned, or NULL.  With at least dit_linear_fp8_workspace_bytes(...) of it, shapes whose output tiles
+ * occupy a part of the chip are summed in pieces of k; without, whole: the two differ in summation order only. */
+PS_API size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k);
+PS_API int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m,
+                   int n_out, int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Group norm over channels-last positions: a group is channels / groups neighbouring channels of a sample at all its positions,
+ *   out = act((x - mean) / sqrt(var + eps) * gamma + beta),
+ * var the mean squared deviation; act 0 none, 1 tanh-GELU, 2 SiLU.  x, out DEVICE [batch, positions, channels] in `dtype`, channels
+ * contiguous, batch and position strides in elements (any alignment, 16 bytes are fastest; x's may be 0; ignored for an extent of 1);
+ * out == x is allowed with equal strides, any other overlap is not.  gamma, beta DEVICE fp32 [channels], either may be NULL (1, 0).
+ * Statistics in fp32, merged pairwise.  batch and positions may be 0; channels <= 65536.
+ * workspace: DEVICE, 256-byte aligned, >= group_norm_workspace_bytes(...) (may be NULL when that is 0). */
+typedef struct {
+    int batch, positions, channels, groups, act, dtype;
+    float eps;
+    int64_t x_batch, x_position, out_batch, out_position;
+} group_norm_shape;
+PS_API size_t group_norm_workspace_bytes(int batch, int positions, int channels, int groups, int dtype);
+PS_API int group_norm(const void* x, const float* gamma, const float* beta, void* out, const group_norm_shape* shape, void* workspace,
+               size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------- scheduler and metric
  * Fused DDIM update  x_out = a*x + b*eps  (the element-wise Scheduler of the paper's

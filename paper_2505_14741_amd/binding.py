@@ -25,6 +25,9 @@ PS_F32, PS_BF16 = 0, 1
 KERNEL_CLASSES = ("attention", "gemm_qkv", "gemm_oproj", "gemm_fc1", "gemm_fc2", "ln_modulate", "other")
 
 
+PS_ERR_SHAPE, PS_ERR_DTYPE = -2, -3
+
+
 class PsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -41,6 +44,16 @@ class _Schedule(C.Structure):
     _fields_ = [("steps", C.c_int), ("timesteps", C.POINTER(C.c_int32)), ("coef_a", C.POINTER(C.c_double)),
                 ("coef_b", C.POINTER(C.c_double)), ("warmup", C.c_int), ("n_cycles", C.c_int),
                 ("cycle_len", C.POINTER(C.c_int32)), ("batched", C.c_int), ("mode", C.c_int)]
+
+
+class _CrossShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("batch", "q_len", "kv_len", "heads", "kv_heads", "head_dim", "dtype")] + [("scale", C.c_float)] + [
+        (f"{t}_{n}", C.c_int64) for t in "qkvo" for n in ("batch", "token", "head")] + [("mask_batch", C.c_int64)]
+
+
+class _GroupNormShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("batch", "positions", "channels", "groups", "act", "dtype")] + [("eps", C.c_float)] + [
+        (n, C.c_int64) for n in ("x_batch", "x_position", "out_batch", "out_position")]
 
 
 class SamplerState(C.Structure):
@@ -74,6 +87,13 @@ def lib():
         "attn3d": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, f32, i32, i32, vp, sz, vp]),
         "dit_linear_workspace_bytes": (C.c_size_t, [i32, i32, i32, i32, i32]),
         "dit_linear": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]),
+        "cross_attn_workspace_bytes": (sz, [C.POINTER(_CrossShape)]),
+        "cross_attn": (i32, [vp, vp, vp, vp, vp, vp, C.POINTER(_CrossShape), vp, sz, vp]),
+        "fp8_quantize": (i32, [vp, vp, vp, i32, i32, C.c_int64, i32, vp]),
+        "dit_linear_fp8_workspace_bytes": (sz, [i32, i32, i32]),
+        "dit_linear_fp8": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
+        "group_norm_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+        "group_norm": (i32, [vp, vp, vp, vp, C.POINTER(_GroupNormShape), vp, sz, vp]),
         "sampler_step_workspace_bytes": (sz, [sz]),
         "sampler_step": (i32, [vp, vp, vp, vp, C.c_double, C.c_double, sz, vp, vp, sz, vp]),
         "sampler_step_noalloc": (i32, [vp, vp, vp, vp, C.c_double, C.c_double, sz, vp, vp]),
@@ -103,7 +123,8 @@ EXPORTED = ("ps_strerror", "ps_mfma_probe", "dit_set_kernel_path", "dit_get_kern
             "attn3d_workspace_bytes", "attn3d", "dit_linear_workspace_bytes", "dit_linear", "sampler_step_workspace_bytes", "sampler_step",
             "rel_mae_workspace_bytes", "rel_mae", "ddim_coefficients", "euler_discrete_coefficients",
             "flow_euler_coefficients", "sampler_workspace_bytes", "sampler_run", "sampler_state_bytes",
-            "sampler_run_steps")
+            "sampler_run_steps", "cross_attn_workspace_bytes", "cross_attn", "fp8_quantize", "dit_linear_fp8_workspace_bytes",
+            "dit_linear_fp8", "group_norm_workspace_bytes", "group_norm")
 
 
 def _check(status: int, where: str):
@@ -246,6 +267,125 @@ def dit_linear(a: torch.Tensor, w: torch.Tensor, bias: torch.Tensor, act: int = 
     ws = _workspace(nb, a.device)
     _check(lib().dit_linear(_ptr(a), _ptr(w), _ptr(bias), _ptr(out), M, Nn, K, int(act), dt, int(kernel_path),
                             _ptr(ws), nb, _stream()), "dit_linear")
+    return out
+
+
+# ------------------------------------- operators of a conditioned predictor block
+_CODE = {torch.float32: PS_F32, torch.bfloat16: PS_BF16}
+
+
+def _need(ok: bool, where: str, what: str, status: int = PS_ERR_SHAPE):
+    if not ok:
+        raise PsError(status, f"{where}: {what}")
+
+
+def _need_here(where: str, *tensors: Optional[torch.Tensor]):
+    """Kernels run on the current device and its current stream, on memory of that device."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.get_device() == dev), where, "tensors must lie on the current GPU")
+
+
+def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, kv_lens: Optional[torch.Tensor] = None,
+               key_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [B, Nq, H, d]; k, v [B, Nk, Hkv, d], any strides whose elements of a head are contiguous; kv_lens int32 [B]; key_mask bool
+    or uint8 [B, Nk], also expanded from one sample's.  A query without a key that counts gets zeros."""
+    w = "cross_attn"
+    _need(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape, w, "q [B, Nq, H, d], k and v [B, Nk, Hkv, d]")
+    B, N, H, d = q.shape
+    _need(k.shape[0] == B and k.shape[3] == d, w, "k and v must have q's batch and head_dim")
+    dt = _CODE.get(q.dtype)
+    _need(dt is not None and k.dtype == q.dtype and v.dtype == q.dtype, w, "float32 or bfloat16, the same for q, k and v", PS_ERR_DTYPE)
+    if out is None:
+        out = torch.empty((B, N, H, d), dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape, w, "out must have q's shape")
+    _need(out.dtype == q.dtype, w, "out must have q's type", PS_ERR_DTYPE)
+    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()
+    _need(qs[3] == ks[3] == vs[3] == os_[3] == 1, w, "the elements of a head must be contiguous")
+    mask_batch = 0
+    if kv_lens is not None:
+        _need(kv_lens.dtype == torch.int32, w, "kv_lens must be int32", PS_ERR_DTYPE)
+        _need(kv_lens.shape == (B,) and kv_lens.is_contiguous(), w, "kv_lens must be [B], contiguous")
+    if key_mask is not None:
+        _need(key_mask.dtype in (torch.bool, torch.uint8), w, "key_mask must be bool or uint8", PS_ERR_DTYPE)
+        _need(key_mask.shape == (B, k.shape[1]) and (k.shape[1] <= 1 or key_mask.stride(1) == 1), w, "key_mask must be [B, Nk], rows contiguous")
+        mask_batch = key_mask.stride(0) if B > 1 else 0
+    _need_here(w, q, k, v, out, kv_lens, key_mask)
+    s = _CrossShape(B, N, k.shape[1], H, k.shape[2], d, dt, float(scale), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                    os_[0], os_[1], os_[2], mask_batch)
+    n = lib().cross_attn_workspace_bytes(C.byref(s))
+    ws = _workspace(n, q.device)
+    _check(lib().cross_attn(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_lens), _ptr(key_mask), _ptr(out), C.byref(s), _ptr(ws), n, _stream()), w)
+    return out
+
+
+def fp8_quantize(x: torch.Tensor):
+    """x [rows, cols], float32 or bfloat16, rows any distance apart -> (q float8_e4m3fn [rows, kp], scale float8_e8m0fnu [kp / 128,
+    pitch]): kp is cols rounded up to 128, pitch is rows rounded up to 16, both filled up as include/parastep.h says."""
+    w = "fp8_quantize"
+    _need(x.dim() == 2 and x.shape[1] >= 1, w, "x must be [rows, cols]")
+    dt = _CODE.get(x.dtype)
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    rows, cols = x.shape
+    _need(x.stride(1) == 1 or cols == 1, w, "the elements of a row must be contiguous")
+    _need_here(w, x)
+    blocks = (cols + 127) // 128
+    q = torch.empty((rows, blocks * 128), dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty((blocks, (rows + 15) // 16 * 16), dtype=torch.float8_e8m0fnu, device=x.device)
+    _check(lib().fp8_quantize(_ptr(x), _ptr(q), _ptr(scale), rows, cols, x.stride(0), dt, _stream()), w)
+    return q, scale
+
+
+def dit_linear_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor, act: int = 0,
+                   out: Optional[torch.Tensor] = None, use_workspace: bool = True) -> torch.Tensor:
+    """act(a w^T + bias) of operands from fp8_quantize: a of [M, K] and w of [n_out, K]; bias float32 [n_out], out bfloat16."""
+    f = "dit_linear_fp8"
+    _need(a.dim() == 2 and w.dim() == 2 and a.shape[1] == w.shape[1] and a.shape[1] % 128 == 0 and a.shape[1] > 0, f,
+          "a [M, kp] and w [n_out, kp], kp a multiple of 128")
+    M, K = a.shape
+    Nn = w.shape[0]
+    _need(a.dtype == torch.float8_e4m3fn and w.dtype == torch.float8_e4m3fn and a_scale.dtype == torch.float8_e8m0fnu and
+          w_scale.dtype == torch.float8_e8m0fnu, f, "values in float8_e4m3fn, scales in float8_e8m0fnu", PS_ERR_DTYPE)
+    _need(bias.dtype == torch.float32, f, "bias must be float32", PS_ERR_DTYPE)
+    _need(a_scale.shape == (K // 128, (M + 15) // 16 * 16) and w_scale.shape == (K // 128, (Nn + 15) // 16 * 16), f,
+          "scales [kp / 128, rows rounded up to 16]")
+    _need(bias.shape == (Nn,), f, "bias must be [n_out]")
+    if out is None:
+        out = torch.empty((M, Nn), dtype=torch.bfloat16, device=a.device)
+    _need(out.shape == (M, Nn), f, "out must be [M, n_out]")
+    _need(out.dtype == torch.bfloat16, f, "out must be bfloat16", PS_ERR_DTYPE)
+    _need(a.is_contiguous() and a_scale.is_contiguous() and w.is_contiguous() and w_scale.is_contiguous() and bias.is_contiguous() and
+          out.is_contiguous(), f, "operands must be contiguous")
+    _need_here(f, a, a_scale, w, w_scale, bias, out)
+    nb = _bytes("dit_linear_fp8_workspace_bytes", M, Nn, K) if use_workspace else 0
+    ws = _workspace(nb, a.device)
+    _check(lib().dit_linear_fp8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(out), M, Nn, K, int(act),
+                                _ptr(ws), nb, _stream()), f)
+    return out
+
+
+def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               act: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [B, positions, C] (channels contiguous, other strides free), float32 or bfloat16; gamma, beta float32 [C]; act 0 none, 1
+    tanh-GELU, 2 SiLU.  out may be x."""
+    w = "group_norm"
+    _need(x.dim() == 3 and x.shape[2] >= 1, w, "x must be [B, positions, C]")
+    B, S, ch = x.shape
+    dt = _CODE.get(x.dtype)
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    if out is None:
+        out = torch.empty((B, S, ch), dtype=x.dtype, device=x.device)
+    _need(out.shape == x.shape, w, "out must have x's shape")
+    _need(out.dtype == x.dtype, w, "out must have x's type", PS_ERR_DTYPE)
+    _need(ch == 1 or (x.stride(2) == 1 and out.stride(2) == 1), w, "channels must be contiguous")
+    for t in (gamma, beta):
+        _need(t is None or t.dtype == torch.float32, w, "gamma and beta must be float32", PS_ERR_DTYPE)
+        _need(t is None or (t.shape == (ch,) and t.is_contiguous()), w, "gamma and beta must be [C], contiguous")
+    _need_here(w, x, out, gamma, beta)
+    s = _GroupNormShape(B, S, ch, int(groups), int(act), dt, float(eps), x.stride(0), x.stride(1), out.stride(0), out.stride(1))
+    n = _bytes("group_norm_workspace_bytes", B, S, ch, int(groups), dt)
+    ws = _workspace(n, x.device)
+    _check(lib().group_norm(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), C.byref(s), _ptr(ws), n, _stream()), w)
     return out
 
 

@@ -7,6 +7,9 @@
 #include <vector>
 
 #include "common.h"
+#include "cross_attention.h"
+#include "fp8.h"
+#include "group_norm.h"
 #include "slim.h"
 
 using namespace ps;
@@ -495,6 +498,135 @@ int dit_linear(const void* a, const void* w, const float* bias, void* out, int m
     ep.split_ws_bytes = workspace ? workspace_bytes : 0;
     hipError_t e = launch_gemm(dtype, a, w, out, 1, m, n_out, k, ep, kernel_path, (hipStream_t)hip_stream);
     return e == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+namespace {
+
+// strides of a [batch, token, head, head_dim] operand that 16-byte accesses can follow; an extent of one has no stride
+bool strides_ok(long n_batch, long n_token, long n_head, int64_t batch, int64_t token, int64_t head, int esize, bool written) {
+    const int64_t unit = 16 / esize, st[3] = {batch, token, head};
+    const long n[3] = {n_batch, n_token, n_head};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (st[i] < 0 || st[i] % unit || st[i] > ((int64_t)1 << 40) || (written && st[i] == 0))) return false;
+    return true;
+}
+
+// PS_OK and the launcher's arguments, or why not
+int cross_args(const cross_attn_shape* s, CrossArgs& a) {
+    if (!s) return PS_ERR_NULL;
+    if (s->dtype != PS_F32 && s->dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (s->head_dim != 16 && s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return PS_ERR_SHAPE;
+    if (s->batch < 0 || s->q_len < 0 || s->kv_len < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads) return PS_ERR_SHAPE;
+    if (s->batch > 65535 || s->heads > 65535 || s->q_len > (1 << 24) || s->kv_len > (1 << 24)) return PS_ERR_SHAPE;
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return PS_ERR_SHAPE;
+    const int es = s->dtype == PS_BF16 ? 2 : 4;
+    if (!strides_ok(s->batch, s->q_len, s->heads, s->q_batch, s->q_token, s->q_head, es, false) ||
+        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->k_batch, s->k_token, s->k_head, es, false) ||
+        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->v_batch, s->v_token, s->v_head, es, false) ||
+        !strides_ok(s->batch, s->q_len, s->heads, s->o_batch, s->o_token, s->o_head, es, true) || s->mask_batch < 0)
+        return PS_ERR_SHAPE;
+    const long share = s->heads / s->kv_heads, rows = s->q_len * share;
+    if (rows > (1L << 30) || (rows + 15) / 16 * s->batch * s->kv_heads > (1L << 27)) return PS_ERR_SHAPE;    // grids of 2^31 with their pieces
+    a = CrossArgs{};
+    a.mask_batch = s->mask_batch;
+    a.batch = s->batch; a.rows = (int)rows; a.share = (int)share; a.kv_len = s->kv_len; a.kv_heads = s->kv_heads;
+    a.head_dim = s->head_dim; a.scale = s->scale;
+    a.s = AttnStrides{(long)s->q_token, (long)s->q_head, (long)s->q_batch, (long)s->k_token, (long)s->k_head, (long)s->k_batch,
+                      (long)s->v_token, (long)s->v_head, (long)s->v_batch, (long)s->o_token, (long)s->o_head, (long)s->o_batch};
+    return PS_OK;
+}
+
+}  // namespace
+
+size_t cross_attn_workspace_bytes(const cross_attn_shape* shape) {
+    CrossArgs a;
+    if (cross_args(shape, a) != PS_OK || a.batch == 0 || a.rows == 0) return 0;
+    return align256(cross_workspace_bytes(shape->dtype, a));
+}
+
+int cross_attn(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* o,
+               const cross_attn_shape* shape, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    CrossArgs a;
+    const int rc = cross_args(shape, a);
+    if (rc != PS_OK) return rc;
+    if (a.batch == 0 || a.rows == 0) return PS_OK;
+    if (!q || !o || (a.kv_len > 0 && (!k || !v))) return PS_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(kv_lens, 4) || o == q || o == k || o == v)
+        return PS_ERR_SHAPE;
+    const size_t need = cross_attn_workspace_bytes(shape);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PS_ERR_WORKSPACE;
+    a.q = q; a.k = k; a.v = v; a.o = o;
+    a.kv_lens = kv_lens; a.key_mask = key_mask;
+    a.part = (float*)workspace;
+    return launch_cross_attention(shape->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream) {
+    if (dtype != PS_F32 && dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (rows < 0 || cols < 1 || rows > (1 << 24) || cols > (1 << 22)) return PS_ERR_SHAPE;
+    if (rows == 0) return PS_OK;
+    if ((long)rows * ((cols + 127) / 128) >= (1L << 31)) return PS_ERR_SHAPE;
+    if (rows > 1 && (x_row < cols || x_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    if (!x || !q || !scale) return PS_ERR_NULL;
+    if (!aligned(x, dtype == PS_BF16 ? 2 : 4) || !aligned(q, 16) || !aligned(scale, 16) || q == x || scale == x || q == scale) return PS_ERR_SHAPE;
+    return launch_fp8_quantize(dtype, x, q, scale, rows, cols, rows > 1 ? (long)x_row : cols, (hipStream_t)hip_stream) == hipSuccess
+               ? PS_OK : PS_ERR_HIP;
+}
+
+size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k) {
+    if (m < 1 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22)) return 0;
+    return align256(fp8_product_workspace_bytes(m, n_out, (k + 127) / 128));
+}
+
+int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out,
+                   int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (m < 0 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22) || (act != 0 && act != 1)) return PS_ERR_SHAPE;
+    if (((m + 63L) / 64) * ((n_out + 63L) / 64) >= (1L << 27)) return PS_ERR_SHAPE;
+    if (m == 0) return PS_OK;
+    if (!a || !a_scale || !w || !w_scale || !bias || !out) return PS_ERR_NULL;
+    if (!aligned(a, 16) || !aligned(w, 16) || !aligned(a_scale, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(out, 16) ||
+        out == a || out == w)
+        return PS_ERR_SHAPE;
+    if (workspace && !aligned(workspace, 256)) return PS_ERR_WORKSPACE;
+    Fp8Product g{};
+    g.a = a; g.w = w; g.a_scale = a_scale; g.w_scale = w_scale; g.bias = bias; g.out = (bf16_t*)out;
+    g.m = m; g.n_out = n_out; g.blocks = (k + 127) / 128; g.act = act;
+    g.a_pitch = (m + 15) / 16 * 16; g.w_pitch = (n_out + 15) / 16 * 16;
+    g.ws = (float*)workspace;
+    g.ws_bytes = workspace ? workspace_bytes : 0;
+    return launch_fp8_product(g, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+size_t group_norm_workspace_bytes(int batch, int positions, int channels, int groups, int dtype) {
+    if (batch < 1 || positions < 1 || channels < 1 || groups < 1 || channels % groups || (dtype != PS_F32 && dtype != PS_BF16)) return 0;
+    return align256(group_norm_scratch_bytes(dtype, batch, positions, channels, groups));
+}
+
+int group_norm(const void* x, const float* gamma, const float* beta, void* out, const group_norm_shape* s, void* workspace,
+               size_t workspace_bytes, void* hip_stream) {
+    if (!s) return PS_ERR_NULL;
+    if (s->dtype != PS_F32 && s->dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (s->batch < 0 || s->positions < 0 || s->channels < 1 || s->groups < 1 || s->channels % s->groups) return PS_ERR_SHAPE;
+    if (s->batch > 65535 || s->positions > (1 << 24) || s->channels > (1 << 16) || s->act < 0 || s->act > 2) return PS_ERR_SHAPE;
+    if (!(s->eps >= 0.f) || !std::isfinite(s->eps)) return PS_ERR_SHAPE;
+    for (int64_t st : {s->x_batch, s->out_batch})
+        if (s->batch > 1 && (st < 0 || st > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    for (int64_t st : {s->x_position, s->out_position})
+        if (s->positions > 1 && (st < 0 || st > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    if ((s->batch > 1 && s->out_batch < s->channels) || (s->positions > 1 && s->out_position < s->channels)) return PS_ERR_SHAPE;
+    if (s->batch == 0 || s->positions == 0) return PS_OK;
+    if (!x || !out) return PS_ERR_NULL;
+    const size_t esize = s->dtype == PS_BF16 ? 2 : 4;
+    if (!aligned(x, esize) || !aligned(out, esize) || !aligned(gamma, 4) || !aligned(beta, 4)) return PS_ERR_SHAPE;
+    if (out == x && ((s->batch > 1 && s->x_batch != s->out_batch) || (s->positions > 1 && s->x_position != s->out_position))) return PS_ERR_SHAPE;
+    const size_t need = group_norm_workspace_bytes(s->batch, s->positions, s->channels, s->groups, s->dtype);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PS_ERR_WORKSPACE;
+    GroupNormArgs a{};
+    a.x = x; a.out = out; a.gamma = gamma; a.beta = beta;
+    a.batch = s->batch; a.positions = s->positions; a.channels = s->channels; a.groups = s->groups; a.act = s->act; a.eps = s->eps;
+    a.x_batch = (long)s->x_batch; a.x_position = (long)s->x_position; a.o_batch = (long)s->out_batch; a.o_position = (long)s->out_position;
+    a.part = (float2*)workspace;
+    return launch_group_norm(s->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
 }
 
 size_t sampler_step_workspace_bytes(size_t n) { return align256(reduce_workspace_bytes(n)); }

@@ -287,4 +287,29 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
     return (size_t)p.nsplit * batch * tokens * Nn * sizeof(float);
 }
 
+// ---- group norm: `slices` slices of slice_groups whole groups (the last may have fewer), each over `chunks` chunks of positions.
+// A function of the sample's shape only, never of the batch.
+constexpr int GROUP_NORM_SLICE_GROUPS = 256;             // most groups of a slice: one thread each
+struct GroupNormPlan { int slice_groups, slices, chunks; };
+constexpr GroupNormPlan group_norm_plan(int positions, int channels, int groups, int elem_bytes) {
+    const int cpg = channels / groups;
+    const long bytes = (long)cpg * elem_bytes;
+    // a cache line of a position at least, and whole 16-byte loads if a few groups more give them
+    long k = (127 + bytes) / bytes;
+    for (int more = 0; more < 8; ++more)
+        if ((k + more) * bytes % 16 == 0) { k += more; break; }
+    if (k > GROUP_NORM_SLICE_GROUPS) k = GROUP_NORM_SLICE_GROUPS;
+    if (k > groups) k = groups;
+    GroupNormPlan p{};
+    p.slice_groups = (int)k;
+    p.slices = (groups + p.slice_groups - 1) / p.slice_groups;
+    const long of_slice = (long)positions * p.slice_groups * bytes;
+    long chunks = of_slice / 32768, most = 2048 / p.slices;
+    if (chunks > most) chunks = most;
+    if (chunks > 512) chunks = 512;
+    if (chunks > positions) chunks = positions;
+    p.chunks = chunks < 1 ? 1 : (int)chunks;
+    return p;
+}
+
 }  // namespace ps
