@@ -12,15 +12,27 @@
 namespace ps {
 
 struct Moments { float n, mean, m2; };
-// (both may be empty)
+// (both may be empty; the weight of b is good for 2^-22 of itself, which is 2^-22 of the distance between the means)
 __device__ __forceinline__ Moments merged(Moments a, Moments b) {
-    const float n = a.n + b.n, d = b.mean - a.mean, w = n > 0.f ? b.n / n : 0.f;
+    const float n = a.n + b.n, d = b.mean - a.mean, w = n > 0.f ? b.n * __builtin_amdgcn_rcpf(n) : 0.f;
     return Moments{n, __builtin_fmaf(d, w, a.mean), a.m2 + b.m2 + d * d * (a.n * w)};
 }
+// over T neighbouring lanes (a power of two up to 64), in all of them
+__device__ __forceinline__ Moments merged_lanes(Moments t, int T) {
+    for (int x = 1; x < T; x *= 2) {
+        Moments o{__shfl_xor(t.n, x), __shfl_xor(t.mean, x), __shfl_xor(t.m2, x)};
+        t = (threadIdx.x & x) ? merged(o, t) : merged(t, o);     // the same order in both lanes: the same bits
+    }
+    return t;
+}
 
+__device__ __forceinline__ float silu_of(float x, float) { return silu_f(x); }
+__device__ __forceinline__ float silu_of(float x, bf16_t) {      // rounded to bf16 behind: two transcendentals
+    return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
+}
 template <typename T> __device__ __forceinline__ float activated(float x, int act) {
     if (act == 1) return gelu_of(x, T{});
-    if (act == 2) return silu_f(x);
+    if (act == 2) return silu_of(x, T{});
     return x;
 }
 
@@ -49,12 +61,14 @@ __device__ __forceinline__ void store_channels(T* p, const float (&v)[V]) {
 }
 
 // PHASE 0: moments of the chunk's groups to a.part; 1: moments of all chunks from a.part, then the result; 2: both, one chunk.
-// 256 threads: `lanes` threads side by side hold the slice's channels, V each, 256 / lanes positions at a time; a slice of more than
-// 256 * V channels is walked in columns of 256 * V.
+// 256 threads: `lanes` threads side by side hold the slice's channels, V each, 256 / lanes positions at a time (rows); a slice of more
+// than 256 * V channels is walked in columns of 256 * V.  A thread keeps a running mean and M2 of each of its channels; they meet in
+// LDS, where `team` threads per group merge its rows x channels.
 template <typename T, int V, int PHASE>
 __global__ void __launch_bounds__(256)
 group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
-    __shared__ Moments sums[256 * V];
+    constexpr int U = 4;                                 // positions in flight per thread
+    __shared__ float2 sums[PHASE == 1 ? 1 : 256 * V];    // mean, M2
     __shared__ float2 stats[GROUP_NORM_SLICE_GROUPS];    // mean, 1 / sqrt(var + eps)
     const int chunk = blockIdx.x % p.chunks, slice = blockIdx.x / p.chunks % p.slices, b = blockIdx.x / (p.chunks * p.slices);
     const int cpg = a.channels / a.groups, g0 = slice * p.slice_groups, ng = min(p.slice_groups, a.groups - g0);
@@ -63,62 +77,75 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
     const int lanes = min(vecs, 256), rows = 256 / lanes;
     const int my = threadIdx.x % lanes, myrow = threadIdx.x / lanes;
     const bool active = myrow < rows;
+    int team = 64;                                       // threads per group
+    while (team * ng > 256) team /= 2;
+    const int tg = threadIdx.x / team, tl = threadIdx.x & (team - 1);
     const T* x = (const T*)a.x + b * a.x_batch + c0;
     T* o = (T*)a.out + b * a.o_batch + c0;
 
+    Moments t{0.f, 0.f, 0.f};                            // of group tg
     if constexpr (PHASE != 1) {
-        for (int g = threadIdx.x; g < ng; g += 256) stats[g] = make_float2(0.f, 0.f);
-        Moments of_group{0.f, 0.f, 0.f};                 // thread g: of group g, over the columns so far
         for (int col = 0; col < vecs; col += lanes) {
-            Moments t[V];
+            float mean[V], m2[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) t[i] = Moments{0.f, 0.f, 0.f};
+            for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.f;
             if (active && col + my < vecs) {
+                const T* q = x + (col + my) * V;
                 float n = 0.f;
-                for (int s = s0 + myrow; s < s1; s += rows) {
-                    float v[V];
-                    load_channels<T, V>(x + s * a.x_position + (col + my) * V, v);
+                auto take = [&](const float (&v)[V]) {
                     n += 1.f;
-                    const float r = 1.0f / n;
+                    const float r = __builtin_amdgcn_rcpf(n);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float d = v[i] - t[i].mean;
-                        t[i].mean = __builtin_fmaf(d, r, t[i].mean);
-                        t[i].m2 = __builtin_fmaf(d, v[i] - t[i].mean, t[i].m2);
+                        const float d = v[i] - mean[i];
+                        mean[i] = __builtin_fmaf(d, r, mean[i]);
+                        m2[i] = __builtin_fmaf(d, v[i] - mean[i], m2[i]);
                     }
-                }
+                };
+                int s = s0 + myrow;
+                for (; s + (U - 1) * rows < s1; s += U * rows) {
+                    float v[U][V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[i].n = n;
+                    for (int u = 0; u < U; ++u) load_channels<T, V>(q + (s + u * rows) * a.x_position, v[u]);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) take(v[u]);
+                }
+                for (; s < s1; s += rows) {
+                    float v[V];
+                    load_channels<T, V>(q + s * a.x_position, v);
+                    take(v);
+                }
             }
-            __syncthreads();
+            if (col > 0) __syncthreads();
             if (active) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) sums[myrow * lanes * V + my * V + i] = t[i];
+                for (int i = 0; i < V; ++i) sums[(myrow * lanes + my) * V + i] = make_float2(mean[i], m2[i]);
             }
             __syncthreads();
-            // group g's channels within this column, all rows, in order
-            for (int g = threadIdx.x; g < ng; g += 256) {
-                const int from = max(g * cpg - col * V, 0), to = min((g + 1) * cpg - col * V, lanes * V);
-                for (int c = from; c < to; ++c)
-                    for (int r = 0; r < rows; ++r) of_group = merged(of_group, sums[r * lanes * V + c]);
+            // the group's channels within this column, rows inside
+            if (tg < ng) {
+                const int from = max(tg * cpg - col * V, 0), to = min((tg + 1) * cpg - col * V, lanes * V), items = (to - from) * rows;
+                for (int e = tl; e < items; e += team) {
+                    const int c = e / rows, r = e - c * rows;
+                    const int n = (s1 - s0 - r + rows - 1) / rows;
+                    const float2 w = sums[r * lanes * V + from + c];
+                    if (n > 0) t = merged(t, Moments{(float)n, w.x, w.y});
+                }
             }
         }
-        for (int g = threadIdx.x; g < ng; g += 256) {
-            if constexpr (PHASE == 0) a.part[((long)b * a.groups + g0 + g) * p.chunks + chunk] = make_float2(of_group.mean, of_group.m2);
-            else stats[g] = make_float2(of_group.mean, 1.0f / sqrtf(of_group.m2 / of_group.n + a.eps));
-        }
-        if constexpr (PHASE == 0) return;
-    } else {
-        for (int g = threadIdx.x; g < ng; g += 256) {
-            Moments t{0.f, 0.f, 0.f};
-            for (int k = 0; k < p.chunks; ++k) {
-                const float2 w = a.part[((long)b * a.groups + g0 + g) * p.chunks + k];
-                const long n = (long)a.positions * (k + 1) / p.chunks - (long)a.positions * k / p.chunks;
-                t = merged(t, Moments{(float)(n * cpg), w.x, w.y});
-            }
-            stats[g] = make_float2(t.mean, 1.0f / sqrtf(t.m2 / t.n + a.eps));
+    } else if (tg < ng) {
+        for (int k = tl; k < p.chunks; k += team) {
+            const float2 w = a.part[((long)b * a.groups + g0 + tg) * p.chunks + k];
+            const int n = (int)((long)a.positions * (k + 1) / p.chunks) - (int)((long)a.positions * k / p.chunks);
+            t = merged(t, Moments{(float)n * (float)cpg, w.x, w.y});
         }
     }
+    t = merged_lanes(t, team);
+    if constexpr (PHASE == 0) {
+        if (tg < ng && tl == 0) a.part[((long)b * a.groups + g0 + tg) * p.chunks + chunk] = make_float2(t.mean, t.m2);
+        return;
+    }
+    if (tg < ng && tl == 0) stats[tg] = make_float2(t.mean, 1.0f / sqrtf(t.m2 / t.n + a.eps));
     __syncthreads();
     if (!active) return;
     for (int col = my; col < vecs; col += lanes) {
@@ -131,12 +158,23 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
             mul[i] = st.y * (a.gamma ? a.gamma[c0 + c] : 1.f);
             add[i] = a.beta ? a.beta[c0 + c] : 0.f;
         }
-        for (int s = s0 + myrow; s < s1; s += rows) {
-            float v[V];
-            load_channels<T, V>(x + s * a.x_position + col * V, v);
+        auto put = [&](float (&v)[V], int s) {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = activated<T>(__builtin_fmaf(v[i] - mean[i], mul[i], add[i]), a.act);
             store_channels<T, V>(o + s * a.o_position + col * V, v);
+        };
+        int s = s0 + myrow;
+        for (; s + (U - 1) * rows < s1; s += U * rows) {
+            float v[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) load_channels<T, V>(x + (s + u * rows) * a.x_position + col * V, v[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) put(v[u], s + u * rows);
+        }
+        for (; s < s1; s += rows) {
+            float v[V];
+            load_channels<T, V>(x + s * a.x_position + col * V, v);
+            put(v, s);
         }
     }
 }
