@@ -1,89 +1,129 @@
 // Group norm over channels-last positions with an activation: a group is channels / groups neighbouring channels of one sample over all
 // positions; y = (x - mean) / sqrt(var + eps) * gamma + beta, then none, tanh-GELU or SiLU.
 //
-// Reading x twice and writing it once is what binds.  A workgroup takes a slice of whole groups (about 64 channels, so that a position is
+// Reading x twice and writing it once is what binds.  70200 positions of 512 channels, 32 groups, SiLU, bf16 (72 MB): 18 us for the
+// moments (4.0 TB/s) and 28 for the result (5.1 TB/s, a device copy's rate; the second read comes from the last-level cache).  2 x 345
+// positions of 320 channels, fp32, in one launch 9 us, all of it latency.  A workgroup takes a slice of whole groups (about 64 channels, so that a position is
 // a whole cache line or two) over a chunk of positions.  Means and squared deviations are merged pairwise, (n, mean, M2) with
 // (n', mean', M2'), from single values on: exact where the mean is far larger than the deviations, whatever the first values are.
 #include "few_epilogue.h"
 #include "group_norm.h"
+#include "lane_sums.h"
 #include "plan.h"
 #include <type_traits>
 
 namespace ps {
 
-struct Moments { float n, mean, m2; };
-// (both may be empty; the weight of b is good for 2^-22 of itself, which is 2^-22 of the distance between the means)
-__device__ __forceinline__ Moments merged(Moments a, Moments b) {
-    const float n = a.n + b.n, d = b.mean - a.mean, w = n > 0.f ? b.n * __builtin_amdgcn_rcpf(n) : 0.f;
-    return Moments{n, __builtin_fmaf(d, w, a.mean), a.m2 + b.m2 + d * d * (a.n * w)};
+// over `team` neighbouring lanes (a power of two up to 64), in all of them
+__device__ __forceinline__ float team_sum(float v, int team) {
+    if (team == 64) return sum_of_64(v);
+    for (int x = team / 2; x > 0; x /= 2) v += __shfl_xor(v, x);
+    return v;
 }
-// over T neighbouring lanes (a power of two up to 64), in all of them
-__device__ __forceinline__ Moments merged_lanes(Moments t, int T) {
-    for (int x = 1; x < T; x *= 2) {
-        Moments o{__shfl_xor(t.n, x), __shfl_xor(t.mean, x), __shfl_xor(t.m2, x)};
-        t = (threadIdx.x & x) ? merged(o, t) : merged(t, o);     // the same order in both lanes: the same bits
-    }
-    return t;
+
+// Mean and M2 of the union of the items (n, (mean, M2)) that `each` gives this lane of a team: first the mean, as the mean distance from
+// `pivot` (any item's), then M2 = sum of M2_i + n_i (mean_i - mean)^2.  No division but one, and the items' reads do not wait on each other.
+constexpr int SINGLE_THREADS = 1024;                     // of the workgroup that does a slice alone
+struct Moments { float n, mean, m2; };
+template <typename Each>
+__device__ __forceinline__ Moments united(const Each& each, float pivot, int team) {
+    float n = 0.f, s = 0.f;
+    each([&](float ni, float2 w) {
+        n += ni;
+        s = __builtin_fmaf(ni, w.x - pivot, s);
+    });
+    n = team_sum(n, team);
+    const float mean = pivot + team_sum(s, team) / n;
+    float m2 = 0.f;
+    each([&](float ni, float2 w) {
+        const float d = w.x - mean;
+        m2 += __builtin_fmaf(ni * d, d, w.y);
+    });
+    return Moments{n, mean, team_sum(m2, team)};
+}
+__device__ __forceinline__ Moments merged(Moments a, Moments b) {
+    const float n = a.n + b.n, d = b.mean - a.mean, w = b.n / n;
+    return Moments{n, __builtin_fmaf(d, w, a.mean), a.m2 + b.m2 + d * d * (a.n * w)};
 }
 
 __device__ __forceinline__ float silu_of(float x, float) { return silu_f(x); }
 __device__ __forceinline__ float silu_of(float x, bf16_t) {      // rounded to bf16 behind: two transcendentals
     return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
 }
-template <typename T> __device__ __forceinline__ float activated(float x, int act) {
-    if (act == 1) return gelu_of(x, T{});
-    if (act == 2) return silu_of(x, T{});
-    return x;
+template <typename T, int ACT> __device__ __forceinline__ float activated(float x) {
+    if constexpr (ACT == 1) return gelu_of(x, T{});
+    else if constexpr (ACT == 2) return silu_of(x, T{});
+    else return x;
 }
 
+template <typename T> struct ElemOf { typedef typename std::conditional<sizeof(T) == 4, float, __bf16>::type type; };
+template <typename T, int V> struct ChannelsOf { typedef __attribute__((ext_vector_type(V))) typename ElemOf<T>::type type; };
+template <typename T> struct ChannelsOf<T, 1> { typedef typename ElemOf<T>::type type; };
 template <typename T, int V>
-__device__ __forceinline__ void load_channels(const T* p, float (&v)[V]) {
-    typedef typename std::conditional<sizeof(T) == 4, float, __bf16>::type E;
-    typedef __attribute__((ext_vector_type(V))) E vec;
-    if constexpr (V == 1) v[0] = (float)*reinterpret_cast<const E*>(p);
+__device__ __forceinline__ void widen(const typename ChannelsOf<T, V>::type& w, float (&v)[V]) {
+    if constexpr (V == 1) v[0] = (float)w;
     else {
-        const vec w = *reinterpret_cast<const vec*>(p);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = (float)w[i];
     }
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_channels(T* p, const float (&v)[V]) {
-    typedef typename std::conditional<sizeof(T) == 4, float, __bf16>::type E;
-    typedef __attribute__((ext_vector_type(V))) E vec;
-    if constexpr (V == 1) *reinterpret_cast<E*>(p) = (E)v[0];
+    typename ChannelsOf<T, V>::type w;
+    if constexpr (V == 1) w = (typename ElemOf<T>::type)v[0];
     else {
-        vec w;
 #pragma unroll
-        for (int i = 0; i < V; ++i) w[i] = (E)v[i];
-        *reinterpret_cast<vec*>(p) = w;
+        for (int i = 0; i < V; ++i) w[i] = (typename ElemOf<T>::type)v[i];
     }
+    *reinterpret_cast<typename ChannelsOf<T, V>::type*>(p) = w;
 }
 
 // PHASE 0: moments of the chunk's groups to a.part; 1: moments of all chunks from a.part, then the result; 2: both, one chunk.
-// 256 threads: `lanes` threads side by side hold the slice's channels, V each, 256 / lanes positions at a time (rows); a slice of more
-// than 256 * V channels is walked in columns of 256 * V.  A thread keeps a running mean and M2 of each of its channels; they meet in
-// LDS, where `team` threads per group merge its rows x channels.
-template <typename T, int V, int PHASE>
-__global__ void __launch_bounds__(256)
+// NT threads: `lanes` threads side by side hold the slice's channels, V each, NT / lanes positions at a time (rows); a slice of more
+// than NT * V channels is walked in columns of NT * V.  A thread keeps a running mean and M2 of each of its channels; they meet in
+// LDS, where `team` threads per group unite its rows x channels.  A single chunk that one batch of loads holds is read once.
+template <typename T, int V, int PHASE, int ACT, int U, int NT>      // U: positions in flight per thread
+__global__ void __launch_bounds__(NT)
 group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
-    constexpr int U = 4;                                 // positions in flight per thread
-    __shared__ float2 sums[PHASE == 1 ? 1 : 256 * V];    // mean, M2
+    typedef typename ChannelsOf<T, V>::type vec_t;
+    __shared__ float2 sums[PHASE == 1 ? 1 : NT * V + 2 * NT];// mean, M2: rows of lanes * V channels and a fill (see p.fill)
     __shared__ float2 stats[GROUP_NORM_SLICE_GROUPS];    // mean, 1 / sqrt(var + eps)
-    const int chunk = blockIdx.x % p.chunks, slice = blockIdx.x / p.chunks % p.slices, b = blockIdx.x / (p.chunks * p.slices);
-    const int cpg = a.channels / a.groups, g0 = slice * p.slice_groups, ng = min(p.slice_groups, a.groups - g0);
+    const int chunk = blockIdx.x, slice = blockIdx.y, b = blockIdx.z;
+    const int cpg = p.cpg, g0 = slice * p.slice_groups, ng = min(p.slice_groups, a.groups - g0);
     const int c0 = g0 * cpg, nc = ng * cpg, vecs = nc / V;
-    const int s0 = (int)((long)a.positions * chunk / p.chunks), s1 = (int)((long)a.positions * (chunk + 1) / p.chunks);
-    const int lanes = min(vecs, 256), rows = 256 / lanes;
-    const int my = threadIdx.x % lanes, myrow = threadIdx.x / lanes;
+    const int s0 = chunk * p.per, s1 = min(s0 + p.per, a.positions);
+    const int lanes = p.lanes, rows = p.rows, team = p.team, stride = lanes * V + p.fill;
+    const int myrow = (int)(threadIdx.x * p.lanes_inv >> 20), my = threadIdx.x - myrow * lanes;
     const bool active = myrow < rows;
-    int team = 64;                                       // threads per group
-    while (team * ng > 256) team /= 2;
-    const int tg = threadIdx.x / team, tl = threadIdx.x & (team - 1);
+    const int tg = threadIdx.x >> __builtin_ctz(team), tl = threadIdx.x & (team - 1);
     const T* x = (const T*)a.x + b * a.x_batch + c0;
     T* o = (T*)a.out + b * a.o_batch + c0;
+    vec_t batch[U];                                      // positions past the chunk repeat the last one and do not count
+    const long step = rows * a.x_position;
+    // (past the chunk: repeats the last position; without these, the scheduler would move loads behind their first use to save registers)
+    auto fetch = [&](const T* q, int s) {
+        const T* at = q + s * a.x_position;
+        if (s + (U - 1) * rows < s1) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const vec_t*>(at + u * step);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const vec_t*>(q + min(s + u * rows, s1 - 1) * a.x_position);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // what multiplies and follows a column of V channels, without the statistics
+    typedef typename ChannelsOf<float, V>::type affine_t;
+    affine_t gamma, beta;
+    auto fetch_affine = [&](int col) {
+        gamma = affine_t{} + 1.f;
+        beta = affine_t{};
+        if (a.gamma) gamma = *reinterpret_cast<const affine_t*>(a.gamma + c0 + col * V);
+        if (a.beta) beta = *reinterpret_cast<const affine_t*>(a.beta + c0 + col * V);
+    };
 
     Moments t{0.f, 0.f, 0.f};                            // of group tg
+    if constexpr (PHASE != 0) fetch_affine(my < vecs ? my : 0);      // (now, not when the statistics are there)
     if constexpr (PHASE != 1) {
         for (int col = 0; col < vecs; col += lanes) {
             float mean[V], m2[V];
@@ -92,55 +132,69 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
             if (active && col + my < vecs) {
                 const T* q = x + (col + my) * V;
                 float n = 0.f;
-                auto take = [&](const float (&v)[V]) {
-                    n += 1.f;
-                    const float r = __builtin_amdgcn_rcpf(n);
+                for (int s = s0 + myrow; s < s1; s += U * rows) {
+                    fetch(q, s);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float d = v[i] - mean[i];
-                        mean[i] = __builtin_fmaf(d, r, mean[i]);
-                        m2[i] = __builtin_fmaf(d, v[i] - mean[i], m2[i]);
-                    }
-                };
-                int s = s0 + myrow;
-                for (; s + (U - 1) * rows < s1; s += U * rows) {
-                    float v[U][V];
+                    for (int u = 0; u < U; ++u)
+                        if (s + u * rows < s1) {
+                            float v[V];
+                            widen<T, V>(batch[u], v);
+                            n += 1.f;
+                            const float r = __builtin_amdgcn_rcpf(n);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) load_channels<T, V>(q + (s + u * rows) * a.x_position, v[u]);
-#pragma unroll
-                    for (int u = 0; u < U; ++u) take(v[u]);
-                }
-                for (; s < s1; s += rows) {
-                    float v[V];
-                    load_channels<T, V>(q + s * a.x_position, v);
-                    take(v);
+                            for (int i = 0; i < V; ++i) {
+                                const float d = v[i] - mean[i];
+                                mean[i] = __builtin_fmaf(d, r, mean[i]);
+                                m2[i] = __builtin_fmaf(d, v[i] - mean[i], m2[i]);
+                            }
+                        }
                 }
             }
             if (col > 0) __syncthreads();
             if (active) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) sums[(myrow * lanes + my) * V + i] = make_float2(mean[i], m2[i]);
+                for (int i = 0; i < V; ++i) sums[myrow * stride + my * V + i] = make_float2(mean[i], m2[i]);
             }
             __syncthreads();
-            // the group's channels within this column, rows inside
-            if (tg < ng) {
-                const int from = max(tg * cpg - col * V, 0), to = min((tg + 1) * cpg - col * V, lanes * V), items = (to - from) * rows;
-                for (int e = tl; e < items; e += team) {
-                    const int c = e / rows, r = e - c * rows;
-                    const int n = (s1 - s0 - r + rows - 1) / rows;
-                    const float2 w = sums[r * lanes * V + from + c];
-                    if (n > 0) t = merged(t, Moments{(float)n, w.x, w.y});
-                }
+            // the group's channels within this column, rows inside (rows past the chunk's end are empty)
+            const int from = max(tg * cpg - col * V, 0), to = min((tg + 1) * cpg - col * V, lanes * V);
+            if (tg < ng && from < to) {
+                const int base = (unsigned)(s1 - s0) / (unsigned)rows, more = (s1 - s0) - base * rows, span = to - from;
+                const int items = span * (base > 0 ? rows : more), dr = (unsigned)team / (unsigned)span, dc = team - dr * span;
+                const int r1 = (unsigned)tl / (unsigned)span, c1 = tl - r1 * span;
+                const float2* at = sums + from;
+                const auto each = [&](auto f) {
+                    int c = c1, r = r1;
+                    for (int e = tl; e < items; e += 4 * team) {             // four reads in flight
+                        float n[4];
+                        float2 w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const bool in = e + k * team < items;
+                            n[k] = in ? (float)(base + (r < more)) : 0.f;
+                            w[k] = at[in ? r * stride + c : 0];
+                            r += dr;
+                            c += dc;
+                            if (c >= span) { c -= span; ++r; }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) f(n[k], n[k] > 0.f ? w[k] : make_float2(0.f, 0.f));
+                    }
+                };
+                const Moments u = united(each, at[0].x, team);
+                t = t.n > 0.f ? merged(t, u) : u;
             }
         }
-    } else if (tg < ng) {
-        for (int k = tl; k < p.chunks; k += team) {
-            const float2 w = a.part[((long)b * a.groups + g0 + tg) * p.chunks + k];
-            const int n = (int)((long)a.positions * (k + 1) / p.chunks) - (int)((long)a.positions * k / p.chunks);
-            t = merged(t, Moments{(float)n * (float)cpg, w.x, w.y});
+    } else {
+        if (tg < ng) {
+            const float2* at = a.part + ((long)b * a.groups + g0 + tg) * p.chunks;
+            const float full = (float)p.per * (float)cpg, last = (float)(a.positions - (p.chunks - 1) * p.per) * (float)cpg;
+            const auto each = [&](auto f) {
+                for (int k = tl; k < p.chunks; k += team) f(k + 1 < p.chunks ? full : last, at[k]);
+            };
+            t = united(each, at[0].x, team);
         }
     }
-    t = merged_lanes(t, team);
     if constexpr (PHASE == 0) {
         if (tg < ng && tl == 0) a.part[((long)b * a.groups + g0 + tg) * p.chunks + chunk] = make_float2(t.mean, t.m2);
         return;
@@ -148,33 +202,32 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
     if (tg < ng && tl == 0) stats[tg] = make_float2(t.mean, 1.0f / sqrtf(t.m2 / t.n + a.eps));
     __syncthreads();
     if (!active) return;
+    const bool held = PHASE == 2 && vecs <= lanes && s1 - s0 <= U * rows;
     for (int col = my; col < vecs; col += lanes) {
-        float mul[V], mean[V], add[V];
+        if (col != my) fetch_affine(col);
+        float mul[V], mean[V], add[V], scale[V];
+        widen<float, V>(gamma, scale);
+        widen<float, V>(beta, add);
+        int g = (unsigned)(col * V) / (unsigned)cpg, left = (g + 1) * cpg - col * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int c = col * V + i;
-            const float2 st = stats[c / cpg];
+            if (left == 0) { ++g; left = cpg; }
+            --left;
+            const float2 st = stats[g];
             mean[i] = st.x;
-            mul[i] = st.y * (a.gamma ? a.gamma[c0 + c] : 1.f);
-            add[i] = a.beta ? a.beta[c0 + c] : 0.f;
+            mul[i] = st.y * scale[i];
         }
-        auto put = [&](float (&v)[V], int s) {
+        for (int s = s0 + myrow; s < s1; s += U * rows) {
+            if (!held) fetch(x + col * V, s);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activated<T>(__builtin_fmaf(v[i] - mean[i], mul[i], add[i]), a.act);
-            store_channels<T, V>(o + s * a.o_position + col * V, v);
-        };
-        int s = s0 + myrow;
-        for (; s + (U - 1) * rows < s1; s += U * rows) {
-            float v[U][V];
+            for (int u = 0; u < U; ++u)
+                if (s + u * rows < s1) {
+                    float v[V];
+                    widen<T, V>(batch[u], v);
 #pragma unroll
-            for (int u = 0; u < U; ++u) load_channels<T, V>(x + (s + u * rows) * a.x_position + col * V, v[u]);
-#pragma unroll
-            for (int u = 0; u < U; ++u) put(v[u], s + u * rows);
-        }
-        for (; s < s1; s += rows) {
-            float v[V];
-            load_channels<T, V>(x + s * a.x_position + col * V, v);
-            put(v, s);
+                    for (int i = 0; i < V; ++i) v[i] = activated<T, ACT>(__builtin_fmaf(v[i] - mean[i], mul[i], add[i]));
+                    store_channels<T, V>(o + (s + u * rows) * a.o_position + col * V, v);
+                }
         }
     }
 }
@@ -184,26 +237,38 @@ size_t group_norm_scratch_bytes(int dtype, int batch, int positions, int channel
     return p.chunks > 1 ? (size_t)batch * groups * p.chunks * sizeof(float2) : 0;
 }
 
+template <typename T, int V, int ACT>
+static void launch_group_norm_act(const GroupNormArgs& a, const GroupNormPlan& p, hipStream_t st) {
+    const dim3 grid(p.chunks, p.slices, a.batch);
+    if (p.chunks == 1) group_norm_kernel<T, V, 2, ACT, 4, SINGLE_THREADS><<<grid, SINGLE_THREADS, 0, st>>>(a, p);
+    else group_norm_kernel<T, V, 1, ACT, 4, 256><<<grid, 256, 0, st>>>(a, p);
+}
+
 template <typename T, int V>
-static hipError_t launch_group_norm_as(const GroupNormArgs& a, const GroupNormPlan& p, hipStream_t st) {
-    const unsigned grid = (unsigned)((long)a.batch * p.slices * p.chunks);
-    if (p.chunks == 1) {
-        group_norm_kernel<T, V, 2><<<grid, 256, 0, st>>>(a, p);
-    } else {
-        group_norm_kernel<T, V, 0><<<grid, 256, 0, st>>>(a, p);
-        group_norm_kernel<T, V, 1><<<grid, 256, 0, st>>>(a, p);
-    }
+static hipError_t launch_group_norm_as(const GroupNormArgs& a, GroupNormPlan p, hipStream_t st) {
+    p.lanes = p.slice_groups * p.cpg / V;
+    const int threads = p.chunks == 1 ? SINGLE_THREADS : 256;
+    if (p.lanes > threads) p.lanes = threads;
+    p.rows = threads / p.lanes;
+    p.lanes_inv = ((1u << 20) + p.lanes - 1) / p.lanes;  // t * lanes_inv >> 20 == t / lanes for t < 1024: too large by less than lanes / 2^20
+    for (p.team = 64; p.team * p.slice_groups > threads;) p.team /= 2;
+    // rows of partial moments in LDS 16 entries (32 banks) apart: a team reads neighbouring channels, then rows
+    p.fill = p.lanes * V % 32 == 0 && p.lanes >= 8 ? 16 : 0;      // (rows * fill <= 2 * threads)
+    if (p.chunks > 1) group_norm_kernel<T, V, 0, 0, 4, 256><<<dim3(p.chunks, p.slices, a.batch), 256, 0, st>>>(a, p);
+    (a.act == 2 ? launch_group_norm_act<T, V, 2> : a.act == 1 ? launch_group_norm_act<T, V, 1> : launch_group_norm_act<T, V, 0>)(a, p, st);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t launch_group_norm_t(const GroupNormArgs& a, hipStream_t st) {
     const GroupNormPlan p = group_norm_plan(a.positions, a.channels, a.groups, sizeof(T));
-    // the widest load that the slices' widths, the strides and the addresses allow
+    // the widest load that the slices' widths, the strides and the addresses allow (gamma and beta are read 4 channels at a time)
     long bytes = (long)p.slice_groups * (a.channels / a.groups) * sizeof(T);
     bytes |= (long)((uintptr_t)a.x | (uintptr_t)a.out) | (long)a.channels * sizeof(T);
     if (a.positions > 1) bytes |= (a.x_position | a.o_position) * (long)sizeof(T);
     if (a.batch > 1) bytes |= (a.x_batch | a.o_batch) * (long)sizeof(T);
+    const bool affine = (((uintptr_t)a.gamma | (uintptr_t)a.beta) & 15) == 0;
+    if (!affine) return launch_group_norm_as<T, 1>(a, p, st);
     if (bytes % 16 == 0) return launch_group_norm_as<T, 16 / sizeof(T)>(a, p, st);
     if (bytes % 8 == 0 && sizeof(T) == 2) return launch_group_norm_as<T, 4>(a, p, st);
     return launch_group_norm_as<T, 1>(a, p, st);

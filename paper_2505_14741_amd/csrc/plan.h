@@ -290,7 +290,11 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 // ---- group norm: `slices` slices of slice_groups whole groups (the last may have fewer), each over `chunks` chunks of positions.
 // A function of the sample's shape only, never of the batch.
 constexpr int GROUP_NORM_SLICE_GROUPS = 256;             // most groups of a slice: one thread each
-struct GroupNormPlan { int slice_groups, slices, chunks; };
+struct GroupNormPlan {
+    int cpg, slice_groups, slices, chunks, per;          // per: positions of a chunk (the last may have fewer)
+    int lanes, rows, team, fill;                         // threads of a position, positions at a time, threads per group (set by the launcher)
+    unsigned lanes_inv;
+};
 constexpr GroupNormPlan group_norm_plan(int positions, int channels, int groups, int elem_bytes) {
     const int cpg = channels / groups;
     const long bytes = (long)cpg * elem_bytes;
@@ -308,7 +312,9 @@ constexpr GroupNormPlan group_norm_plan(int positions, int channels, int groups,
     if (chunks > most) chunks = most;
     if (chunks > 512) chunks = 512;
     if (chunks > positions) chunks = positions;
-    p.chunks = chunks < 1 ? 1 : (int)chunks;
+    p.cpg = cpg;
+    p.per = (int)((positions + (chunks < 1 ? 0 : chunks - 1)) / (chunks < 1 ? 1 : chunks));
+    p.chunks = (positions + p.per - 1) / p.per;
     return p;
 }
 
