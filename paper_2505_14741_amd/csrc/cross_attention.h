@@ -15,7 +15,7 @@ struct CrossArgs {
     float scale;
     AttnStrides s;
     float* part;                  // scratch of cross_workspace_bytes()
-    int row_blocks, nsplit;       // (set by the launcher)
+    int nsplit;                   // (set by the launcher)
 };
 size_t cross_workspace_bytes(int dtype, const CrossArgs& a);
 hipError_t launch_cross_attention(int dtype, CrossArgs a, hipStream_t st);

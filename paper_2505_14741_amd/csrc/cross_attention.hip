@@ -8,6 +8,7 @@
 // Keys that do not count get a score of -infinity, and their V rows are zeros in LDS: what lies there is never multiplied.
 #include "cross_attention.h"
 #include "lane_sums.h"
+#include "plan.h"
 #include "tile_ops.h"
 
 namespace ps {
@@ -25,19 +26,23 @@ __device__ __forceinline__ unsigned long long cross_counts(const CrossArgs& a, i
     return __ballot(in);
 }
 
-// workgroup id -> sample, key/value head, block of rows and share of the keys
+// Grid: (key/value head, piece of the keys, block of rows) in x, heads innermost, since a token's heads are neighbours in memory; samples in z.
 struct CrossItem { int b, g, block, piece; };
-__device__ __forceinline__ CrossItem cross_item(const CrossArgs& a, int id) {
+__device__ __forceinline__ CrossItem cross_item(const CrossArgs& a) {
     CrossItem t;
-    t.piece = id % a.nsplit; id /= a.nsplit;
-    t.block = id % a.row_blocks; id /= a.row_blocks;
-    t.g = id % a.kv_heads;
-    t.b = id / a.kv_heads;
+    const unsigned id = blockIdx.x;
+    unsigned of_head = id / (unsigned)a.kv_heads;
+    t.g = (int)(id - of_head * a.kv_heads);
+    t.piece = 0;
+    if (a.nsplit > 1) { const unsigned q = of_head / (unsigned)a.nsplit; t.piece = (int)(of_head - q * a.nsplit); of_head = q; }
+    t.block = (int)of_head;
+    t.b = blockIdx.z;
     return t;
 }
-// offset of a row in q (tok, head) and in o
+// offset of a row in q or o
 __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, long tok, long head) {
-    const int t = row / a.share;
+    if (a.share == 1) return row * tok + g * head;
+    const int t = (unsigned)row / (unsigned)a.share;
     return t * tok + (long)(g * a.share + (row - t * a.share)) * head;
 }
 
@@ -59,6 +64,36 @@ __device__ __forceinline__ s16x4_t read_tr16(const bf16_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
 }
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+// acc + the sum of eight bf16 values
+__device__ __forceinline__ float add_bf16x8(bf16x8_t p, float acc) {
+    const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 0, 1), ones, acc, false);
+    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 2, 3), ones, acc, false);
+    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 4, 5), ones, acc, false);
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 6, 7), ones, acc, false);
+}
+
+// Stores a row's outputs (16 d blocks of 4 values a lane): lanes of neighbouring kgrp swap quads of two blocks, so that each has 8
+// adjacent values and the four lanes of a row write 64 bytes.
+template <int NB>
+__device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB], float inv, int kgrp, bool in) {
+    if constexpr (NB == 1) {
+        if (in) *reinterpret_cast<bf16x4_t*>(row + kgrp * 4) = __builtin_convertvector(acc[0] * inv, bf16x4_t);
+    } else {
+#pragma unroll
+        for (int d = 0; d < NB; d += 2) {
+            typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
+            const u32x2_t x = __builtin_bit_cast(u32x2_t, __builtin_convertvector(acc[d] * inv, bf16x4_t));
+            const u32x2_t y = __builtin_bit_cast(u32x2_t, __builtin_convertvector(acc[d + 1] * inv, bf16x4_t));
+            const auto lo = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false), hi = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+            // even kgrp: block d, values 4 kgrp .. + 7; odd: block d + 1, values 4 (kgrp - 1) .. + 7
+            if (in) *reinterpret_cast<i32x4_t*>(row + (d + (kgrp & 1)) * 16 + (kgrp & 2) * 4) = i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+        }
+    }
+}
+
 template <int HD, int QT>
 __global__ void __launch_bounds__(256, 2)
 cross_bf16_kernel(CrossArgs a) {
@@ -67,13 +102,40 @@ cross_bf16_kernel(CrossArgs a) {
     constexpr int LOADS = (KT * CH + 255) / 256;
     __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * LD], Vs[KT * LD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
-    const CrossItem it = cross_item(a, xcd_remap(blockIdx.x, gridDim.x));
+    const CrossItem it = cross_item(a);
     const bf16_t* kb = (const bf16_t*)a.k + it.b * a.s.k_batch + it.g * a.s.k_head;
     const bf16_t* vb = (const bf16_t*)a.v + it.b * a.s.v_batch + it.g * a.s.v_head;
     const int keys = cross_keys(a, it.b), tiles = (keys + KT - 1) / KT;
-    const int j0 = (int)((long)tiles * it.piece / a.nsplit), j1 = (int)((long)tiles * (it.piece + 1) / a.nsplit);
+    int j0 = 0, j1 = tiles;
+    if (a.nsplit > 1) { j0 = (int)((long)tiles * it.piece / a.nsplit); j1 = (int)((long)tiles * (it.piece + 1) / a.nsplit); }
     const int r0 = it.block * BQ + wave * QT * 16 + l16;
     const float c = a.scale * CROSS_LOG2E, ahead = CROSS_AHEAD / c;
+
+    typedef __attribute__((ext_vector_type(4))) int chunk_t;
+    chunk_t kn[LOADS], vn[LOADS];                        // the next tile; rows past the end are zeros
+    int at[LOADS];                                       // row of the tile
+    long koff[LOADS], voff[LOADS];
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+        const int e = threadIdx.x + 256 * u;
+        at[u] = e / CH;
+        koff[u] = at[u] * a.s.k_tok + e % CH * 8;
+        voff[u] = at[u] * a.s.v_tok + e % CH * 8;
+    }
+    auto fetch = [&](int kv0) {
+        const bf16_t *kt = kb + kv0 * a.s.k_tok, *vt = vb + kv0 * a.s.v_tok;
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            if (kv0 + KT > keys || KT * CH % 256) {
+                kn[u] = vn[u] = chunk_t{0, 0, 0, 0};
+                if (at[u] >= KT || kv0 + at[u] >= keys) continue;
+            }
+            kn[u] = *reinterpret_cast<const chunk_t*>(kt + koff[u]);
+            vn[u] = *reinterpret_cast<const chunk_t*>(vt + voff[u]);
+        }
+    };
+    unsigned long long counts_next = j0 < j1 ? cross_counts(a, it.b, j0 * KT, keys, lane) : 0;
+    if (j0 < j1) fetch(j0 * KT);
 
     // queries: second operand of S^T, 8 consecutive d (4 for heads of 16) of row l16; rows past the end repeat the last one
     bf16x8_t qf[QT][QS];
@@ -88,40 +150,29 @@ cross_bf16_kernel(CrossArgs a) {
             for (int s = 0; s < QS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 32 + kgrp * 8);
         }
     }
-
-    typedef __attribute__((ext_vector_type(4))) int chunk_t;
-    chunk_t kn[LOADS], vn[LOADS];                        // the next tile; rows past the end are zeros
-    auto fetch = [&](int kv0) {
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int e = threadIdx.x + 256 * u, r = kv0 + e / CH, d = e % CH * 8;
-            kn[u] = vn[u] = chunk_t{0, 0, 0, 0};
-            if (e < KT * CH && r < keys) {
-                kn[u] = *reinterpret_cast<const chunk_t*>(kb + (long)r * a.s.k_tok + d);
-                vn[u] = *reinterpret_cast<const chunk_t*>(vb + (long)r * a.s.v_tok + d);
-            }
-        }
-    };
     f32x4_t acc[QT][NB];                                 // O^T: row l16, d = 16 * block + 4 * kgrp + i
     float m[QT], l[QT];                                  // l: over this lane's keys only
+    f32x4_t bias[4];                                     // what the scores' sums start from: 0, or -infinity for keys that do not count
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         m[t] = -INFINITY; l[t] = 0.f;
 #pragma unroll
         for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    unsigned long long counts_next = j0 < j1 ? cross_counts(a, it.b, j0 * KT, keys, lane) : 0;
-    if (j0 < j1) fetch(j0 * KT);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) bias[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    bool biased = false;
     for (int j = j0; j < j1; ++j) {
         const unsigned long long counts = counts_next;
+        const bool whole = counts == ~0ull;
         __syncthreads();                                 // nobody reads the last tile any more
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int e = threadIdx.x + 256 * u, r = e / CH;
-            if (e < KT * CH) {
-                *reinterpret_cast<chunk_t*>(Ks + r * LD + e % CH * 8) = kn[u];
-                *reinterpret_cast<chunk_t*>(Vs + r * LD + e % CH * 8) = (counts >> r & 1) ? vn[u] : chunk_t{0, 0, 0, 0};
-            }
+            if (KT * CH % 256 && at[u] >= KT) continue;
+            if (!whole && !(counts >> at[u] & 1)) kn[u] = vn[u] = chunk_t{0, 0, 0, 0};
+            const int off = at[u] * LD + (threadIdx.x + 256 * u) % CH * 8;
+            *reinterpret_cast<chunk_t*>(Ks + off) = kn[u];
+            *reinterpret_cast<chunk_t*>(Vs + off) = vn[u];
         }
         __syncthreads();
         if (j + 1 < j1) {
@@ -129,31 +180,27 @@ cross_bf16_kernel(CrossArgs a) {
             fetch((j + 1) * KT);
         }
         if (counts == 0) continue;                       // (the whole workgroup)
+        if (!whole || biased) {
+            const unsigned long long mine = counts >> (4 * kgrp);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bias[g][i] = (mine >> (16 * g + i) & 1) ? 0.f : -INFINITY;
+            biased = !whole;
+        }
         f32x4_t sc[QT][4];
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
                 if constexpr (HD == 16) {
                     const s16x4_t kf = *reinterpret_cast<const s16x4_t*>(Ks + (g * 16 + l16) * LD + kgrp * 4);
                     const bf16x4_t ql = __builtin_shufflevector(qf[t][0], qf[t][0], 0, 1, 2, 3);
-                    sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(kf, __builtin_bit_cast(s16x4_t, ql), z, 0, 0, 0);
+                    sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(kf, __builtin_bit_cast(s16x4_t, ql), bias[g], 0, 0, 0);
                 } else {
-                    sc[t][g] = cross_scores<HD>(Ks + (g * 16 + l16) * LD + kgrp * 8, qf[t], z);
+                    sc[t][g] = cross_scores<HD>(Ks + (g * 16 + l16) * LD + kgrp * 8, qf[t], bias[g]);
                 }
             }
-        if (counts != ~0ull) {
-            const unsigned long long mine = counts >> (4 * kgrp);
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(mine >> (16 * g + i) & 1)) {
-#pragma unroll
-                        for (int t = 0; t < QT; ++t) sc[t][g][i] = -INFINITY;
-                    }
-        }
         float top[QT];
         bool over = false;
 #pragma unroll
@@ -176,18 +223,18 @@ cross_bf16_kernel(CrossArgs a) {
                 for (int d = 0; d < NB; ++d) acc[t][d] *= alpha;
             }
         }
+        // probabilities are rounded to bf16 for the second product, and summed as rounded: one key alone has weight 1 exactly
         bf16x8_t pf[QT][2];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const float mc = m[t] == -INFINITY ? 0.f : m[t] * c;
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
+            for (int s = 0; s < 2; ++s) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][g][i], c, -mc));
-                    l[t] += p;
-                    pf[t][g >> 1][(g & 1) * 4 + i] = (__bf16)p;
-                }
+                for (int e = 0; e < 8; ++e)
+                    pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc));
+                l[t] = add_bf16x8(pf[t][s], l[t]);
+            }
         }
         // k slot (kgrp, e) of step s is key 32 s + 16 (e / 4) + 4 kgrp + e % 4
 #pragma unroll
@@ -205,12 +252,59 @@ cross_bf16_kernel(CrossArgs a) {
     for (int t = 0; t < QT; ++t) {
         const int row = r0 + t * 16;
         const float sum = sum_xor32(sum_xor16(l[t]));
-        if (row >= a.rows) continue;
-        bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, row, a.s.o_tok, a.s.o_head) + kgrp * 4;
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        if (a.nsplit > 1) {
+            if (row >= a.rows) continue;
+            float* p = a.part + ((((long)it.b * a.kv_heads + it.g) * a.nsplit + it.piece) * a.rows + row) * (HD + 4);
 #pragma unroll
-        for (int d = 0; d < NB; ++d) *reinterpret_cast<bf16x4_t*>(p + d * 16) = __builtin_convertvector(acc[t][d] * inv, bf16x4_t);
+            for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[t][d];
+            if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m[t] * c};
+        } else {
+            bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head);
+            cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : 1.0f / sum, kgrp, row < a.rows);
+        }
     }
+}
+
+// Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = 2^(ref_i - max); a piece without a key that counts has the reference
+// -infinity.  (fp32: references are natural, exponentials as exact as expf.)  A wave takes a row: HD / 4 lanes hold 4 adjacent values each, and
+// the wave's 256 / HD teams of them take a piece each in turn.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256)
+cross_join_kernel(CrossArgs a, long lines) {
+    constexpr int W = HD / 4, TEAMS = 64 / W;
+    const int lane = threadIdx.x & 63, d = lane % W * 4, team = lane / W;
+    const long line = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (line >= lines) return;                           // whole waves
+    const long bg = line / a.rows;
+    const int row = (int)(line - bg * a.rows), b = (int)(bg / a.kv_heads), g = (int)(bg - (long)b * a.kv_heads);
+    const float* p = a.part + (bg * a.nsplit * a.rows + row) * (HD + 4);
+    const long step = (long)a.rows * (HD + 4);
+    float top = -INFINITY;
+    for (int i = lane; i < a.nsplit; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float ref = top == -INFINITY ? 0.f : top;      // (then every weight is zero, and so are the sums)
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll 4
+    for (int i = team; i < a.nsplit; i += TEAMS) {
+        const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
+        const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(s[1] - ref) : expf(s[1] - ref);
+        acc += v * w;
+        l = __builtin_fmaf(s[0], w, l);
+    }
+#pragma unroll
+    for (int x = W; x < 64; x *= 2) {
+        l += __shfl_xor(l, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], x);
+    }
+    if (team != 0) return;
+    acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
+    T* o = (T*)a.o + b * a.s.o_batch + cross_row(a, g, row, a.s.o_tok, a.s.o_head) + d;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(o) = __builtin_convertvector(acc, bf16x4_t);
+    else *reinterpret_cast<f32x4_t*>(o) = acc;
 }
 
 // ------------------------------------------------------------------------------------ fp32
@@ -221,7 +315,7 @@ cross_f32_kernel(CrossArgs a) {
     constexpr int KT = 64, LD = HD + 4, NB = HD / 16, BQ = 64, CH = HD / 4, LOADS = KT * CH / 256;
     __shared__ __attribute__((aligned(16))) float Ks[KT * LD], Vs[KT * LD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
-    const CrossItem it = cross_item(a, xcd_remap(blockIdx.x, gridDim.x));
+    const CrossItem it = cross_item(a);
     const float* kb = (const float*)a.k + it.b * a.s.k_batch + it.g * a.s.k_head;
     const float* vb = (const float*)a.v + it.b * a.s.v_batch + it.g * a.s.v_head;
     const int keys = cross_keys(a, it.b), tiles = (keys + KT - 1) / KT;
@@ -306,22 +400,41 @@ cross_f32_kernel(CrossArgs a) {
     }
     l = sum_xor32(sum_xor16(l));
     if (row >= a.rows) return;
+    if (a.nsplit > 1) {
+        float* p = a.part + ((((long)it.b * a.kv_heads + it.g) * a.nsplit + it.piece) * a.rows + row) * (HD + 4);
+#pragma unroll
+        for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[d];
+        if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{l, m};
+        return;
+    }
     float* p = (float*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, row, a.s.o_tok, a.s.o_head) + kgrp * 4;
 #pragma unroll
     for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16) = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc[d] / l;
 }
 
-size_t cross_workspace_bytes(int, const CrossArgs&) { return 0; }
+static CrossPlan cross_plan_of(int dtype, const CrossArgs& a) {
+    return cross_plan(dtype == PS_BF16, a.rows, a.kv_len, a.kv_heads, a.head_dim, compute_units());
+}
+
+size_t cross_workspace_bytes(int dtype, const CrossArgs& a) {
+    const CrossPlan p = cross_plan_of(dtype, a);
+    return p.nsplit > 1 ? (size_t)a.batch * a.kv_heads * p.nsplit * a.rows * (a.head_dim + 4) * sizeof(float) : 0;
+}
 
 template <int HD>
 static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
-    a.nsplit = 1;
-    constexpr int QT = HD == 128 ? 2 : 4;
-    const int bq = dtype == PS_BF16 ? 4 * QT * 16 : 64;
-    a.row_blocks = (a.rows + bq - 1) / bq;
-    const unsigned grid = (unsigned)((long)a.batch * a.kv_heads * a.row_blocks * a.nsplit);
-    if (dtype == PS_BF16) cross_bf16_kernel<HD, QT><<<grid, 256, 0, st>>>(a);
-    else cross_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
+    const CrossPlan p = cross_plan_of(dtype, a);
+    a.nsplit = p.nsplit;
+    const dim3 grid((unsigned)(a.kv_heads * p.nsplit) * (unsigned)((a.rows + p.block - 1) / p.block), 1, a.batch);
+    if (dtype != PS_BF16) cross_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
+    else if (p.block == 64) cross_bf16_kernel<HD, 1><<<grid, 256, 0, st>>>(a);
+    else if (p.block == 128) cross_bf16_kernel<HD, 2><<<grid, 256, 0, st>>>(a);
+    else if constexpr (HD <= 64) cross_bf16_kernel<HD, 4><<<grid, 256, 0, st>>>(a);
+    if (p.nsplit > 1) {
+        const long lines = (long)a.batch * a.kv_heads * a.rows;
+        if (dtype == PS_BF16) cross_join_kernel<bf16_t, HD><<<(unsigned)((lines + 3) / 4), 256, 0, st>>>(a, lines);
+        else cross_join_kernel<float, HD><<<(unsigned)((lines + 3) / 4), 256, 0, st>>>(a, lines);
+    }
     return hipGetLastError();
 }
 

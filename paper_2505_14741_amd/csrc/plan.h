@@ -287,6 +287,18 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
     return (size_t)p.nsplit * batch * tokens * Nn * sizeof(float);
 }
 
+// ---- cross attention: query rows per workgroup, and pieces of the keys.  A function of the sample's shape only, never of the batch.
+struct CrossPlan { int block, nsplit; };
+constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, int head_dim, int cus) {
+    CrossPlan p{};
+    p.block = !bf16 || rows <= 64 ? 64 : rows <= 128 || head_dim == 128 ? 128 : 256;
+    const long items = (long)((rows + p.block - 1) / p.block) * kv_heads, tiles = (kv_len + 63) / 64;
+    long n = 1L * cus / items;                           // two workgroups per compute unit
+    if (n > tiles / 4) n = tiles / 4;                    // 256 keys each at least: the partial sums pass through memory
+    p.nsplit = n < 2 ? 1 : (int)n;
+    return p;
+}
+
 // ---- group norm: `slices` slices of slice_groups whole groups (the last may have fewer), each over `chunks` chunks of positions.
 // A function of the sample's shape only, never of the batch.
 constexpr int GROUP_NORM_SLICE_GROUPS = 256;             // most groups of a slice: one thread each

@@ -46,6 +46,17 @@ def test_cross_attention_refuses_pointers():
     assert call_cross(cross_shape(kv_len=0), o=None) == -1
 
 
+def test_cross_attention_workspace():
+    """Few rows over many keys need scratch; a missing, small or misaligned one is refused."""
+    s = cross_shape(batch=1, q_len=1, kv_len=100000)
+    n = B.lib().cross_attn_workspace_bytes(C.byref(s))
+    assert n > 0 and n % 256 == 0
+    assert call_cross(s) == -4 and call_cross(s, ws=FAKE, ws_bytes=n - 1) == -4 and call_cross(s, ws=FAKE + 128, ws_bytes=n) == -4
+    two = cross_shape(batch=2, q_len=1, kv_len=100000)
+    assert B.lib().cross_attn_workspace_bytes(C.byref(two)) == 2 * n          # a sample's plan does not depend on the batch
+    assert B.lib().cross_attn_workspace_bytes(C.byref(cross_shape(q_len=17550, kv_len=226))) == 0
+
+
 def test_quantize_refuses():
     L = B.lib()
     call = lambda x=FAKE, q=2 * FAKE, s=3 * FAKE, rows=4, cols=100, x_row=100, dtype=1: L.fp8_quantize(x, q, s, rows, cols, x_row, dtype, None)  # noqa: E731
