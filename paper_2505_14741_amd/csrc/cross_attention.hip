@@ -94,6 +94,62 @@ __device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB
     }
 }
 
+// Moves the references (in powers of two: times c) where a score of the tile is ahead of one, and what has been summed with them.
+template <int QT, int NB>
+__device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_t (&acc)[QT][NB], float (&m)[QT], float (&l)[QT], float c, float ahead) {
+    float top[QT];
+    bool over = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        top[t] = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], sc[t][g][i]);
+        over = over || top[t] > m[t] + ahead;
+    }
+    if (__any(over)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const float mn = fmaxf(m[t], max_xor32(max_xor16(top[t])));
+            const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f((m[t] - mn) * c);      // exp2(-inf) = 0 on the first tile
+            m[t] = mn;
+            l[t] *= alpha;
+#pragma unroll
+            for (int d = 0; d < NB; ++d) acc[t][d] *= alpha;
+        }
+    }
+}
+// Probabilities, rounded to bf16 for the second product and summed as rounded: one key alone has weight 1 exactly.
+template <int QT>
+__device__ __forceinline__ void cross_weights(const f32x4_t (&sc)[QT][4], const float (&m)[QT], float (&l)[QT], float c, bf16x8_t (&pf)[QT][2]) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const float mc = m[t] == -INFINITY ? 0.f : m[t] * c;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc));
+            l[t] = add_bf16x8(pf[t][s], l[t]);
+        }
+    }
+}
+// acc += V^T P^T; vt: the lane's place in the first rows of V.  k slot (kgrp, e) of step s is key 32 s + 16 (e / 4) + 4 kgrp + e % 4.
+template <int QT, int NB, int LD>
+__device__ __forceinline__ void cross_values(const bf16_t* vt, const bf16x8_t (&pf)[QT][2], f32x4_t (&acc)[QT][NB]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int d = 0; d < NB; ++d) {
+            const bf16_t* p = vt + s * 32 * LD + d * 16;
+            const bf16x4_t lo = __builtin_bit_cast(bf16x4_t, read_tr16(p)), hi = __builtin_bit_cast(bf16x4_t, read_tr16(p + 16 * LD));
+            const bf16x8_t vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][s], acc[t][d], 0, 0, 0);
+        }
+}
+
 template <int HD, int QT>
 __global__ void __launch_bounds__(256, 2)
 cross_bf16_kernel(CrossArgs a) {
@@ -201,52 +257,10 @@ cross_bf16_kernel(CrossArgs a) {
                     sc[t][g] = cross_scores<HD>(Ks + (g * 16 + l16) * LD + kgrp * 8, qf[t], bias[g]);
                 }
             }
-        float top[QT];
-        bool over = false;
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            top[t] = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], sc[t][g][i]);
-            over = over || top[t] > m[t] + ahead;
-        }
-        if (__any(over)) {
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                const float mn = fmaxf(m[t], max_xor32(max_xor16(top[t])));
-                const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f((m[t] - mn) * c);      // exp2(-inf) = 0 on the first tile
-                m[t] = mn;
-                l[t] *= alpha;
-#pragma unroll
-                for (int d = 0; d < NB; ++d) acc[t][d] *= alpha;
-            }
-        }
-        // probabilities are rounded to bf16 for the second product, and summed as rounded: one key alone has weight 1 exactly
+        cross_softmax<QT, NB>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            const float mc = m[t] == -INFINITY ? 0.f : m[t] * c;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc));
-                l[t] = add_bf16x8(pf[t][s], l[t]);
-            }
-        }
-        // k slot (kgrp, e) of step s is key 32 s + 16 (e / 4) + 4 kgrp + e % 4
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int d = 0; d < NB; ++d) {
-                const bf16_t* p = Vs + (s * 32 + 4 * kgrp + (l16 >> 2)) * LD + d * 16 + (l16 & 3) * 4;
-                const bf16x4_t lo = __builtin_bit_cast(bf16x4_t, read_tr16(p)), hi = __builtin_bit_cast(bf16x4_t, read_tr16(p + 16 * LD));
-                const bf16x8_t vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                for (int t = 0; t < QT; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][s], acc[t][d], 0, 0, 0);
-            }
+        cross_weights<QT>(sc, m, l, c, pf);
+        cross_values<QT, NB, LD>(Vs + (4 * kgrp + (l16 >> 2)) * LD + (l16 & 3) * 4, pf, acc);
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -261,6 +275,101 @@ cross_bf16_kernel(CrossArgs a) {
         } else {
             bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head);
             cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : 1.0f / sum, kgrp, row < a.rows);
+        }
+    }
+}
+
+// Short key sequences and many rows (a prompt's states under a video's tokens): all keys and values of a (sample, key/value head) lie in LDS, and
+// the 8 waves of a workgroup take 32 rows each in turn, without a barrier.  n workgroups share a head.  A row's values depend on its
+// own 32 rows only, whatever n is.
+template <int HD>
+__global__ void __launch_bounds__(512, 4)
+cross_resident_kernel(CrossArgs a, int n) {
+    constexpr int KT = 64, LD = HD + 8, QT = 2, NB = HD / 16, CH = HD / 8, QS = HD < 32 ? 1 : HD / 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int slots = (a.kv_len + KT - 1) / KT * KT;     // (of the longest sample)
+    bf16_t *const Ks = reinterpret_cast<bf16_t*>(lds), *const Vs = Ks + slots * LD;
+    float* const Bs = reinterpret_cast<float*>(Vs + slots * LD);     // what the scores' sums start from: 0, or -infinity
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
+    const int g = (int)(blockIdx.x % (unsigned)a.kv_heads), part = (int)(blockIdx.x / (unsigned)a.kv_heads), b = blockIdx.z;
+    const bf16_t* kb = (const bf16_t*)a.k + b * a.s.k_batch + g * a.s.k_head;
+    const bf16_t* vb = (const bf16_t*)a.v + b * a.s.v_batch + g * a.s.v_head;
+    const bf16_t* qb = (const bf16_t*)a.q + b * a.s.q_batch;
+    bf16_t* ob = (bf16_t*)a.o + b * a.s.o_batch;
+    const int keys = cross_keys(a, b), tiles = (keys + KT - 1) / KT;
+    const int chunks = (a.rows + 32 - 1) / 32, stride = n * 8;
+    const float c = a.scale * CROSS_LOG2E, ahead = CROSS_AHEAD / c;
+
+    bf16x8_t qf[QT][QS], qn[QT][QS];
+    auto fetch = [&](int chunk) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const bf16_t* p = qb + cross_row(a, g, min(chunk * 32 + t * 16 + l16, a.rows - 1), a.s.q_tok, a.s.q_head);
+            if constexpr (HD == 16) {
+                const bf16x4_t w = *reinterpret_cast<const bf16x4_t*>(p + kgrp * 4);
+                qn[t][0] = __builtin_shufflevector(w, w, 0, 1, 2, 3, 0, 1, 2, 3);
+            } else {
+#pragma unroll
+                for (int s = 0; s < QS; ++s) qn[t][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 32 + kgrp * 8);
+            }
+        }
+    };
+    int chunk = part * 8 + wave;
+    fetch(min(chunk, chunks - 1));
+    for (int e = threadIdx.x; e < tiles * KT * CH; e += 512) {
+        const int r = e / CH, d = e % CH * 8;
+        const bool in = r < keys && (!a.key_mask || a.key_mask[b * a.mask_batch + r] != 0);
+        i32x4_t kv = {0, 0, 0, 0}, vv = kv;
+        if (in) {
+            kv = *reinterpret_cast<const i32x4_t*>(kb + r * a.s.k_tok + d);
+            vv = *reinterpret_cast<const i32x4_t*>(vb + r * a.s.v_tok + d);
+        }
+        *reinterpret_cast<i32x4_t*>(Ks + r * LD + d) = kv;
+        *reinterpret_cast<i32x4_t*>(Vs + r * LD + d) = vv;
+        if (d == 0) Bs[r] = in ? 0.f : -INFINITY;
+    }
+    __syncthreads();
+    for (; chunk < chunks; chunk += stride) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int s = 0; s < QS; ++s) qf[t][s] = qn[t][s];
+        if (chunk + stride < chunks) fetch(chunk + stride);
+        f32x4_t acc[QT][NB];
+        float m[QT], l[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            m[t] = -INFINITY; l[t] = 0.f;
+#pragma unroll
+            for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        for (int j = 0; j < tiles; ++j) {
+            const bf16_t *kt = Ks + (j * KT + l16) * LD, *vt = Vs + (j * KT + 4 * kgrp + (l16 >> 2)) * LD + (l16 & 3) * 4;
+            f32x4_t sc[QT][4];
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(Bs + j * KT + g4 * 16 + kgrp * 4);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    if constexpr (HD == 16) {
+                        const s16x4_t kf = *reinterpret_cast<const s16x4_t*>(kt + g4 * 16 * LD + kgrp * 4);
+                        const bf16x4_t ql = __builtin_shufflevector(qf[t][0], qf[t][0], 0, 1, 2, 3);
+                        sc[t][g4] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(kf, __builtin_bit_cast(s16x4_t, ql), bias, 0, 0, 0);
+                    } else {
+                        sc[t][g4] = cross_scores<HD>(kt + g4 * 16 * LD + kgrp * 8, qf[t], bias);
+                    }
+                }
+            }
+            cross_softmax<QT, NB>(sc, acc, m, l, c, ahead);
+            bf16x8_t pf[QT][2];
+            cross_weights<QT>(sc, m, l, c, pf);
+            cross_values<QT, NB, LD>(vt, pf, acc);
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const int row = chunk * 32 + t * 16 + l16;
+            const float sum = sum_xor32(sum_xor16(l[t]));
+            cross_store<NB>(ob + cross_row(a, g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head), acc[t], sum == 0.f ? 0.f : 1.0f / sum, kgrp, row < a.rows);
         }
     }
 }
@@ -425,6 +534,15 @@ template <int HD>
 static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     const CrossPlan p = cross_plan_of(dtype, a);
     a.nsplit = p.nsplit;
+    if (p.resident) {
+        // workgroups per head: two for every compute unit over the whole batch, 32 rows for every wave at least
+        long n = 2L * compute_units() / ((long)a.kv_heads * a.batch);
+        const long most = ((a.rows + 31) / 32 + 7) / 8;
+        n = n > most ? most : n < 1 ? 1 : n;
+        const int bytes = (a.kv_len + 63) / 64 * 64 * cross_resident_key_bytes(HD);
+        cross_resident_kernel<HD><<<dim3((unsigned)(a.kv_heads * n), 1, a.batch), 512, bytes, st>>>(a, (int)n);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)(a.kv_heads * p.nsplit) * (unsigned)((a.rows + p.block - 1) / p.block), 1, a.batch);
     if (dtype != PS_BF16) cross_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
     else if (p.block == 64) cross_bf16_kernel<HD, 1><<<grid, 256, 0, st>>>(a);

@@ -288,7 +288,10 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 }
 
 // ---- cross attention: query rows per workgroup, and pieces of the keys.  A function of the sample's shape only, never of the batch.
-struct CrossPlan { int block, nsplit; };
+// resident: all keys in LDS (bf16), which has to hold two such workgroups.
+struct CrossPlan { int block, nsplit; bool resident; };
+constexpr int cross_resident_key_bytes(int head_dim) { return 4 * (head_dim + 8) + 4; }
+
 constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, int head_dim, int cus) {
     CrossPlan p{};
     p.block = !bf16 || rows <= 64 ? 64 : rows <= 128 || head_dim == 128 ? 128 : 256;
@@ -296,6 +299,7 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
     long n = 1L * cus / items;                           // two workgroups per compute unit
     if (n > tiles / 4) n = tiles / 4;                    // 256 keys each at least: the partial sums pass through memory
     p.nsplit = n < 2 ? 1 : (int)n;
+    p.resident = bf16 && p.nsplit == 1 && rows >= 256 && tiles * 64 * cross_resident_key_bytes(head_dim) <= 80 * 1024;
     return p;
 }
 
