@@ -10,9 +10,11 @@
 #include "lane_sums.h"
 #include "plan.h"
 #include "tile_ops.h"
+#include <type_traits>
 
 namespace ps {
 
+constexpr int CROSS_RESIDENT_WAVES = 8;
 constexpr float CROSS_LOG2E = 1.4426950408889634f;
 
 // the sample's keys, and which of the 64 keys from kv0 on count (wave-uniform)
@@ -51,14 +53,6 @@ __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, lo
 // stay below 2^8, sums far from overflow): a tile then costs no rescaling and no maximum over lanes.
 constexpr float CROSS_AHEAD = 8.0f;
 
-template <int HD>
-__device__ __forceinline__ f32x4_t cross_scores(const bf16_t* k, const bf16x8_t* q, f32x4_t acc) {
-#pragma unroll
-    for (int s = 0; s < HD / 32; ++s)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8_t*>(k + s * 32), q[s], acc, 0, 0, 0);
-    return acc;
-}
-
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 __device__ __forceinline__ s16x4_t read_tr16(const bf16_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
@@ -94,8 +88,61 @@ __device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB
     }
 }
 
+// The K fragments of a tile of 64 keys: first operand of S^T, 8 consecutive d (4 for heads of 16) of row l16 of each 16 keys.
+// kt: the lane's place in the tile's first 16 rows.
+template <int HD> struct CrossK { static constexpr int STEPS = HD < 32 ? 1 : HD / 32; bf16x8_t f[4][STEPS]; };
+template <int HD, int LD>
+__device__ __forceinline__ void cross_read_k(const bf16_t* kt, CrossK<HD>& k) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if constexpr (HD == 16) {
+            const bf16x4_t w = *reinterpret_cast<const bf16x4_t*>(kt + g * 16 * LD);
+            k.f[g][0] = __builtin_shufflevector(w, w, 0, 1, 2, 3, 0, 1, 2, 3);
+        } else {
+#pragma unroll
+            for (int s = 0; s < HD / 32; ++s) k.f[g][s] = *reinterpret_cast<const bf16x8_t*>(kt + g * 16 * LD + s * 32);
+        }
+    }
+}
+template <int HD, int QT>
+__device__ __forceinline__ void cross_scores(const CrossK<HD>& k, const bf16x8_t (&q)[QT][CrossK<HD>::STEPS], f32x4_t (&sc)[QT][4]) {
+    constexpr f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            if constexpr (HD == 16) {
+                const bf16x4_t kl = __builtin_shufflevector(k.f[g][0], k.f[g][0], 0, 1, 2, 3), ql = __builtin_shufflevector(q[t][0], q[t][0], 0, 1, 2, 3);
+                sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, kl), __builtin_bit_cast(s16x4_t, ql), zero, 0, 0, 0);
+            } else {
+                sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[g][0], q[t][0], zero, 0, 0, 0);
+            }
+        }
+#pragma unroll
+    for (int s = 1; s < HD / 32; ++s)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[g][s], q[t][s], sc[t][g], 0, 0, 0);
+}
+// The V fragments of a tile: first operand of O^T, row d = l16 of each 16 d, k slot (kgrp, e) of step s is key 32 s + 16 (e / 4) + 4 kgrp + e % 4.
+// vt: the lane's place in the tile's first rows.
+template <int HD> struct CrossV { bf16x8_t f[2][HD / 16]; };
+template <int HD, int LD>
+__device__ __forceinline__ void cross_read_v(const bf16_t* vt, CrossV<HD>& v) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) {
+            const bf16_t* p = vt + s * 32 * LD + d * 16;
+            const bf16x4_t lo = __builtin_bit_cast(bf16x4_t, read_tr16(p)), hi = __builtin_bit_cast(bf16x4_t, read_tr16(p + 16 * LD));
+            v.f[s][d] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+}
+
 // Moves the references (in powers of two: times c) where a score of the tile is ahead of one, and what has been summed with them.
-template <int QT, int NB>
+// FIRST: of the row's first tile, nothing has been summed.
+template <int QT, int NB, bool FIRST = false>
 __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_t (&acc)[QT][NB], float (&m)[QT], float (&l)[QT], float c, float ahead) {
     float top[QT];
     bool over = false;
@@ -106,9 +153,14 @@ __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_
         for (int g = 0; g < 4; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], sc[t][g][i]);
-        over = over || top[t] > m[t] + ahead;
+        if constexpr (FIRST) {
+            m[t] = max_xor32(max_xor16(top[t]));
+            l[t] = 0.f;
+        } else {
+            over = over || top[t] > m[t] + ahead;
+        }
     }
-    if (__any(over)) {
+    if (!FIRST && __any(over)) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const float mn = fmaxf(m[t], max_xor32(max_xor16(top[t])));
@@ -135,28 +187,25 @@ __device__ __forceinline__ void cross_weights(const f32x4_t (&sc)[QT][4], const 
         }
     }
 }
-// acc += V^T P^T; vt: the lane's place in the first rows of V.  k slot (kgrp, e) of step s is key 32 s + 16 (e / 4) + 4 kgrp + e % 4.
-template <int QT, int NB, int LD>
-__device__ __forceinline__ void cross_values(const bf16_t* vt, const bf16x8_t (&pf)[QT][2], f32x4_t (&acc)[QT][NB]) {
+// acc += V^T P^T
+template <int HD, int QT, bool FIRST = false>
+__device__ __forceinline__ void cross_values(const CrossV<HD>& v, const bf16x8_t (&pf)[QT][2], f32x4_t (&acc)[QT][HD / 16]) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int d = 0; d < NB; ++d) {
-            const bf16_t* p = vt + s * 32 * LD + d * 16;
-            const bf16x4_t lo = __builtin_bit_cast(bf16x4_t, read_tr16(p)), hi = __builtin_bit_cast(bf16x4_t, read_tr16(p + 16 * LD));
-            const bf16x8_t vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-            for (int t = 0; t < QT; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][s], acc[t][d], 0, 0, 0);
-        }
+            for (int t = 0; t < QT; ++t)
+                acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.f[s][d], pf[t][s], FIRST && s == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc[t][d], 0, 0, 0);
 }
 
 template <int HD, int QT>
 __global__ void __launch_bounds__(256, 2)
 cross_bf16_kernel(CrossArgs a) {
-    constexpr int KT = 64, LD = HD + 8, BQ = 4 * QT * 16, NB = HD / 16, CH = HD / 8;
+    constexpr int KT = 64, LD = HD + 8, LDV = cross_v_pitch(HD), BQ = 4 * QT * 16, NB = HD / 16, CH = HD / 8;
     constexpr int QS = HD < 32 ? 1 : HD / 32;            // fragments of a query row
     constexpr int LOADS = (KT * CH + 255) / 256;
-    __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * LD], Vs[KT * LD];
+    __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * LD], Vs[KT * LDV];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
     const CrossItem it = cross_item(a);
     const bf16_t* kb = (const bf16_t*)a.k + it.b * a.s.k_batch + it.g * a.s.k_head;
@@ -208,16 +257,12 @@ cross_bf16_kernel(CrossArgs a) {
     }
     f32x4_t acc[QT][NB];                                 // O^T: row l16, d = 16 * block + 4 * kgrp + i
     float m[QT], l[QT];                                  // l: over this lane's keys only
-    f32x4_t bias[4];                                     // what the scores' sums start from: 0, or -infinity for keys that do not count
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         m[t] = -INFINITY; l[t] = 0.f;
 #pragma unroll
         for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll
-    for (int g = 0; g < 4; ++g) bias[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    bool biased = false;
     for (int j = j0; j < j1; ++j) {
         const unsigned long long counts = counts_next;
         const bool whole = counts == ~0ull;
@@ -226,9 +271,9 @@ cross_bf16_kernel(CrossArgs a) {
         for (int u = 0; u < LOADS; ++u) {
             if (KT * CH % 256 && at[u] >= KT) continue;
             if (!whole && !(counts >> at[u] & 1)) kn[u] = vn[u] = chunk_t{0, 0, 0, 0};
-            const int off = at[u] * LD + (threadIdx.x + 256 * u) % CH * 8;
-            *reinterpret_cast<chunk_t*>(Ks + off) = kn[u];
-            *reinterpret_cast<chunk_t*>(Vs + off) = vn[u];
+            const int d = (threadIdx.x + 256 * u) % CH * 8;
+            *reinterpret_cast<chunk_t*>(Ks + at[u] * LD + d) = kn[u];
+            *reinterpret_cast<chunk_t*>(Vs + at[u] * LDV + d) = vn[u];
         }
         __syncthreads();
         if (j + 1 < j1) {
@@ -236,31 +281,30 @@ cross_bf16_kernel(CrossArgs a) {
             fetch((j + 1) * KT);
         }
         if (counts == 0) continue;                       // (the whole workgroup)
-        if (!whole || biased) {
+        // reads are requested together, ahead of their use: V while the softmax runs
+        CrossK<HD> kf;
+        cross_read_k<HD, LD>(Ks + l16 * LD + kgrp * (HD == 16 ? 4 : 8), kf);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4_t sc[QT][4];
+        cross_scores<HD, QT>(kf, qf, sc);
+        CrossV<HD> vf;
+        cross_read_v<HD, LDV>(Vs + (4 * kgrp + (l16 >> 2)) * LDV + (l16 & 3) * 4, vf);
+        if constexpr (QT * HD <= 128) __builtin_amdgcn_sched_barrier(0);     // (more would not fit the registers)
+        if (!whole) {
             const unsigned long long mine = counts >> (4 * kgrp);
 #pragma unroll
             for (int g = 0; g < 4; ++g)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bias[g][i] = (mine >> (16 * g + i) & 1) ? 0.f : -INFINITY;
-            biased = !whole;
-        }
-        f32x4_t sc[QT][4];
+                for (int i = 0; i < 4; ++i) {
+                    const float bias = (mine >> (16 * g + i) & 1) ? 0.f : -INFINITY;     // (K rows that do not count are zeros)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                if constexpr (HD == 16) {
-                    const s16x4_t kf = *reinterpret_cast<const s16x4_t*>(Ks + (g * 16 + l16) * LD + kgrp * 4);
-                    const bf16x4_t ql = __builtin_shufflevector(qf[t][0], qf[t][0], 0, 1, 2, 3);
-                    sc[t][g] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(kf, __builtin_bit_cast(s16x4_t, ql), bias[g], 0, 0, 0);
-                } else {
-                    sc[t][g] = cross_scores<HD>(Ks + (g * 16 + l16) * LD + kgrp * 8, qf[t], bias[g]);
+                    for (int t = 0; t < QT; ++t) sc[t][g][i] += bias;
                 }
-            }
+        }
         cross_softmax<QT, NB>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
         cross_weights<QT>(sc, m, l, c, pf);
-        cross_values<QT, NB, LD>(Vs + (4 * kgrp + (l16 >> 2)) * LD + (l16 & 3) * 4, pf, acc);
+        cross_values<HD, QT>(vf, pf, acc);
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -274,102 +318,130 @@ cross_bf16_kernel(CrossArgs a) {
             if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m[t] * c};
         } else {
             bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head);
-            cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : 1.0f / sum, kgrp, row < a.rows);
+            cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp, row < a.rows);
         }
     }
 }
 
 // Short key sequences and many rows (a prompt's states under a video's tokens): all keys and values of a (sample, key/value head) lie in LDS, and
-// the 8 waves of a workgroup take 32 rows each in turn, without a barrier.  n workgroups share a head.  A row's values depend on its
-// own 32 rows only, whatever n is.
-template <int HD>
-__global__ void __launch_bounds__(512, 4)
+// the 8 waves of a workgroup (four per SIMD of two workgroups) take QT * 16 rows each in turn, without a barrier.  n workgroups share a head.  A row's values depend on
+// the rows of its own chunk only, whatever n is.
+template <int HD, int QT>
+__global__ void __launch_bounds__(CROSS_RESIDENT_WAVES * 64, CROSS_RESIDENT_WAVES / 2)
 cross_resident_kernel(CrossArgs a, int n) {
-    constexpr int KT = 64, LD = HD + 8, QT = 2, NB = HD / 16, CH = HD / 8, QS = HD < 32 ? 1 : HD / 32;
+    constexpr int KT = 64, LDK = HD + 8, LDV = cross_v_pitch(HD), BQ = QT * 16, NB = HD / 16, CH = HD / 8, QS = HD < 32 ? 1 : HD / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int slots = (a.kv_len + KT - 1) / KT * KT;     // (of the longest sample)
-    bf16_t *const Ks = reinterpret_cast<bf16_t*>(lds), *const Vs = Ks + slots * LD;
-    float* const Bs = reinterpret_cast<float*>(Vs + slots * LD);     // what the scores' sums start from: 0, or -infinity
+    bf16_t *const Ks = reinterpret_cast<bf16_t*>(lds), *const Vs = Ks + slots * LDK;
+    float* const Bs = reinterpret_cast<float*>(Vs + slots * LDV);    // what the scores' sums start from: 0, or -infinity
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
-    const int g = (int)(blockIdx.x % (unsigned)a.kv_heads), part = (int)(blockIdx.x / (unsigned)a.kv_heads), b = blockIdx.z;
+    const int part = (int)(blockIdx.x / (unsigned)a.kv_heads), g = (int)blockIdx.x - part * a.kv_heads, b = blockIdx.z;
     const bf16_t* kb = (const bf16_t*)a.k + b * a.s.k_batch + g * a.s.k_head;
     const bf16_t* vb = (const bf16_t*)a.v + b * a.s.v_batch + g * a.s.v_head;
     const bf16_t* qb = (const bf16_t*)a.q + b * a.s.q_batch;
     bf16_t* ob = (bf16_t*)a.o + b * a.s.o_batch;
     const int keys = cross_keys(a, b), tiles = (keys + KT - 1) / KT;
-    const int chunks = (a.rows + 32 - 1) / 32, stride = n * 8;
+    const int chunks = (a.rows + BQ - 1) / BQ, stride = n * CROSS_RESIDENT_WAVES;
     const float c = a.scale * CROSS_LOG2E, ahead = CROSS_AHEAD / c;
 
-    bf16x8_t qf[QT][QS], qn[QT][QS];
+    // offset of row t * 16 + l16 of a chunk: the lane's share of it is the same for all chunks that are whole, if heads share no keys
+    const long q_lane = l16 * a.s.q_tok + kgrp * (HD == 16 ? 4 : 8), o_lane = l16 * a.s.o_tok;
+    const auto row_at = [&](int chunk, int t, long tok, long head, long of_lane, long plus) {
+        const int row = chunk * BQ + t * 16;
+        if (a.share == 1 && row + 16 <= a.rows) return row * tok + g * head + of_lane;
+        return cross_row(a, g, min(row + l16, a.rows - 1), tok, head) + plus;
+    };
+    bf16x8_t qf[QT][QS];
     auto fetch = [&](int chunk) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const bf16_t* p = qb + cross_row(a, g, min(chunk * 32 + t * 16 + l16, a.rows - 1), a.s.q_tok, a.s.q_head);
+            const bf16_t* p = qb + row_at(chunk, t, a.s.q_tok, a.s.q_head, q_lane, kgrp * (HD == 16 ? 4 : 8));
             if constexpr (HD == 16) {
-                const bf16x4_t w = *reinterpret_cast<const bf16x4_t*>(p + kgrp * 4);
-                qn[t][0] = __builtin_shufflevector(w, w, 0, 1, 2, 3, 0, 1, 2, 3);
+                const bf16x4_t w = *reinterpret_cast<const bf16x4_t*>(p);
+                qf[t][0] = __builtin_shufflevector(w, w, 0, 1, 2, 3, 0, 1, 2, 3);
             } else {
 #pragma unroll
-                for (int s = 0; s < QS; ++s) qn[t][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 32 + kgrp * 8);
+                for (int s = 0; s < QS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 32);
             }
         }
     };
-    int chunk = part * 8 + wave;
+    int chunk = part * CROSS_RESIDENT_WAVES + wave;
     fetch(min(chunk, chunks - 1));
-    for (int e = threadIdx.x; e < tiles * KT * CH; e += 512) {
-        const int r = e / CH, d = e % CH * 8;
-        const bool in = r < keys && (!a.key_mask || a.key_mask[b * a.mask_batch + r] != 0);
-        i32x4_t kv = {0, 0, 0, 0}, vv = kv;
-        if (in) {
-            kv = *reinterpret_cast<const i32x4_t*>(kb + r * a.s.k_tok + d);
-            vv = *reinterpret_cast<const i32x4_t*>(vb + r * a.s.v_tok + d);
+    constexpr int NT = CROSS_RESIDENT_WAVES * 64, U = 4; // U: keys and values in flight per thread
+    const int pieces = tiles * KT * CH;
+    for (int e0 = threadIdx.x; e0 < pieces; e0 += U * NT) {
+        i32x4_t kv[U], vv[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = (e0 + u * NT) / CH, rc = min(r, keys - 1), d = (e0 + u * NT) % CH * 8;
+            in[u] = r < keys && (!a.key_mask || a.key_mask[b * a.mask_batch + rc] != 0);
+            kv[u] = *reinterpret_cast<const i32x4_t*>(kb + rc * a.s.k_tok + d);
+            vv[u] = *reinterpret_cast<const i32x4_t*>(vb + rc * a.s.v_tok + d);
         }
-        *reinterpret_cast<i32x4_t*>(Ks + r * LD + d) = kv;
-        *reinterpret_cast<i32x4_t*>(Vs + r * LD + d) = vv;
-        if (d == 0) Bs[r] = in ? 0.f : -INFINITY;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = (e0 + u * NT) / CH, d = (e0 + u * NT) % CH * 8;
+            if (e0 + u * NT >= pieces) continue;
+            *reinterpret_cast<i32x4_t*>(Ks + r * LDK + d) = in[u] ? kv[u] : i32x4_t{0, 0, 0, 0};
+            *reinterpret_cast<i32x4_t*>(Vs + r * LDV + d) = in[u] ? vv[u] : i32x4_t{0, 0, 0, 0};
+            if (d == 0) Bs[r] = in[u] ? 0.f : -INFINITY;
+        }
     }
     __syncthreads();
-    for (; chunk < chunks; chunk += stride) {
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int s = 0; s < QS; ++s) qf[t][s] = qn[t][s];
-        if (chunk + stride < chunks) fetch(chunk + stride);
-        f32x4_t acc[QT][NB];
-        float m[QT], l[QT];
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            m[t] = -INFINITY; l[t] = 0.f;
-#pragma unroll
-            for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-        for (int j = 0; j < tiles; ++j) {
-            const bf16_t *kt = Ks + (j * KT + l16) * LD, *vt = Vs + (j * KT + 4 * kgrp + (l16 >> 2)) * LD + (l16 & 3) * 4;
-            f32x4_t sc[QT][4];
+    unsigned whole = 0;                                  // tiles all of whose keys count
+    for (int j = 0; j < tiles; ++j) whole |= (__ballot(Bs[j * KT + lane] == 0.f) == ~0ull ? 1u : 0u) << j;
+
+    const bf16_t *const k0 = Ks + l16 * LDK + kgrp * (HD == 16 ? 4 : 8), *const v0 = Vs + (4 * kgrp + (l16 >> 2)) * LDV + (l16 & 3) * 4;
+    f32x4_t acc[QT][NB];
+    float m[QT], l[QT];
+    // One tile; the next chunk's queries are requested when the last tile has used this one's.  (K and V fragments requested ahead of
+    // their use do not leave room for four waves per SIMD: 67 us at three, 57 so.)
+    const auto tile = [&](int j, auto first_c) {
+        constexpr bool FIRST = decltype(first_c)::value;
+        f32x4_t sc[QT][4];
+        CrossK<HD> kf;
+        cross_read_k<HD, LDK>(k0 + j * (KT * LDK), kf);
+        cross_scores<HD, QT>(kf, qf, sc);
+        CrossV<HD> vf;
+        if (j == tiles - 1 && chunk + stride < chunks) fetch(chunk + stride);
+        if (!(whole >> j & 1)) {
 #pragma unroll
             for (int g4 = 0; g4 < 4; ++g4) {
                 const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(Bs + j * KT + g4 * 16 + kgrp * 4);
 #pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    if constexpr (HD == 16) {
-                        const s16x4_t kf = *reinterpret_cast<const s16x4_t*>(kt + g4 * 16 * LD + kgrp * 4);
-                        const bf16x4_t ql = __builtin_shufflevector(qf[t][0], qf[t][0], 0, 1, 2, 3);
-                        sc[t][g4] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(kf, __builtin_bit_cast(s16x4_t, ql), bias, 0, 0, 0);
-                    } else {
-                        sc[t][g4] = cross_scores<HD>(kt + g4 * 16 * LD + kgrp * 8, qf[t], bias);
-                    }
-                }
+                for (int t = 0; t < QT; ++t) sc[t][g4] += bias;
             }
-            cross_softmax<QT, NB>(sc, acc, m, l, c, ahead);
-            bf16x8_t pf[QT][2];
-            cross_weights<QT>(sc, m, l, c, pf);
-            cross_values<QT, NB, LD>(vt, pf, acc);
         }
+        cross_softmax<QT, NB, FIRST>(sc, acc, m, l, c, ahead);
+        bf16x8_t pf[QT][2];
+        cross_weights<QT>(sc, m, l, c, pf);
+        cross_read_v<HD, LDV>(v0 + j * (KT * LDV), vf);
+        cross_values<HD, QT, FIRST>(vf, pf, acc);
+    };
+    for (; chunk < chunks; chunk += stride) {
+        if (tiles > 0) {
+            tile(0, std::true_type{});
+        } else {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                l[t] = 0.f;
+#pragma unroll
+                for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        for (int j = 1; j < tiles; ++j) tile(j, std::false_type{});
+        // the next queries' loads are waited for here: behind the stores, whose number the compiler cannot know, it would wait for these too
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qf[t][s]));
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const int row = chunk * 32 + t * 16 + l16;
             const float sum = sum_xor32(sum_xor16(l[t]));
-            cross_store<NB>(ob + cross_row(a, g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head), acc[t], sum == 0.f ? 0.f : 1.0f / sum, kgrp, row < a.rows);
+            cross_store<NB>(ob + row_at(chunk, t, a.s.o_tok, a.s.o_head, o_lane, 0), acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp,
+                            chunk * BQ + t * 16 + l16 < a.rows);
         }
     }
 }
@@ -534,13 +606,15 @@ template <int HD>
 static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     const CrossPlan p = cross_plan_of(dtype, a);
     a.nsplit = p.nsplit;
+    if constexpr (HD <= 64)
     if (p.resident) {
-        // workgroups per head: two for every compute unit over the whole batch, 32 rows for every wave at least
+        // workgroups per head: two for every compute unit over the whole batch, a chunk for every wave at least
         long n = 2L * compute_units() / ((long)a.kv_heads * a.batch);
-        const long most = ((a.rows + 31) / 32 + 7) / 8;
+        constexpr int QT = 2;
+        const long most = ((a.rows + QT * 16 - 1) / (QT * 16) + CROSS_RESIDENT_WAVES - 1) / CROSS_RESIDENT_WAVES;
         n = n > most ? most : n < 1 ? 1 : n;
         const int bytes = (a.kv_len + 63) / 64 * 64 * cross_resident_key_bytes(HD);
-        cross_resident_kernel<HD><<<dim3((unsigned)(a.kv_heads * n), 1, a.batch), 512, bytes, st>>>(a, (int)n);
+        cross_resident_kernel<HD, QT><<<dim3((unsigned)(a.kv_heads * n), 1, a.batch), CROSS_RESIDENT_WAVES * 64, bytes, st>>>(a, (int)n);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)(a.kv_heads * p.nsplit) * (unsigned)((a.rows + p.block - 1) / p.block), 1, a.batch);

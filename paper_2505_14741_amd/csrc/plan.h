@@ -290,7 +290,10 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 // ---- cross attention: query rows per workgroup, and pieces of the keys.  A function of the sample's shape only, never of the batch.
 // resident: all keys in LDS (bf16), which has to hold two such workgroups.
 struct CrossPlan { int block, nsplit; bool resident; };
-constexpr int cross_resident_key_bytes(int head_dim) { return 4 * (head_dim + 8) + 4; }
+// Pitches of K and V rows in LDS (64 banks of 4 bytes).  A K fragment is 16-byte reads of 16 rows: an odd number of 16 bytes apart, they
+// fall into different banks.  A V fragment is 8-byte reads of 8 rows x 32 bytes: an odd number of 32 bytes apart (heads of 16: of 16).
+constexpr int cross_v_pitch(int head_dim) { return head_dim == 16 ? 24 : head_dim + 16; }
+constexpr int cross_resident_key_bytes(int head_dim) { return 2 * (head_dim + 8 + cross_v_pitch(head_dim)) + 4; }
 
 constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, int head_dim, int cus) {
     CrossPlan p{};
@@ -299,7 +302,7 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
     long n = 1L * cus / items;                           // two workgroups per compute unit
     if (n > tiles / 4) n = tiles / 4;                    // 256 keys each at least: the partial sums pass through memory
     p.nsplit = n < 2 ? 1 : (int)n;
-    p.resident = bf16 && p.nsplit == 1 && rows >= 256 && tiles * 64 * cross_resident_key_bytes(head_dim) <= 80 * 1024;
+    p.resident = bf16 && head_dim <= 64 && p.nsplit == 1 && rows >= 256 && tiles * 64 * cross_resident_key_bytes(head_dim) <= 80 * 1024;
     return p;
 }
 
