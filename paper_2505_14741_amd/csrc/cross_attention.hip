@@ -284,12 +284,12 @@ cross_bf16_kernel(CrossArgs a) {
         // reads are requested together, ahead of their use: V while the softmax runs
         CrossK<HD> kf;
         cross_read_k<HD, LD>(Ks + l16 * LD + kgrp * (HD == 16 ? 4 : 8), kf);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (QT * HD <= 128) __builtin_amdgcn_sched_barrier(0);     // (more would not fit the registers)
         f32x4_t sc[QT][4];
         cross_scores<HD, QT>(kf, qf, sc);
         CrossV<HD> vf;
         cross_read_v<HD, LDV>(Vs + (4 * kgrp + (l16 >> 2)) * LDV + (l16 & 3) * 4, vf);
-        if constexpr (QT * HD <= 128) __builtin_amdgcn_sched_barrier(0);     // (more would not fit the registers)
+        if constexpr (QT * HD <= 128) __builtin_amdgcn_sched_barrier(0);
         if (!whole) {
             const unsigned long long mine = counts >> (4 * kgrp);
 #pragma unroll

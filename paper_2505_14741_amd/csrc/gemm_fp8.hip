@@ -6,7 +6,9 @@
 #include "fp8.h"
 #include "few_epilogue.h"
 #include "lane_sums.h"
+#include "plan.h"
 #include "tile_ops.h"
+#include <type_traits>
 
 namespace ps {
 
@@ -107,36 +109,58 @@ __device__ __forceinline__ void lds_dma4_base(unsigned voff, const void* sbase, 
                  : "memory", "m0");
 }
 
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// 4 adjacent columns of a row, behind the bias
+__device__ __forceinline__ f32x4_t fp8_finish(const Fp8Product& g, f32x4_t x) {
+    if (g.act) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = gelu_fast(x[i]);
+    }
+    return x;
+}
+__device__ __forceinline__ f32x4_t fp8_bias(const Fp8Product& g, int col) {
+    if (g.n_out % 4 == 0) return *reinterpret_cast<const f32x4_t*>(g.bias + min(col, g.n_out - 4));
+    f32x4_t b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = g.bias[min(col + i, g.n_out - 1)];
+    return b;
+}
 __device__ __forceinline__ void fp8_store(const Fp8Product& g, int row, int col, f32x4_t x) {
     bf16_t* out = g.out + (long)row * g.n_out + col;
     if (g.n_out % 4 == 0) {                              // a lane's 4 columns are inside or outside together
-        x += *reinterpret_cast<const f32x4_t*>(g.bias + col);
-        if (g.act) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = gelu_fast(x[i]);
-        }
         store_quad(out, x);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (col + i < g.n_out) {
-                const float y = x[i] + g.bias[col + i];
-                out[i] = from_f32<bf16_t>(g.act ? gelu_fast(y) : y);
-            }
+            if (col + i < g.n_out) out[i] = from_f32<bf16_t>(x[i]);
     }
 }
 
+// WR x WC waves of TM x TN blocks of 16 x 16 outputs (rows x columns).  A ring of NST stages of one block of k.
+// A stage has two halves of TM / 2 row blocks.  The first goes row block by row block: as soon as the products of one are issued, its
+// registers are read again with the one TM / 2 further down.  Then the next stage's data are waited for and the slot of this one, all of
+// whose fragments are in registers, is requested anew; the second half goes column block by column block and reads the next stage's W, and
+// in its last column the next stage's first A fragments.  So one set of registers per operand is enough (128 x 64 outputs a wave).
 template <int TM, int TN, int WR, int WC, int NST, int OCC>
 __global__ void __launch_bounds__(WR * WC * 64, OCC)
 gemm_fp8_kernel(Fp8Product g) {
-    constexpr int NW = WR * WC, BM = WR * TM * 16, BN = WC * TN * 16;
-    static_assert((BM + BN) % (8 * NW) == 0 && BM % 8 == 0 && BM <= 256 && BN <= 256, "load groups");
+    constexpr int NW = WR * WC, BM = WR * TM * 16, BN = WC * TN * 16, H = TM / 2;
+    static_assert((BM + BN) % (8 * NW) == 0 && BM % 8 == 0 && BM <= 256 && BN <= 256 && TM % 2 == 0 && NST >= 2 && NST <= 4, "tile");
     constexpr int GPW = (BM + BN) / 8 / NW, DATA = (BM + BN) * 128, STAGE = DATA + 1024;   // scales: 256 bytes of A, 256 of W
     __shared__ __attribute__((aligned(1024))) unsigned char lds[NST * STAGE];
-    const int id = xcd_remap(blockIdx.x, gridDim.x);
-    const int band = id / (8 * g.tiles_n), in_band = id % (8 * g.tiles_n), rows_here = min(8, g.tiles_m - band * 8);
-    const int m0 = (band * 8 + in_band % rows_here) * BM, n0 = in_band / rows_here * BN;
-    const int nkt = g.blocks;
+    int id = xcd_remap(blockIdx.x, gridDim.x), k0 = 0, nkt = g.blocks, piece = 0;
+    if (g.pieces > 1) {
+        const int tiles = g.tiles_m * g.tiles_n;
+        piece = id / tiles;
+        id -= piece * tiles;
+        k0 = g.blocks * piece / g.pieces;
+        nkt = g.blocks * (piece + 1) / g.pieces - k0;
+    }
+    const int band = id / (8 * g.tiles_n), in_band = id - band * (8 * g.tiles_n), rows_here = min(8, g.tiles_m - band * 8);
+    const int tn = in_band / rows_here;
+    const int m0 = (band * 8 + in_band - tn * rows_here) * BM, n0 = tn * BN;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WC, wn = wave % WC, l16 = lane & 15, kgrp = lane >> 4;
@@ -149,20 +173,20 @@ gemm_fp8_kernel(Fp8Product g) {
     for (int i = 0; i < GPW; ++i) {
         const int group = wave * GPW + i, row = group * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
         const bool of_a = group * 8 < BM;
-        base[i] = of_a ? (const char*)g.a + m0 * row_bytes : (const char*)g.w + n0 * row_bytes;
+        base[i] = (of_a ? (const char*)g.a + m0 * row_bytes : (const char*)g.w + n0 * row_bytes) + (long)k0 * 128;
         off[i] = (unsigned)(of_a ? min(row, g.m - 1 - m0) : min(row - BM, g.n_out - 1 - n0)) * (unsigned)row_bytes + chunk * 16;
     }
     // every wave requests one of the two strips of scales (so that all have the same number of loads out); 4 rows a lane
     const bool scale_a = (wave & 1) == 0;
     const int pitch = scale_a ? g.a_pitch : g.w_pitch, s0 = scale_a ? m0 : n0;
-    const char* const sbase = (const char*)(scale_a ? g.a_scale : g.w_scale) + s0;
+    const char* const sbase = (const char*)(scale_a ? g.a_scale : g.w_scale) + s0 + (long)k0 * pitch;
     const unsigned soff = (unsigned)min(lane * 4, pitch - 4 - s0);
     const unsigned lds_base = (unsigned)(size_t)PS_LDS_PTR(lds);
-    auto issue = [&](int kt, int slot) {
-#pragma unroll
-        for (int i = 0; i < GPW; ++i)
+    auto issue_one = [&](int kt, int slot, int i) {      // i == GPW: the scales
+        if (i < GPW)
             lds_dma16_base(off[i], base[i] + (long)kt * 128, __builtin_amdgcn_readfirstlane(lds_base + slot * STAGE + (wave * GPW + i) * 1024));
-        lds_dma4_base(soff, sbase + (long)kt * pitch, __builtin_amdgcn_readfirstlane(lds_base + slot * STAGE + DATA + (scale_a ? 0 : 256)));
+        else
+            lds_dma4_base(soff, sbase + (long)kt * pitch, __builtin_amdgcn_readfirstlane(lds_base + slot * STAGE + DATA + (scale_a ? 0 : 256)));
     };
 
     f32x4_t acc[TN][TM];
@@ -176,57 +200,156 @@ gemm_fp8_kernel(Fp8Product g) {
         const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(row + c0), hi = *reinterpret_cast<const i32x4_t*>(row + (c0 ^ 64));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
+    i32x8_t fa[H], fw[TN];
+    int sa[H], sw[TN];
+    auto read_a = [&](const unsigned char* st, int slot, int x) {
+        fa[slot] = fragment(st + aoff + x * 2048);
+        sa[slot] = st[DATA + (wm * TM + x) * 16 + l16];
+    };
+    auto read_w = [&](const unsigned char* st, int y) {
+        fw[y] = fragment(st + woff + y * 2048);
+        sw[y] = st[DATA + 256 + (wn * TN + y) * 16 + l16];
+    };
 #pragma unroll
-    for (int p = 0; p < NST - 1; ++p)
-        if (p < nkt) issue(p, p);
-    for (int kt = 0; kt < nkt; ++kt) {
-        if (NST > 2 && nkt - kt > NST - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * (GPW + 1)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                                 // stage kt is there, and nobody reads stage kt - 1 any more
-        if (kt + NST - 1 < nkt) issue(kt + NST - 1, (kt + NST - 1) % NST);
-        const unsigned char* st = lds + kt % NST * STAGE;
-        i32x8_t fw[TN];
-        int sw[TN];
+    for (int p = 0; p < NST; ++p)
+        if (p < nkt) {
 #pragma unroll
-        for (int y = 0; y < TN; ++y) {
-            fw[y] = fragment(st + woff + y * 2048);
-            sw[y] = st[DATA + 256 + (wn * TN + y) * 16 + l16];
+            for (int i = 0; i <= GPW; ++i) issue_one(p, p, i);
         }
+    if (nkt >= NST) wait_loads<(NST - 1) * (GPW + 1)>(); else wait_loads<0>();       // stage 0
+    __syncthreads();
 #pragma unroll
-        for (int x = 0; x < TM; ++x) {
-            const i32x8_t fa = fragment(st + aoff + x * 2048);
-            const int sa = st[DATA + (wm * TM + x) * 16 + l16];
+    for (int y = 0; y < TN; ++y) read_w(lds, y);
+#pragma unroll
+    for (int x = 0; x < H; ++x) read_a(lds, x, x);
+    int slot = 0;
+    // One stage.  LEFT: stages behind it, NST or more: any number, which is the steady state; no form has a branch inside (with one the
+    // compiler sinks the first half's products behind it).
+    auto stage = [&](int kt, auto left_c) {
+        constexpr int LEFT = decltype(left_c)::value;
+        const int next = slot + 1 == NST ? 0 : slot + 1;
+        const unsigned char *st = lds + slot * STAGE, *nx = lds + next * STAGE;
+#pragma unroll
+        for (int x = 0; x < H; ++x) {
 #pragma unroll
             for (int y = 0; y < TN; ++y)
-                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[y], fa, acc[y][x], 0, 0, 0, sw[y], 0, sa);
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[y], fa[x], acc[y][x], 0, 0, 0, sw[y], 0, sa[x]);
+            read_a(st, x, x + H);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (LEFT > 0) {
+            // own share of stage kt + 1 has landed; what may be out are the stages behind it
+            wait_loads<(LEFT - 1 < NST - 2 ? LEFT - 1 : NST - 2) * (GPW + 1)>();
+            __syncthreads();                             // ... everyone's; and nobody reads stage kt any more
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int LPC = (GPW + TN) / TN;             // loads per column block
+#pragma unroll
+        for (int y = 0; y < TN; ++y) {
+            if constexpr (LEFT >= NST) {
+#pragma unroll
+                for (int i = y * LPC; i < (y + 1) * LPC && i <= GPW; ++i) issue_one(kt + NST, slot, i);
+            }
+#pragma unroll
+            for (int x = 0; x < H; ++x) {
+                acc[y][x + H] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[y], fa[x], acc[y][x + H], 0, 0, 0, sw[y], 0, sa[x]);
+                if (LEFT > 0 && y == TN - 1) read_a(nx, x, x);
+            }
+            if constexpr (LEFT > 0) read_w(nx, y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = next;
+    };
+    int kt = 0;
+    for (; kt + NST < nkt; ++kt) stage(kt, std::integral_constant<int, NST>{});
+    if (NST > 3 && kt + 3 < nkt) stage(kt++, std::integral_constant<int, 3>{});
+    if (NST > 2 && kt + 2 < nkt) stage(kt++, std::integral_constant<int, 2>{});
+    if (kt + 1 < nkt) stage(kt++, std::integral_constant<int, 1>{});
+    stage(kt, std::integral_constant<int, 0>{});
+    // (every load has landed: the last hand-over waited for all)
+    if (g.pieces > 1) {                                  // [piece][row][column], rows of n_out rounded up to 4
+        const int ldn = (g.n_out + 3) & ~3;
+#pragma unroll
+        for (int x = 0; x < TM; ++x) {
+            const int row = m0 + (wm * TM + x) * 16 + l16;
+            if (row >= g.m) continue;
+#pragma unroll
+            for (int y = 0; y < TN; ++y) {
+                const int col = n0 + (wn * TN + y) * 16 + kgrp * 4;
+                if (col < g.n_out) *reinterpret_cast<f32x4_t*>(g.ws + ((long)piece * g.m + row) * ldn + col) = acc[y][x];
+            }
+        }
+        return;
     }
+    f32x4_t bias[TN];
+#pragma unroll
+    for (int y = 0; y < TN; ++y) bias[y] = fp8_bias(g, n0 + (wn * TN + y) * 16 + kgrp * 4);
+    const bool wide = g.n_out % 8 == 0;
 #pragma unroll
     for (int x = 0; x < TM; ++x) {
         const int row = m0 + (wm * TM + x) * 16 + l16;
-        if (row >= g.m) continue;
 #pragma unroll
-        for (int y = 0; y < TN; ++y) {
-            const int col = n0 + (wn * TN + y) * 16 + kgrp * 4;
-            if (col < g.n_out) fp8_store(g, row, col, acc[y][x]);
+        for (int y = 0; y < TN; y += 2) {
+            const f32x4_t u = fp8_finish(g, acc[y][x] + bias[y]), v = fp8_finish(g, acc[y + 1][x] + bias[y + 1]);
+            const int col = n0 + (wn * TN + y) * 16;
+            if (wide) {
+                // lanes of neighbouring kgrp swap quads of two column blocks: 8 adjacent columns each, 64 bytes of a row by four lanes
+                typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
+                const u32x2_t p = __builtin_bit_cast(u32x2_t, __builtin_convertvector(u, bf16x4_t));
+                const u32x2_t q = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, bf16x4_t));
+                const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+                const int c = col + (kgrp & 1) * 16 + (kgrp & 2) * 4;
+                if (row < g.m && c < g.n_out)
+                    *reinterpret_cast<i32x4_t*>(g.out + (long)row * g.n_out + c) = i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+            } else if (row < g.m) {
+                if (col + kgrp * 4 < g.n_out) fp8_store(g, row, col + kgrp * 4, u);
+                if (col + 16 + kgrp * 4 < g.n_out) fp8_store(g, row, col + 16 + kgrp * 4, v);
+            }
         }
     }
 }
 
+// Adds the pieces of 4 adjacent columns in order.
+__global__ void __launch_bounds__(256)
+gemm_fp8_join_kernel(Fp8Product g, long quads) {
+    const long id = (long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= quads) return;
+    const int per_row = (g.n_out + 3) / 4;
+    const long row = id / per_row;
+    const int col = (int)(id - row * per_row) * 4;
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = 0; p < g.pieces; ++p) s += *reinterpret_cast<const f32x4_t*>(g.ws + ((long)p * g.m + row) * (per_row * 4) + col);
+    fp8_store(g, (int)row, col, fp8_finish(g, s + fp8_bias(g, col)));
+}
+
 template <int TM, int TN, int WR, int WC, int NST, int OCC>
-static hipError_t launch_product_tile(Fp8Product g, hipStream_t st) {
+static void launch_product_tile(Fp8Product g, hipStream_t st) {
     constexpr int BM = WR * TM * 16, BN = WC * TN * 16;
     g.tiles_m = (g.m + BM - 1) / BM;
     g.tiles_n = (g.n_out + BN - 1) / BN;
-    const unsigned grid = (unsigned)((long)g.tiles_m * g.tiles_n);
-    gemm_fp8_kernel<TM, TN, WR, WC, NST, OCC><<<grid, WR * WC * 64, 0, st>>>(g);
-    return hipGetLastError();
+    gemm_fp8_kernel<TM, TN, WR, WC, NST, OCC><<<(unsigned)((long)g.tiles_m * g.tiles_n * g.pieces), WR * WC * 64, 0, st>>>(g);
 }
 
-size_t fp8_product_workspace_bytes(int, int, int) { return 0; }
+size_t fp8_product_workspace_bytes(int m, int n_out, int blocks) {
+    const Fp8Plan p = fp8_plan(m, n_out, blocks, true, compute_units());
+    return p.pieces > 1 ? (size_t)p.pieces * m * ((n_out + 3) / 4 * 4) * sizeof(float) : 0;
+}
 
 hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
-    return launch_product_tile<2, 2, 2, 2, 3, 3>(g, st);
+    const size_t need = fp8_product_workspace_bytes(g.m, g.n_out, g.blocks);
+    const Fp8Plan p = fp8_plan(g.m, g.n_out, g.blocks, need > 0 && g.ws && g.ws_bytes >= need, compute_units());
+    g.pieces = p.pieces;
+    switch (p.tile) {
+        case FP8_64x64: launch_product_tile<2, 2, 2, 2, 4, 2>(g, st); break;
+        case FP8_128x128: launch_product_tile<4, 4, 2, 2, 2, 2>(g, st); break;
+        default: launch_product_tile<8, 4, 2, 4, 2, 2>(g, st); break;
+    }
+    if (p.pieces > 1) {
+        const long quads = (long)g.m * ((g.n_out + 3) / 4);
+        gemm_fp8_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, quads);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace ps

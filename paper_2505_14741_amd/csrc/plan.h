@@ -287,6 +287,22 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
     return (size_t)p.nsplit * batch * tokens * Nn * sizeof(float);
 }
 
+// ---- 8-bit products (gemm_fp8.hip): which tile, and how many pieces of k
+enum Fp8TileId { FP8_64x64, FP8_128x128, FP8_256x256 };
+struct Fp8Plan { int tile, pieces; };
+constexpr Fp8Plan fp8_plan(int m, int n_out, int blocks, bool split, int cus) {
+    Fp8Plan p{};
+    const auto tiles = [&](int b) { return ((long)m + b - 1) / b * (((long)n_out + b - 1) / b); };
+    p.tile = tiles(256) >= cus ? FP8_256x256 : tiles(128) >= cus ? FP8_128x128 : FP8_64x64;
+    p.pieces = 1;
+    if (split && p.tile == FP8_64x64) {
+        long n = 2L * cus / tiles(64);
+        if (n > blocks / 8) n = blocks / 8;
+        if (n >= 2) p.pieces = (int)n;
+    }
+    return p;
+}
+
 // ---- cross attention: query rows per workgroup, and pieces of the keys.  A function of the sample's shape only, never of the batch.
 // resident: all keys in LDS (bf16), which has to hold two such workgroups.
 struct CrossPlan { int block, nsplit; bool resident; };
