@@ -142,7 +142,7 @@ __device__ __forceinline__ void fp8_store(const Fp8Product& g, int row, int col,
 // A stage has two halves of TM / 2 row blocks.  The first goes row block by row block: as soon as the products of one are issued, its
 // registers are read again with the one TM / 2 further down.  Then the next stage's data are waited for and the slot of this one, all of
 // whose fragments are in registers, is requested anew; the second half goes column block by column block and reads the next stage's W, and
-// in its last column the next stage's first A fragments.  So one set of registers per operand is enough (128 x 64 outputs a wave).
+// in its last column the next stage's first A fragments.  So one set of registers per operand is enough.
 template <int TM, int TN, int WR, int WC, int NST, int OCC>
 __global__ void __launch_bounds__(WR * WC * 64, OCC)
 gemm_fp8_kernel(Fp8Product g) {
@@ -342,8 +342,8 @@ hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
     g.pieces = p.pieces;
     switch (p.tile) {
         case FP8_64x64: launch_product_tile<2, 2, 2, 2, 4, 2>(g, st); break;
-        case FP8_128x128: launch_product_tile<4, 4, 2, 2, 2, 2>(g, st); break;
-        default: launch_product_tile<8, 4, 2, 4, 2, 2>(g, st); break;
+        case FP8_128x128: launch_product_tile<2, 4, 4, 2, 3, 2>(g, st); break;
+        default: launch_product_tile<6, 4, 2, 4, 2, 2>(g, st); break;
     }
     if (p.pieces > 1) {
         const long quads = (long)g.m * ((g.n_out + 3) / 4);

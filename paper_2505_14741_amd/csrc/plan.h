@@ -288,17 +288,39 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 }
 
 // ---- 8-bit products (gemm_fp8.hip): which tile, and how many pieces of k
-enum Fp8TileId { FP8_64x64, FP8_128x128, FP8_256x256 };
+// Us of a round of workgroups: fixed + blocks of 128 k * stage; `lone`: up to one workgroup per compute unit where two fit.
+// Measured, us on 64 x 64 / 128 x 128 / 192 x 256 tiles (operands that change from call to call): 112 rows x 7680, k = 1920 9.3 / 10.6 / 17.7;
+// 448 x 7680 15.7 / 11.7 / 19.5; 1100 x 5760 25.8 / 21.3 / 20.9; 1100 x 1920, k = 7680 38.8 / 30.2 / 58; 4516 x 1920, k = 7680 108 / 92 / 62;
+// 17776 x 5760, k = 1920 333 / 243 / 192; 17776 x 1920, k = 7680 422 / 302 / 234.  (256 x 256: 190 and 260 on the last two, 79 at 4516 rows;
+// 128 x 128 in 4 waves, two workgroups per unit 207, 274, 94 and 42 at 1100 rows.)
+enum Fp8TileId { FP8_64x64, FP8_128x128, FP8_192x256, FP8_TILES };
+struct Fp8Tile { int bm, bn, per_cu; float fixed, stage, lone_fixed, lone_stage; };
+constexpr Fp8Tile kFp8Tiles[FP8_TILES] = {
+    {64, 64, 2, 3.0f, 0.39f, 4.0f, 0.15f},               // 4 waves of 32 x 32
+    {128, 128, 1, 4.0f, 0.44f, 4.0f, 0.44f},             // 8 waves of 32 x 64
+    {192, 256, 1, 5.5f, 1.1f, 5.5f, 1.1f},               // 8 waves of 96 x 64
+};
 struct Fp8Plan { int tile, pieces; };
+constexpr long fp8_tile_count(int id, int m, int n_out) {
+    return ((long)m + kFp8Tiles[id].bm - 1) / kFp8Tiles[id].bm * (((long)n_out + kFp8Tiles[id].bn - 1) / kFp8Tiles[id].bn);
+}
 constexpr Fp8Plan fp8_plan(int m, int n_out, int blocks, bool split, int cus) {
     Fp8Plan p{};
-    const auto tiles = [&](int b) { return ((long)m + b - 1) / b * (((long)n_out + b - 1) / b); };
-    p.tile = tiles(256) >= cus ? FP8_256x256 : tiles(128) >= cus ? FP8_128x128 : FP8_64x64;
+    float best = 0.f;
+    for (int id = 0; id < FP8_TILES; ++id) {
+        const Fp8Tile& t = kFp8Tiles[id];
+        const long n = fp8_tile_count(id, m, n_out), slots = (long)t.per_cu * cus;
+        const float rounds = n > 4 * slots ? (float)n / slots : (float)((n + slots - 1) / slots);    // (many rounds drift apart)
+        const float us = n <= cus ? t.lone_fixed + blocks * t.lone_stage : rounds * (t.fixed + blocks * t.stage);
+        if (id == 0 || us < best) { best = us; p.tile = id; }
+    }
     p.pieces = 1;
     if (split && p.tile == FP8_64x64) {
-        long n = 2L * cus / tiles(64);
+        // tiles that leave compute units idle: pieces of 8 blocks at least, and three of them, to be worth the second launch (1920 columns,
+        // k = 7680, us whole / split: 1 to 112 rows 16 / 13.5 in 7 pieces, 200 16.4 / 14.8 in 4, 448 in two 16.7 / 19.6)
+        long n = 2L * cus / fp8_tile_count(FP8_64x64, m, n_out);
         if (n > blocks / 8) n = blocks / 8;
-        if (n >= 2) p.pieces = (int)n;
+        if (n >= 3) p.pieces = (int)n;
     }
     return p;
 }
