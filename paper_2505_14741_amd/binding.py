@@ -279,43 +279,55 @@ def _need(ok: bool, where: str, what: str, status: int = PS_ERR_SHAPE):
         raise PsError(status, f"{where}: {what}")
 
 
-def _need_here(where: str, *tensors: Optional[torch.Tensor]):
+def _need_here(where: str, first: torch.Tensor, *others: Optional[torch.Tensor]):
     """Kernels run on the current device and its current stream, on memory of that device."""
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
-    for t in tensors:
-        _need(t is None or (t.is_cuda and t.get_device() == dev), where, "tensors must lie on the current GPU")
+    dev = first.get_device()
+    ok = dev >= 0 and dev == torch._C._cuda_getDevice()
+    for t in others:
+        ok = ok and (t is None or t.get_device() == dev)
+    if not ok:
+        raise PsError(PS_ERR_SHAPE, f"{where}: tensors must lie on the current GPU")
+
+
+# What a call checks and computes from types, shapes and strides alone is done once for each (these are microseconds); addresses and devices
+# are looked at in every call.
+@functools.lru_cache(maxsize=1024)
+def _cross_plan(dtypes, q, qs, k, ks, v, vs, o, os_, lens, mask, scale, device):
+    w = "cross_attn"
+    _need(len(q) == 4 and len(k) == 4 and v == k, w, "q [B, Nq, H, d], k and v [B, Nk, Hkv, d]")
+    B, N, H, d = q
+    _need(k[0] == B and k[3] == d, w, "k and v must have q's batch and head_dim")
+    dt = _CODE.get(dtypes[0])
+    _need(dt is not None and dtypes[1] == dtypes[0] and dtypes[2] == dtypes[0], w, "float32 or bfloat16, the same for q, k and v", PS_ERR_DTYPE)
+    _need(o == q, w, "out must have q's shape")
+    _need(dtypes[3] == dtypes[0], w, "out must have q's type", PS_ERR_DTYPE)
+    _need(qs[3] == ks[3] == vs[3] == os_[3] == 1, w, "the elements of a head must be contiguous")
+    mask_batch = 0
+    if lens is not None:
+        _need(lens[0] == torch.int32, w, "kv_lens must be int32", PS_ERR_DTYPE)
+        _need(lens[1] == (B,) and (B <= 1 or lens[2] == (1,)), w, "kv_lens must be [B], contiguous")
+    if mask is not None:
+        _need(mask[0] in (torch.bool, torch.uint8), w, "key_mask must be bool or uint8", PS_ERR_DTYPE)
+        _need(mask[1] == (B, k[1]) and (k[1] <= 1 or mask[2][1] == 1), w, "key_mask must be [B, Nk], rows contiguous")
+        mask_batch = mask[2][0] if B > 1 else 0
+    s = _CrossShape(B, N, k[1], H, k[2], d, dt, scale, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                    os_[0], os_[1], os_[2], mask_batch)
+    return C.byref(s), lib().cross_attn_workspace_bytes(C.byref(s))
 
 
 def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, kv_lens: Optional[torch.Tensor] = None,
                key_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q [B, Nq, H, d]; k, v [B, Nk, Hkv, d], any strides whose elements of a head are contiguous; kv_lens int32 [B]; key_mask bool
     or uint8 [B, Nk], also expanded from one sample's.  A query without a key that counts gets zeros."""
-    w = "cross_attn"
-    _need(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape, w, "q [B, Nq, H, d], k and v [B, Nk, Hkv, d]")
-    B, N, H, d = q.shape
-    _need(k.shape[0] == B and k.shape[3] == d, w, "k and v must have q's batch and head_dim")
-    dt = _CODE.get(q.dtype)
-    _need(dt is not None and k.dtype == q.dtype and v.dtype == q.dtype, w, "float32 or bfloat16, the same for q, k and v", PS_ERR_DTYPE)
     if out is None:
-        out = torch.empty((B, N, H, d), dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape, w, "out must have q's shape")
-    _need(out.dtype == q.dtype, w, "out must have q's type", PS_ERR_DTYPE)
-    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()
-    _need(qs[3] == ks[3] == vs[3] == os_[3] == 1, w, "the elements of a head must be contiguous")
-    mask_batch = 0
-    if kv_lens is not None:
-        _need(kv_lens.dtype == torch.int32, w, "kv_lens must be int32", PS_ERR_DTYPE)
-        _need(kv_lens.shape == (B,) and kv_lens.is_contiguous(), w, "kv_lens must be [B], contiguous")
-    if key_mask is not None:
-        _need(key_mask.dtype in (torch.bool, torch.uint8), w, "key_mask must be bool or uint8", PS_ERR_DTYPE)
-        _need(key_mask.shape == (B, k.shape[1]) and (k.shape[1] <= 1 or key_mask.stride(1) == 1), w, "key_mask must be [B, Nk], rows contiguous")
-        mask_batch = key_mask.stride(0) if B > 1 else 0
-    _need_here(w, q, k, v, out, kv_lens, key_mask)
-    s = _CrossShape(B, N, k.shape[1], H, k.shape[2], d, dt, float(scale), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                    os_[0], os_[1], os_[2], mask_batch)
-    n = lib().cross_attn_workspace_bytes(C.byref(s))
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape, n = _cross_plan((q.dtype, k.dtype, v.dtype, out.dtype), q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), out.shape, out.stride(),
+                           None if kv_lens is None else (kv_lens.dtype, kv_lens.shape, kv_lens.stride()),
+                           None if key_mask is None else (key_mask.dtype, key_mask.shape, key_mask.stride()), float(scale), q.get_device())
+    _need_here("cross_attn", q, k, v, out, kv_lens, key_mask)
     ws = _workspace(n, q.device)
-    _check(lib().cross_attn(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_lens), _ptr(key_mask), _ptr(out), C.byref(s), _ptr(ws), n, _stream()), w)
+    _check(lib().cross_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(kv_lens), _ptr(key_mask), out.data_ptr(), shape, _ptr(ws), n, _stream()),
+           "cross_attn")
     return out
 
 
@@ -332,60 +344,72 @@ def fp8_quantize(x: torch.Tensor):
     blocks = (cols + 127) // 128
     q = torch.empty((rows, blocks * 128), dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.empty((blocks, (rows + 15) // 16 * 16), dtype=torch.float8_e8m0fnu, device=x.device)
-    _check(lib().fp8_quantize(_ptr(x), _ptr(q), _ptr(scale), rows, cols, x.stride(0), dt, _stream()), w)
+    _check(lib().fp8_quantize(x.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, x.stride(0), dt, _stream()), w)
     return q, scale
+
+
+@functools.lru_cache(maxsize=1024)
+def _fp8_plan(dtypes, a, a_scale, w, w_scale, bias, out, use_workspace, device):
+    f = "dit_linear_fp8"
+    _need(len(a) == 2 and len(w) == 2 and a[1] == w[1] and a[1] % 128 == 0 and a[1] > 0, f, "a [M, kp] and w [n_out, kp], kp a multiple of 128")
+    M, K = a
+    Nn = w[0]
+    _need(dtypes[:4] == (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float8_e4m3fn, torch.float8_e8m0fnu), f,
+          "values in float8_e4m3fn, scales in float8_e8m0fnu", PS_ERR_DTYPE)
+    _need(dtypes[4] == torch.float32, f, "bias must be float32", PS_ERR_DTYPE)
+    _need(a_scale == (K // 128, (M + 15) // 16 * 16) and w_scale == (K // 128, (Nn + 15) // 16 * 16), f, "scales [kp / 128, rows rounded up to 16]")
+    _need(bias == (Nn,), f, "bias must be [n_out]")
+    _need(out == (M, Nn), f, "out must be [M, n_out]")
+    _need(dtypes[5] == torch.bfloat16, f, "out must be bfloat16", PS_ERR_DTYPE)
+    return M, Nn, K, lib().dit_linear_fp8_workspace_bytes(M, Nn, K) if use_workspace else 0
 
 
 def dit_linear_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor, act: int = 0,
                    out: Optional[torch.Tensor] = None, use_workspace: bool = True) -> torch.Tensor:
     """act(a w^T + bias) of operands from fp8_quantize: a of [M, K] and w of [n_out, K]; bias float32 [n_out], out bfloat16."""
     f = "dit_linear_fp8"
-    _need(a.dim() == 2 and w.dim() == 2 and a.shape[1] == w.shape[1] and a.shape[1] % 128 == 0 and a.shape[1] > 0, f,
-          "a [M, kp] and w [n_out, kp], kp a multiple of 128")
-    M, K = a.shape
-    Nn = w.shape[0]
-    _need(a.dtype == torch.float8_e4m3fn and w.dtype == torch.float8_e4m3fn and a_scale.dtype == torch.float8_e8m0fnu and
-          w_scale.dtype == torch.float8_e8m0fnu, f, "values in float8_e4m3fn, scales in float8_e8m0fnu", PS_ERR_DTYPE)
-    _need(bias.dtype == torch.float32, f, "bias must be float32", PS_ERR_DTYPE)
-    _need(a_scale.shape == (K // 128, (M + 15) // 16 * 16) and w_scale.shape == (K // 128, (Nn + 15) // 16 * 16), f,
-          "scales [kp / 128, rows rounded up to 16]")
-    _need(bias.shape == (Nn,), f, "bias must be [n_out]")
     if out is None:
-        out = torch.empty((M, Nn), dtype=torch.bfloat16, device=a.device)
-    _need(out.shape == (M, Nn), f, "out must be [M, n_out]")
-    _need(out.dtype == torch.bfloat16, f, "out must be bfloat16", PS_ERR_DTYPE)
+        _need(a.dim() == 2 and w.dim() == 2, f, "a [M, kp] and w [n_out, kp]")
+        out = torch.empty((a.shape[0], w.shape[0]), dtype=torch.bfloat16, device=a.device)
+    M, Nn, K, nb = _fp8_plan((a.dtype, a_scale.dtype, w.dtype, w_scale.dtype, bias.dtype, out.dtype), a.shape, a_scale.shape, w.shape, w_scale.shape,
+                             bias.shape, out.shape, use_workspace, a.get_device())
     _need(a.is_contiguous() and a_scale.is_contiguous() and w.is_contiguous() and w_scale.is_contiguous() and bias.is_contiguous() and
           out.is_contiguous(), f, "operands must be contiguous")
     _need_here(f, a, a_scale, w, w_scale, bias, out)
-    nb = _bytes("dit_linear_fp8_workspace_bytes", M, Nn, K) if use_workspace else 0
     ws = _workspace(nb, a.device)
-    _check(lib().dit_linear_fp8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(out), M, Nn, K, int(act),
+    _check(lib().dit_linear_fp8(a.data_ptr(), a_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), bias.data_ptr(), out.data_ptr(), M, Nn, K, int(act),
                                 _ptr(ws), nb, _stream()), f)
     return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _gnorm_plan(dtypes, x, xs, o, os_, affine, groups, eps, act, device):
+    w = "group_norm"
+    _need(len(x) == 3 and x[2] >= 1, w, "x must be [B, positions, C]")
+    dt = _CODE.get(dtypes[0])
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    _need(o == x, w, "out must have x's shape")
+    _need(dtypes[1] == dtypes[0], w, "out must have x's type", PS_ERR_DTYPE)
+    _need(x[2] == 1 or (xs[2] == 1 and os_[2] == 1), w, "channels must be contiguous")
+    for t in affine:
+        _need(t is None or t[0] == torch.float32, w, "gamma and beta must be float32", PS_ERR_DTYPE)
+        _need(t is None or (t[1] == (x[2],) and (x[2] == 1 or t[2] == (1,))), w, "gamma and beta must be [C], contiguous")
+    s = _GroupNormShape(x[0], x[1], x[2], groups, act, dt, eps, xs[0], xs[1], os_[0], os_[1])
+    return C.byref(s), lib().group_norm_workspace_bytes(x[0], x[1], x[2], groups, dt)
 
 
 def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
                act: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [B, positions, C] (channels contiguous, other strides free), float32 or bfloat16; gamma, beta float32 [C]; act 0 none, 1
     tanh-GELU, 2 SiLU.  out may be x."""
-    w = "group_norm"
-    _need(x.dim() == 3 and x.shape[2] >= 1, w, "x must be [B, positions, C]")
-    B, S, ch = x.shape
-    dt = _CODE.get(x.dtype)
-    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
     if out is None:
-        out = torch.empty((B, S, ch), dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape, w, "out must have x's shape")
-    _need(out.dtype == x.dtype, w, "out must have x's type", PS_ERR_DTYPE)
-    _need(ch == 1 or (x.stride(2) == 1 and out.stride(2) == 1), w, "channels must be contiguous")
-    for t in (gamma, beta):
-        _need(t is None or t.dtype == torch.float32, w, "gamma and beta must be float32", PS_ERR_DTYPE)
-        _need(t is None or (t.shape == (ch,) and t.is_contiguous()), w, "gamma and beta must be [C], contiguous")
-    _need_here(w, x, out, gamma, beta)
-    s = _GroupNormShape(B, S, ch, int(groups), int(act), dt, float(eps), x.stride(0), x.stride(1), out.stride(0), out.stride(1))
-    n = _bytes("group_norm_workspace_bytes", B, S, ch, int(groups), dt)
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    shape, n = _gnorm_plan((x.dtype, out.dtype), x.shape, x.stride(), out.shape, out.stride(),
+                           (None if gamma is None else (gamma.dtype, gamma.shape, gamma.stride()),
+                            None if beta is None else (beta.dtype, beta.shape, beta.stride())), int(groups), float(eps), int(act), x.get_device())
+    _need_here("group_norm", x, out, gamma, beta)
     ws = _workspace(n, x.device)
-    _check(lib().group_norm(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(out), C.byref(s), _ptr(ws), n, _stream()), w)
+    _check(lib().group_norm(x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), shape, _ptr(ws), n, _stream()), "group_norm")
     return out
 
 
