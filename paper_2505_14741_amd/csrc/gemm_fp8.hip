@@ -289,7 +289,7 @@ gemm_fp8_kernel(Fp8Product g) {
     for (int x = 0; x < TM; ++x) {
         const int row = m0 + (wm * TM + x) * 16 + l16;
 #pragma unroll
-        for (int y = 0; y < TN; y += 2) {
+        for (int y = 0; y + 1 < TN; y += 2) {
             const f32x4_t u = fp8_finish(g, acc[y][x] + bias[y]), v = fp8_finish(g, acc[y + 1][x] + bias[y + 1]);
             const int col = n0 + (wn * TN + y) * 16;
             if (wide) {
@@ -305,6 +305,10 @@ gemm_fp8_kernel(Fp8Product g) {
                 if (col + kgrp * 4 < g.n_out) fp8_store(g, row, col + kgrp * 4, u);
                 if (col + 16 + kgrp * 4 < g.n_out) fp8_store(g, row, col + 16 + kgrp * 4, v);
             }
+        }
+        if constexpr (TN % 2) {
+            const int col = n0 + (wn * TN + TN - 1) * 16 + kgrp * 4;
+            if (row < g.m && col < g.n_out) fp8_store(g, row, col, fp8_finish(g, acc[TN - 1][x] + bias[TN - 1]));
         }
     }
 }
@@ -343,6 +347,7 @@ hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
     switch (p.tile) {
         case FP8_64x64: launch_product_tile<2, 2, 2, 2, 4, 2>(g, st); break;
         case FP8_128x128: launch_product_tile<2, 4, 4, 2, 3, 2>(g, st); break;
+        case FP8_192x192: launch_product_tile<6, 3, 2, 4, 3, 2>(g, st); break;
         default: launch_product_tile<6, 4, 2, 4, 2, 2>(g, st); break;
     }
     if (p.pieces > 1) {

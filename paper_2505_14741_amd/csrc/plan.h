@@ -289,16 +289,17 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 
 // ---- 8-bit products (gemm_fp8.hip): which tile, and how many pieces of k
 // Us of a round of workgroups: fixed + blocks of 128 k * stage; `lone`: up to one workgroup per compute unit where two fit.
-// Measured, us on 64 x 64 / 128 x 128 / 192 x 256 tiles (operands that change from call to call): 112 rows x 7680, k = 1920 9.3 / 10.6 / 17.7;
-// 448 x 7680 15.7 / 11.7 / 19.5; 1100 x 5760 25.8 / 21.3 / 20.9; 1100 x 1920, k = 7680 38.8 / 30.2 / 58; 4516 x 1920, k = 7680 108 / 92 / 62;
-// 17776 x 5760, k = 1920 333 / 243 / 192; 17776 x 1920, k = 7680 422 / 302 / 234.  (256 x 256: 190 and 260 on the last two, 79 at 4516 rows;
-// 128 x 128 in 4 waves, two workgroups per unit 207, 274, 94 and 42 at 1100 rows.)
-enum Fp8TileId { FP8_64x64, FP8_128x128, FP8_192x256, FP8_TILES };
+// Measured, us on 64 x 64 / 128 x 128 / 192 x 192 / 192 x 256 tiles (operands that change from call to call): 448 rows x 7680, k = 1920
+// 15.9 / 12.0 / 17.9 / 19.9; 1100 x 5760 27.2 / 22.0 / 19.6 / 20.7; 1100 x 1920, k = 7680 39 / 31 / 48 / 58; 4516 x 1920, k = 7680 111 / 92 /
+// 58 / 63, behind the quantization of its rows, from memory, 115 / 95 / 61 / 76 (the third stage); 17776 x 5760, k = 1920 338 / 249 / 210 / 197;
+// 17776 x 1920, k = 7680 430 / 305 / 245 / 239.  (256 x 256: 195 and 263 on the last two, 79 at 4516 rows.)
+enum Fp8TileId { FP8_64x64, FP8_128x128, FP8_192x192, FP8_192x256, FP8_TILES };
 struct Fp8Tile { int bm, bn, per_cu; float fixed, stage, lone_fixed, lone_stage; };
 constexpr Fp8Tile kFp8Tiles[FP8_TILES] = {
     {64, 64, 2, 3.0f, 0.39f, 4.0f, 0.15f},               // 4 waves of 32 x 32
     {128, 128, 1, 4.0f, 0.44f, 4.0f, 0.44f},             // 8 waves of 32 x 64
-    {192, 256, 1, 5.5f, 1.1f, 5.5f, 1.1f},               // 8 waves of 96 x 64
+    {192, 192, 1, 4.0f, 0.95f, 4.0f, 0.95f},             // 8 waves of 96 x 48, three stages
+    {192, 256, 1, 5.5f, 1.1f, 5.5f, 1.1f},               // 8 waves of 96 x 64, two stages
 };
 struct Fp8Plan { int tile, pieces; };
 constexpr long fp8_tile_count(int id, int m, int n_out) {
