@@ -52,22 +52,14 @@ __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, lo
 // The reference of a row's exponents moves only where some score of a tile exceeds it by 8 in powers of two (probabilities
 // stay below 2^8, sums far from overflow): a tile then costs no rescaling and no maximum over lanes.
 constexpr float CROSS_AHEAD = 8.0f;
+constexpr float CROSS_SUM_MAX = 0x1p+100f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 __device__ __forceinline__ s16x4_t read_tr16(const bf16_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
 }
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(4))) int i32x4_t;
-// acc + the sum of eight bf16 values
-__device__ __forceinline__ float add_bf16x8(bf16x8_t p, float acc) {
-    const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
-    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 0, 1), ones, acc, false);
-    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 2, 3), ones, acc, false);
-    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 4, 5), ones, acc, false);
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 6, 7), ones, acc, false);
-}
 
 // Stores a row's outputs (16 d blocks of 4 values a lane): lanes of neighbouring kgrp swap quads of two blocks, so that each has 8
 // adjacent values and the four lanes of a row write 64 bytes.
@@ -140,10 +132,10 @@ __device__ __forceinline__ void cross_read_v(const bf16_t* vt, CrossV<HD>& v) {
         }
 }
 
-// Moves the references (in powers of two: times c) where a score of the tile is ahead of one, and what has been summed with them.
-// FIRST: of the row's first tile, nothing has been summed.
-template <int QT, int NB, bool FIRST = false>
-__device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_t (&acc)[QT][NB], float (&m)[QT], float (&l)[QT], float c, float ahead) {
+// FIRST (a row's first tile, nothing has been summed): the reference is the maximum.  Else references move (in powers of two: times c)
+// where a score of the tile is ahead of one, and what has been summed with them.
+template <int QT, int NB, bool FIRST>
+__device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_t (&acc)[QT][NB], float (&m)[QT], f32x4_t (&l)[QT], float c, float ahead) {
     float top[QT];
     bool over = false;
 #pragma unroll
@@ -153,12 +145,8 @@ __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_
         for (int g = 0; g < 4; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], sc[t][g][i]);
-        if constexpr (FIRST) {
-            m[t] = max_xor32(max_xor16(top[t]));
-            l[t] = 0.f;
-        } else {
-            over = over || top[t] > m[t] + ahead;
-        }
+        if constexpr (FIRST) m[t] = max_xor32(max_xor16(top[t]));
+        else over = over || top[t] > m[t] + ahead;
     }
     if (!FIRST && __any(over)) {
 #pragma unroll
@@ -166,37 +154,42 @@ __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_
             const float mn = fmaxf(m[t], max_xor32(max_xor16(top[t])));
             const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f((m[t] - mn) * c);      // exp2(-inf) = 0 on the first tile
             m[t] = mn;
-            l[t] *= alpha;
+            l[t][0] *= alpha;                            // (the only one that is looked at)
 #pragma unroll
             for (int d = 0; d < NB; ++d) acc[t][d] *= alpha;
         }
     }
 }
-// Probabilities, rounded to bf16 for the second product and summed as rounded: one key alone has weight 1 exactly.
+// Probabilities, rounded to bf16 for the second product.
 template <int QT>
-__device__ __forceinline__ void cross_weights(const f32x4_t (&sc)[QT][4], const float (&m)[QT], float (&l)[QT], float c, bf16x8_t (&pf)[QT][2]) {
+__device__ __forceinline__ void cross_weights(const f32x4_t (&sc)[QT][4], const float (&m)[QT], float c, bf16x8_t (&pf)[QT][2]) {
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const float mc = m[t] == -INFINITY ? 0.f : m[t] * c;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc));
-            l[t] = add_bf16x8(pf[t][s], l[t]);
-        }
     }
 }
-// acc += V^T P^T
+// acc += V^T P^T, l += 1 P^T: the sums of the probabilities as they were rounded (one key alone has weight 1 exactly), for which the matrix
+// pipes have time and the vector ones have not.  Every lane has its row's whole sum.
 template <int HD, int QT, bool FIRST = false>
-__device__ __forceinline__ void cross_values(const CrossV<HD>& v, const bf16x8_t (&pf)[QT][2], f32x4_t (&acc)[QT][HD / 16]) {
+__device__ __forceinline__ void cross_values(const CrossV<HD>& v, const bf16x8_t (&pf)[QT][2], f32x4_t (&acc)[QT][HD / 16], f32x4_t (&l)[QT]) {
+    const __bf16 one = (__bf16)1.0f;
+    const bf16x8_t ones = {one, one, one, one, one, one, one, one};
+    constexpr f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
             for (int t = 0; t < QT; ++t)
-                acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.f[s][d], pf[t][s], FIRST && s == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc[t][d], 0, 0, 0);
+                acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.f[s][d], pf[t][s], FIRST && s == 0 ? zero : acc[t][d], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t][s], FIRST && s == 0 ? zero : l[t], 0, 0, 0);
+    }
 }
 
 template <int HD, int QT>
@@ -256,10 +249,11 @@ cross_bf16_kernel(CrossArgs a) {
         }
     }
     f32x4_t acc[QT][NB];                                 // O^T: row l16, d = 16 * block + 4 * kgrp + i
-    float m[QT], l[QT];                                  // l: over this lane's keys only
+    f32x4_t l[QT];                                       // [0]: the row's sum
+    float m[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        m[t] = -INFINITY; l[t] = 0.f;
+        m[t] = -INFINITY; l[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -301,15 +295,15 @@ cross_bf16_kernel(CrossArgs a) {
                     for (int t = 0; t < QT; ++t) sc[t][g][i] += bias;
                 }
         }
-        cross_softmax<QT, NB>(sc, acc, m, l, c, ahead);
+        cross_softmax<QT, NB, false>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
-        cross_weights<QT>(sc, m, l, c, pf);
-        cross_values<HD, QT>(vf, pf, acc);
+        cross_weights<QT>(sc, m, c, pf);
+        cross_values<HD, QT>(vf, pf, acc, l);
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int row = r0 + t * 16;
-        const float sum = sum_xor32(sum_xor16(l[t]));
+        const float sum = l[t][0];
         if (a.nsplit > 1) {
             if (row >= a.rows) continue;
             float* p = a.part + ((((long)it.b * a.kv_heads + it.g) * a.nsplit + it.piece) * a.rows + row) * (HD + 4);
@@ -391,21 +385,25 @@ cross_resident_kernel(CrossArgs a, int n) {
     }
     __syncthreads();
     unsigned whole = 0;                                  // tiles all of whose keys count
-    for (int j = 0; j < tiles; ++j) whole |= (__ballot(Bs[j * KT + lane] == 0.f) == ~0ull ? 1u : 0u) << j;
+    bool first_counts = false;                           // some key of the first tile does
+    for (int j = 0; j < tiles; ++j) {
+        const unsigned long long in = __ballot(Bs[j * KT + lane] == 0.f);
+        whole |= (in == ~0ull ? 1u : 0u) << j;
+        if (j == 0) first_counts = in != 0;
+    }
 
     const bf16_t *const k0 = Ks + l16 * LDK + kgrp * (HD == 16 ? 4 : 8), *const v0 = Vs + (4 * kgrp + (l16 >> 2)) * LDV + (l16 & 3) * 4;
-    f32x4_t acc[QT][NB];
-    float m[QT], l[QT];
-    // One tile; the next chunk's queries are requested when the last tile has used this one's.  (K and V fragments requested ahead of
-    // their use do not leave room for four waves per SIMD: 67 us at three, 57 so.)
-    const auto tile = [&](int j, auto first_c) {
-        constexpr bool FIRST = decltype(first_c)::value;
+    f32x4_t acc[QT][NB], l[QT];
+    float m[QT];
+    // One tile of the scores against the first tile's maximum (FIRST: that tile), or with a reference that moves (TRACKED).
+    const auto tile = [&](int j, auto first_c, auto tracked_c) {
+        constexpr bool FIRST = decltype(first_c)::value, TRACKED = decltype(tracked_c)::value;
         f32x4_t sc[QT][4];
-        CrossK<HD> kf;
-        cross_read_k<HD, LDK>(k0 + j * (KT * LDK), kf);
-        cross_scores<HD, QT>(kf, qf, sc);
-        CrossV<HD> vf;
-        if (j == tiles - 1 && chunk + stride < chunks) fetch(chunk + stride);
+        {
+            CrossK<HD> kf;
+            cross_read_k<HD, LDK>(k0 + j * (KT * LDK), kf);
+            cross_scores<HD, QT>(kf, qf, sc);
+        }
         if (!(whole >> j & 1)) {
 #pragma unroll
             for (int g4 = 0; g4 < 4; ++g4) {
@@ -414,24 +412,38 @@ cross_resident_kernel(CrossArgs a, int n) {
                 for (int t = 0; t < QT; ++t) sc[t][g4] += bias;
             }
         }
-        cross_softmax<QT, NB, FIRST>(sc, acc, m, l, c, ahead);
+        if constexpr (FIRST || TRACKED) cross_softmax<QT, NB, FIRST>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
-        cross_weights<QT>(sc, m, l, c, pf);
+        cross_weights<QT>(sc, m, c, pf);
+        CrossV<HD> vf;
         cross_read_v<HD, LDV>(v0 + j * (KT * LDV), vf);
-        cross_values<HD, QT, FIRST>(vf, pf, acc);
+        cross_values<HD, QT, FIRST>(vf, pf, acc, l);
     };
+    const std::true_type yes;
+    const std::false_type no;
     for (; chunk < chunks; chunk += stride) {
-        if (tiles > 0) {
-            tile(0, std::true_type{});
-        } else {
+        // Relative to the first tile's maximum, which is one of the row's scores, sums are at least 1; what they are at most is looked at
+        // behind the last tile, instead of every tile's maxima: rows whose later scores are so much larger are computed again.
+        bool done = false;
+        if (first_counts) {
+            tile(0, yes, no);
+            for (int j = 1; j < tiles; ++j) tile(j, no, no);
+            bool fits = true;
+#pragma unroll
+            for (int t = 0; t < QT; ++t) fits = fits && l[t][0] < CROSS_SUM_MAX;
+            done = __all(fits);
+        }
+        if (!done) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                l[t] = 0.f;
+                m[t] = -INFINITY;
+                l[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
+            for (int j = 0; j < tiles; ++j) tile(j, no, yes);
         }
-        for (int j = 1; j < tiles; ++j) tile(j, std::false_type{});
+        if (chunk + stride < chunks) fetch(chunk + stride);
         // the next queries' loads are waited for here: behind the stores, whose number the compiler cannot know, it would wait for these too
 #pragma unroll
         for (int t = 0; t < QT; ++t)
@@ -439,7 +451,7 @@ cross_resident_kernel(CrossArgs a, int n) {
             for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qf[t][s]));
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const float sum = sum_xor32(sum_xor16(l[t]));
+            const float sum = l[t][0];
             cross_store<NB>(ob + row_at(chunk, t, a.s.o_tok, a.s.o_head, o_lane, 0), acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp,
                             chunk * BQ + t * 16 + l16 < a.rows);
         }
@@ -621,7 +633,7 @@ static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     if (dtype != PS_BF16) cross_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
     else if (p.block == 64) cross_bf16_kernel<HD, 1><<<grid, 256, 0, st>>>(a);
     else if (p.block == 128) cross_bf16_kernel<HD, 2><<<grid, 256, 0, st>>>(a);
-    else if constexpr (HD <= 64) cross_bf16_kernel<HD, 4><<<grid, 256, 0, st>>>(a);
+    else if constexpr (HD <= 64) cross_bf16_kernel<HD, 3><<<grid, 256, 0, st>>>(a);
     if (p.nsplit > 1) {
         const long lines = (long)a.batch * a.kv_heads * a.rows;
         if (dtype == PS_BF16) cross_join_kernel<bf16_t, HD><<<(unsigned)((lines + 3) / 4), 256, 0, st>>>(a, lines);

@@ -336,10 +336,15 @@ constexpr int cross_resident_key_bytes(int head_dim) { return 2 * (head_dim + 8 
 
 constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, int head_dim, int cus) {
     CrossPlan p{};
-    p.block = !bf16 || rows <= 64 ? 64 : rows <= 128 || head_dim == 128 ? 128 : 256;
-    const long items = (long)((rows + p.block - 1) / p.block) * kv_heads, tiles = (kv_len + 63) / 64;
-    long n = 1L * cus / items;                           // two workgroups per compute unit
-    if (n > tiles / 4) n = tiles / 4;                    // 256 keys each at least: the partial sums pass through memory
+    // bf16: 64, 128 or 192 rows, whichever of the last two wastes less; more registers than heads of 128 leave spill (16 heads, 4290 rows x 512
+    // keys: 64 rows 49 us, 128 85).
+    const auto filled = [rows](int block) { return ((long)rows + block - 1) / block * block; };
+    p.block = !bf16 || rows <= 64 || head_dim == 128 ? 64 : rows > 128 && filled(192) <= filled(128) ? 192 : 128;
+    // Pieces of 256 keys at least, as many as there are compute units, twice as many for few rows, whose partial sums are small (us at one /
+    // two per unit: a token of 30 heads, 17776 keys 55 / 35, 60 tokens 57 / 38; 32 tokens of 30 heads over 6 key heads 29 / 36).
+    const long items = (filled(p.block) / p.block) * kv_heads, tiles = (kv_len + 63) / 64;
+    long n = (rows <= 64 ? 2L : 1L) * cus / items;
+    if (n > tiles / 4) n = tiles / 4;
     p.nsplit = n < 2 ? 1 : (int)n;
     p.resident = bf16 && head_dim <= 64 && p.nsplit == 1 && rows >= 256 && tiles * 64 * cross_resident_key_bytes(head_dim) <= 80 * 1024;
     return p;

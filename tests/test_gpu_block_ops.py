@@ -187,6 +187,30 @@ def test_cross_attention_of_a_batch_equals_its_samples(dtype, nq, nk):
     assert torch.equal(whole, B.cross_attn(q, k, v, 0.125, kv_lens=lens))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,heads,kv_heads", [(16, 3, 3), (32, 4, 2), (64, 2, 2), (64, 3, 1), (128, 2, 2)])
+def test_cross_attention_many_rows(dtype, d, heads, kv_heads):
+    """Rows enough to go over the keys again and again, key counts around whole tiles and around what a workgroup can hold, masks that
+    leave nothing in the first tile or at all, scores that grow far beyond the first tile's."""
+    g = gen(d + heads)
+    for nq, nk in ((300, 1), (256, 64), (257, 65), (700, 226), (1111, 256), (300, 257), (431, 448), (333, 832)):
+        print(f"cross_attn {dtype} d={d} heads={heads}/{kv_heads} q={nq} k={nk}", flush=True)
+        q, k, v = randn(g, 4, nq, heads, d).to(dtype), randn(g, 4, nk, kv_heads, d).to(dtype), randn(g, 4, nk, kv_heads, d).to(dtype)
+        mask = torch.rand(4, nk, generator=g, device=DEV) < 0.8
+        mask[0] = True
+        mask[1, :64] = False
+        mask[2] = False
+        lens = torch.tensor([nk, nk, nk, (nk + 1) // 2], dtype=torch.int32, device=DEV)
+        check_cross(q, k, v, 1.0 / math.sqrt(d))
+        check_cross(q, k, v, 1.0 / math.sqrt(d), kv_lens=lens, key_mask=mask)
+        steep = (k.float() * torch.linspace(0.01, 150.0, nk, device=DEV)[None, :, None, None]).to(dtype)
+        check_cross(q, steep, v, 1.0, kv_lens=lens)
+        check_cross(q, steep.flip(1), v, 1.0, kv_lens=lens)
+        whole = B.cross_attn(q, k, v, 0.2, kv_lens=lens, key_mask=mask)
+        for b in range(4):
+            assert torch.equal(whole[b:b + 1], B.cross_attn(q[b:b + 1], k[b:b + 1], v[b:b + 1], 0.2, kv_lens=lens[b:b + 1], key_mask=mask[b:b + 1]))
+
+
 # ------------------------------------------------------------------------------------------------- 8-bit blocks
 def quantize_ref(x):
     """(values q, scales) in 64 bits from the definition."""
