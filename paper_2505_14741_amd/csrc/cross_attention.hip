@@ -503,7 +503,7 @@ cross_join_kernel(CrossArgs a, long lines) {
 // ------------------------------------------------------------------------------------ fp32
 // The same tiles with full fp32 products (v_mfma_f32_16x16x4_f32), probabilities in fp32 and exponentials as exact as expf.
 template <int HD>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, HD >= 128 ? 2 : HD == 64 ? 3 : 4)
 cross_f32_kernel(CrossArgs a) {
     constexpr int KT = 64, LD = HD + 4, NB = HD / 16, BQ = 64, CH = HD / 4, LOADS = KT * CH / 256;
     __shared__ __attribute__((aligned(16))) float Ks[KT * LD], Vs[KT * LD];
@@ -553,22 +553,31 @@ cross_f32_kernel(CrossArgs a) {
             fetch((j + 1) * KT);
         }
         if (counts == 0) continue;
-        f32x4_t sc[4];
+        const int blocks = min(4, (keys - j * KT + 15) / 16);        // 16-key blocks with a key in them
+        const bool whole = counts == ~0ull;
         const unsigned long long mine = counts >> (4 * kgrp);
-        float top = -INFINITY;
+        f32x4_t sc[4];
+        float top = -INFINITY, low = INFINITY;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             sc[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (g < blocks) {
 #pragma unroll
-            for (int d = 0; d < NB; ++d) {
-                const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + (g * 16 + l16) * LD + d * 16 + kgrp * 4);
+                for (int d = 0; d < NB; ++d) {
+                    const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + (g * 16 + l16) * LD + d * 16 + kgrp * 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[d][e], sc[g], 0, 0, 0);
+                    for (int e = 0; e < 4; ++e) sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[d][e], sc[g], 0, 0, 0);
+                }
+            }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(mine >> (16 * g + i) & 1)) sc[g][i] = -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (!(mine >> (16 * g + i) & 1)) sc[g][i] = -INFINITY;
                 top = fmaxf(top, sc[g][i]);
+                low = fminf(low, sc[g][i]);
             }
         }
         const float mn = fmaxf(m, max_xor32(max_xor16(top)));
@@ -577,13 +586,14 @@ cross_f32_kernel(CrossArgs a) {
         l *= alpha;
 #pragma unroll
         for (int d = 0; d < NB; ++d) acc[d] *= alpha;
+        const bool near = __ballot(low - ref < EXP_NEAR) == 0;       // (of the whole wave; not with keys that do not count)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
+            if (g >= blocks) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sc[g][i] = expf(sc[g][i] - ref);
-                l += sc[g][i];
-            }
+            for (int i = 0; i < 4; ++i) sc[g][i] = near ? exp_near(sc[g][i] - ref) : expf(sc[g][i] - ref);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l += sc[g][i];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
