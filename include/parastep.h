@@ -194,7 +194,7 @@ PS_API int dit_linear(const void* a, const void* w, const float* bias, void* out
  * k and v kv_heads (a divisor): query heads h * (heads / kv_heads) .. share key head h.  head_dim in {16, 32, 64, 128}, its
  * elements contiguous; every other stride is free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0 to repeat
  * an operand; of an extent of 1 they are ignored), so k and v may be the halves of one projection.  Pointers 16-byte aligned; o
- * must not overlap the inputs.  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).  Scores times scale * log2(e) must be
+ * must not overlap the inputs.  batch and heads <= 65535, q_len and kv_len <= 2^24, batch * q_len * heads < 2^29.  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).  Scores times scale * log2(e) must be
  * finite in fp32.  bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32;
  * fp32: everything in fp32.
  * workspace: DEVICE, 256-byte aligned, >= cross_attn_workspace_bytes(...) (may be NULL when that is 0): where the rows of a sample
@@ -216,11 +216,11 @@ PS_API int cross_attn(const void* q, const void* k, const void* v, const int32_t
  *   scale  DEVICE e8m0 bytes [kp / 128][pitch], pitch = rows rounded up to a multiple of 16, filled up with 0
  * fp8_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment, 16 bytes are fastest).  A block's scale is the
  * least power of two >= 2^-127 under which its largest finite |x| is at most 448; values are rounded once, to nearest even; NaN and
- * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^31 blocks. */
+ * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^28 blocks. */
 PS_API int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream);
 
 /* out[m, n_out] = act(a * w^T + bias) for operands in the format above, a of m rows and w of n_out rows, both of k columns; out DEVICE bf16, row-major; act 0 none, 1 tanh-GELU.  bias DEVICE fp32 [n_out].  All pointers
- * 16-byte aligned; out must not overlap the operands; m may be 0; k <= 2^22.  Products are summed 8 at a time as the matrix
+ * 16-byte aligned; out must not overlap the operands; m may be 0; m, n_out <= 2^24, fewer than 2^24 tiles of 64 x 64, k <= 2^22.  Products are summed 8 at a time as the matrix
  * instruction does it, which cuts off what lies below 2^-13 of the largest of the 8 (in the mean 1e-5 of the result's norm), and from
  * there on in fp32: that is why out is bf16 only.
  * workspace: DEVICE, 256-byte aligned, or NULL.  With at least dit_linear_fp8_workspace_bytes(...) of it, shapes whose output tiles

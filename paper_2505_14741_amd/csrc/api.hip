@@ -565,7 +565,7 @@ int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_
     if (dtype != PS_F32 && dtype != PS_BF16) return PS_ERR_DTYPE;
     if (rows < 0 || cols < 1 || rows > (1 << 24) || cols > (1 << 22)) return PS_ERR_SHAPE;
     if (rows == 0) return PS_OK;
-    if ((long)rows * ((cols + 127) / 128) >= (1L << 31)) return PS_ERR_SHAPE;
+    if ((long)rows * ((cols + 127) / 128) >= (1L << 28)) return PS_ERR_SHAPE;        // (threads of a launch stay below 2^32)
     if (rows > 1 && (x_row < cols || x_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
     if (!x || !q || !scale) return PS_ERR_NULL;
     if (!aligned(x, dtype == PS_BF16 ? 2 : 4) || !aligned(q, 16) || !aligned(scale, 16) || q == x || scale == x || q == scale) return PS_ERR_SHAPE;
@@ -581,7 +581,7 @@ size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k) {
 int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out,
                    int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (m < 0 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22) || (act != 0 && act != 1)) return PS_ERR_SHAPE;
-    if (((m + 63L) / 64) * ((n_out + 63L) / 64) >= (1L << 27)) return PS_ERR_SHAPE;
+    if (((m + 63L) / 64) * ((n_out + 63L) / 64) >= (1L << 24)) return PS_ERR_SHAPE;  // (the same)
     if (m == 0) return PS_OK;
     if (!a || !a_scale || !w || !w_scale || !bias || !out) return PS_ERR_NULL;
     if (!aligned(a, 16) || !aligned(w, 16) || !aligned(a_scale, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(out, 16) ||

@@ -466,38 +466,38 @@ __global__ void __launch_bounds__(256)
 cross_join_kernel(CrossArgs a, long lines) {
     constexpr int W = HD / 4, TEAMS = 64 / W;
     const int lane = threadIdx.x & 63, d = lane % W * 4, team = lane / W;
-    const long line = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (line >= lines) return;                           // whole waves
-    const long bg = line / a.rows;
-    const int row = (int)(line - bg * a.rows), b = (int)(bg / a.kv_heads), g = (int)(bg - (long)b * a.kv_heads);
-    const float* p = a.part + (bg * a.nsplit * a.rows + row) * (HD + 4);
-    const long step = (long)a.rows * (HD + 4);
-    float top = -INFINITY;
-    for (int i = lane; i < a.nsplit; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
+    for (long line = (long)blockIdx.x * 4 + (threadIdx.x >> 6); line < lines; line += (long)gridDim.x * 4) {      // (whole waves)
+        const long bg = line / a.rows;
+        const int row = (int)(line - bg * a.rows), b = (int)(bg / a.kv_heads), g = (int)(bg - (long)b * a.kv_heads);
+        const float* p = a.part + (bg * a.nsplit * a.rows + row) * (HD + 4);
+        const long step = (long)a.rows * (HD + 4);
+        float top = -INFINITY;
+        for (int i = lane; i < a.nsplit; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float ref = top == -INFINITY ? 0.f : top;      // (then every weight is zero, and so are the sums)
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
+        for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+        const float ref = top == -INFINITY ? 0.f : top;      // (then every weight is zero, and so are the sums)
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
 #pragma unroll 4
-    for (int i = team; i < a.nsplit; i += TEAMS) {
-        const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-        const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(s[1] - ref) : expf(s[1] - ref);
-        acc += v * w;
-        l = __builtin_fmaf(s[0], w, l);
-    }
+        for (int i = team; i < a.nsplit; i += TEAMS) {
+            const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
+            const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(s[1] - ref) : expf(s[1] - ref);
+            acc += v * w;
+            l = __builtin_fmaf(s[0], w, l);
+        }
 #pragma unroll
-    for (int x = W; x < 64; x *= 2) {
-        l += __shfl_xor(l, x);
+        for (int x = W; x < 64; x *= 2) {
+            l += __shfl_xor(l, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], x);
+            for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], x);
+        }
+        if (team != 0) continue;
+        acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
+        T* o = (T*)a.o + b * a.s.o_batch + cross_row(a, g, row, a.s.o_tok, a.s.o_head) + d;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(o) = __builtin_convertvector(acc, bf16x4_t);
+        else *reinterpret_cast<f32x4_t*>(o) = acc;
     }
-    if (team != 0) return;
-    acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
-    T* o = (T*)a.o + b * a.s.o_batch + cross_row(a, g, row, a.s.o_tok, a.s.o_head) + d;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(o) = __builtin_convertvector(acc, bf16x4_t);
-    else *reinterpret_cast<f32x4_t*>(o) = acc;
 }
 
 // ------------------------------------------------------------------------------------ fp32
@@ -646,8 +646,9 @@ static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     else if constexpr (HD <= 64) cross_bf16_kernel<HD, 3><<<grid, 256, 0, st>>>(a);
     if (p.nsplit > 1) {
         const long lines = (long)a.batch * a.kv_heads * a.rows;
-        if (dtype == PS_BF16) cross_join_kernel<bf16_t, HD><<<(unsigned)((lines + 3) / 4), 256, 0, st>>>(a, lines);
-        else cross_join_kernel<float, HD><<<(unsigned)((lines + 3) / 4), 256, 0, st>>>(a, lines);
+        const unsigned wgs = (unsigned)((lines + 3) / 4 < (1L << 22) ? (lines + 3) / 4 : 1L << 22);
+        if (dtype == PS_BF16) cross_join_kernel<bf16_t, HD><<<wgs, 256, 0, st>>>(a, lines);
+        else cross_join_kernel<float, HD><<<wgs, 256, 0, st>>>(a, lines);
     }
     return hipGetLastError();
 }

@@ -62,7 +62,7 @@ def test_quantize_refuses():
     call = lambda x=FAKE, q=2 * FAKE, s=3 * FAKE, rows=4, cols=100, x_row=100, dtype=1: L.fp8_quantize(x, q, s, rows, cols, x_row, dtype, None)  # noqa: E731
     assert call(dtype=2) == -3
     for bad in (dict(rows=-1), dict(cols=0), dict(rows=(1 << 24) + 1), dict(cols=(1 << 22) + 1), dict(x_row=99), dict(x_row=1 << 41),
-                dict(rows=1 << 24, cols=1 << 15, x_row=1 << 15), dict(x=FAKE + 1), dict(q=2 * FAKE + 8), dict(s=3 * FAKE + 4), dict(q=FAKE), dict(s=FAKE)):
+                dict(rows=1 << 24, cols=1 << 15, x_row=1 << 15), dict(rows=1 << 24, cols=2048, x_row=2048), dict(x=FAKE + 1), dict(q=2 * FAKE + 8), dict(s=3 * FAKE + 4), dict(q=FAKE), dict(s=FAKE)):
         assert call(**bad) == -2, bad
     for name in ("x", "q", "s"):
         assert call(**{name: None}) == -1
@@ -74,7 +74,7 @@ def test_product_refuses():
 
     def call(a=FAKE, a_s=2 * FAKE, w=3 * FAKE, w_s=4 * FAKE, bias=5 * FAKE, out=6 * FAKE, m=4, n=8, k=128, act=0, ws=None, nb=0):
         return L.dit_linear_fp8(a, a_s, w, w_s, bias, out, m, n, k, act, ws, nb, None)
-    for bad in (dict(m=-1), dict(n=0), dict(k=0), dict(m=(1 << 24) + 1), dict(n=(1 << 24) + 1), dict(k=(1 << 22) + 1), dict(act=2), dict(act=-1), dict(m=1 << 24, n=1 << 24),
+    for bad in (dict(m=-1), dict(n=0), dict(k=0), dict(m=(1 << 24) + 1), dict(n=(1 << 24) + 1), dict(k=(1 << 22) + 1), dict(act=2), dict(act=-1), dict(m=1 << 24, n=1 << 24), dict(m=1 << 18, n=1 << 18),
                 dict(a=FAKE + 8), dict(a_s=FAKE + 8), dict(w=FAKE + 8), dict(w_s=FAKE + 4), dict(bias=FAKE + 4), dict(out=FAKE + 2), dict(out=FAKE), dict(out=3 * FAKE)):
         assert call(**bad) == -2, bad
     for name in ("a", "a_s", "w", "w_s", "bias", "out"):
