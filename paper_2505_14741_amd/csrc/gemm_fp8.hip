@@ -16,7 +16,7 @@ namespace ps {
 // A block's scale is the least power of two 2^e, e >= -127, under which its largest finite value is at most 448, the largest of
 // e4m3: with amax = 1.f * 2^x, e = x - 8 where 1.f <= 1.75 and x - 7 above (448 = 1.75 * 2^8).  Multiplying by 2^-e is exact, so
 // each value is rounded once, to the nearest e4m3.  What is not finite becomes NaN and does not count for the scale.
-// Memory binds: 16 lanes take a block, 8 values each.
+// Memory binds: 16 lanes take a block, 8 values each, a 16-byte load of bf16.  17776 x 7680 bf16 (410 MB) 73 us, 5.6 TB/s.
 typedef __attribute__((ext_vector_type(8))) float f32x8_t;
 
 __device__ __forceinline__ unsigned max_u32(unsigned a, unsigned b) { return a > b ? a : b; }
@@ -97,6 +97,8 @@ hipError_t launch_fp8_quantize(int dtype, const void* x, void* q, void* scale, i
 // bits below 2^-13 of the power of two of the largest, and adds exactly enough from there on: 1.3e-5 of the result's norm for
 // Gaussian operands, whatever the 8-bit instruction.  The output is bf16.)  Rows of both operands are contiguous in k;
 // stages of one block (128 bytes of a row) go straight into an LDS ring, with the tile's scale bytes behind them.
+// 17776 x 5760, K = 1920: 199 us, 1.98 PFLOP/s; 4516 x 1920, K = 7680: 61 us, 2.18 (a library's 8-bit product of 8192^3 reaches 2.7); the tiles
+// and what each measured are in plan.h.
 // Slot p of LDS row r holds 16-byte chunk p ^ ((r >> 1) & 7), so that the 16 rows of a fragment read fall into different bank
 // groups.  A lane's 32 bytes of a fragment are chunks l / 16 and 4 + l / 16 of its row, of both operands alike (the instruction's
 // own order of k inside a block does not matter then).
