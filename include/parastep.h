@@ -225,7 +225,8 @@ PS_API int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols,
  * instruction does it, which cuts off what lies below 2^-13 of the largest of the 8 (in the mean 1e-5 of the result's norm), and from
  * there on in fp32: that is why out is bf16 only.
  * workspace: DEVICE, 256-byte aligned, or NULL.  With at least dit_linear_fp8_workspace_bytes(...) of it, shapes whose output tiles
- * occupy a part of the chip are summed in pieces of k; without, whole: the two differ in summation order only. */
+ * occupy a part of the chip are summed in pieces of k; without, whole: the two differ in summation order only.  Which shapes these are
+ * depends on m; summed whole, a row's result does not depend on the rows beside it. */
 PS_API size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k);
 PS_API int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m,
                    int n_out, int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -115,7 +115,22 @@ def test_cross_attention_masks_with_garbage_behind_them(dtype, d, nq, nk):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_cross_attention_of_many_tokens(dtype):
+    """Half a million query rows; the last ones as in a call of their own (from a multiple of the rows of a workgroup on)."""
+    n, cut = (1 << 19) + 7, 384 * 1365
+    g = gen(22)
+    q, k, v = randn(g, 1, n, 1, 64).to(dtype), randn(g, 1, 77, 1, 64).to(dtype), randn(g, 1, 77, 1, 64).to(dtype)
+    out = B.cross_attn(q, k, v, 0.125)
+    check_cross(q[:, cut:], k, v, 0.125)
+    assert torch.equal(out[:, cut:], B.cross_attn(q[:, cut:], k, v, 0.125))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_cross_attention_empty_extents(dtype):
+    many = torch.ones(2, 300, 2, 32, dtype=dtype, device=DEV)
+    assert bool((B.cross_attn(many, many[:, :0], many[:, :0], 0.2) == 0).all())
+    some = B.cross_attn(many, many[:, :40], many[:, :40], 0.2, kv_lens=torch.tensor([0, 40], dtype=torch.int32, device=DEV))
+    assert bool((some[0] == 0).all()) and bool((some[1] == 1).all())
     q = torch.ones(2, 5, 2, 32, dtype=dtype, device=DEV)
     none = torch.empty(2, 0, 2, 32, dtype=dtype, device=DEV)
     assert bool((B.cross_attn(q, none, none, 0.2) == 0).all())
@@ -303,6 +318,32 @@ def test_product_of_blocks(rows, n_out, k, act):
         assert bool((err <= tol).all()), (kw, float((err / tol).max()))
 
 
+def test_product_rows_do_not_depend_on_their_neighbours():
+    """Summed whole, a row has the same bits in a call of its own (64 x 64 tiles) and among hundreds and thousands (the other tiles)."""
+    g = gen(20)
+    for n_out, k in ((1920, 1920), (516, 300)):
+        a, s = B.fp8_quantize(randn(g, 4600, k))
+        w, bias = B.fp8_quantize(randn(g, n_out, k)), randn(g, n_out)
+        full = B.dit_linear_fp8(a, s, *w, bias, act=1, use_workspace=False)
+        for rows in (16, 48, 448, 1104):
+            part = B.dit_linear_fp8(a[:rows], s[:, :rows].contiguous(), *w, bias, act=1, use_workspace=False)
+            assert torch.equal(part, full[:rows]), (n_out, k, rows)
+
+
+def test_quantize_and_product_beyond_32_bits():
+    """600000 rows of 7680: 4.6 10^9 values; the last rows as in a call of their own."""
+    rows, k = 600000, 7680
+    g = gen(21)
+    x = randn(g, 1000, k).bfloat16().repeat(rows // 1000, 1)
+    x[-100:] = randn(g, 100, k).bfloat16()
+    w, bias = B.fp8_quantize(randn(g, 64, k)), randn(g, 64)
+    a, s = B.fp8_quantize(x)
+    b, t = B.fp8_quantize(x[-100:])
+    assert torch.equal(a[-100:].view(torch.uint8), b.view(torch.uint8)) and torch.equal(s[:, -100:].contiguous().view(torch.uint8), t[:, :100].contiguous().view(torch.uint8))
+    out = B.dit_linear_fp8(a, s, *w, bias, use_workspace=False)
+    assert torch.equal(out[-100:], B.dit_linear_fp8(b, t, *w, bias, use_workspace=False))
+
+
 def test_product_spreads_nan_along_its_row_only():
     g = gen(9)
     x, w = randn(g, 40, 300), randn(g, 70, 300)
@@ -380,6 +421,18 @@ def test_group_norm_far_means_outliers_and_constants(dtype):
         x[0, 0] = 3000.0
         check_gnorm(x.to(dtype), 8)
         assert bool((check_gnorm(torch.full((1, positions, 128), 3.0, dtype=dtype, device=DEV), 8) == 0).all())
+
+
+def test_group_norm_beyond_32_bits():
+    """2^22 positions of 768 channels are 3.2 10^9 values: a block of 4096 positions over and over has the block's moments."""
+    g = gen(23)
+    block = randn(g, 1, 4096, 768).bfloat16()
+    x = block.expand(1024, 4096, 768).reshape(1, 1 << 22, 768)
+    out = B.group_norm(x, 32, act=2, out=x)                     # (in place)
+    ref, tol = gnorm_ref(block, 32, None, None, 1e-5, 2)
+    for at in (0, 1 << 21, (1 << 22) - 4096):
+        err = (out[:, at:at + 4096].double() - ref).abs()
+        assert bool((err <= tol + U[torch.bfloat16] * ref.abs() + 1e-30).all()), at
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
