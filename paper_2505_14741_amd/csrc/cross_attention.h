@@ -16,6 +16,7 @@ struct CrossArgs {
     AttnStrides s;
     float* part;                  // scratch of cross_workspace_bytes()
     int nsplit;                   // (set by the launcher)
+    bool stream;                  // (the same: o is larger than STREAM_BYTES)
 };
 size_t cross_workspace_bytes(int dtype, const CrossArgs& a);
 hipError_t launch_cross_attention(int dtype, CrossArgs a, hipStream_t st);

@@ -68,7 +68,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 // Stores a row's outputs (16 d blocks of 4 values a lane): lanes of neighbouring kgrp swap quads of two blocks, so that each has 8
 // adjacent values and the four lanes of a row write 64 bytes.
 template <int NB>
-__device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB], float inv, int kgrp, bool in) {
+__device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB], float inv, int kgrp, bool in, bool stream) {
     if constexpr (NB == 1) {
         if (in) *reinterpret_cast<bf16x4_t*>(row + kgrp * 4) = __builtin_convertvector(acc[0] * inv, bf16x4_t);
     } else {
@@ -79,7 +79,9 @@ __device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB
             const u32x2_t y = __builtin_bit_cast(u32x2_t, __builtin_convertvector(acc[d + 1] * inv, bf16x4_t));
             const auto lo = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false), hi = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
             // even kgrp: block d, values 4 kgrp .. + 7; odd: block d + 1, values 4 (kgrp - 1) .. + 7
-            if (in) *reinterpret_cast<i32x4_t*>(row + (d + (kgrp & 1)) * 16 + (kgrp & 2) * 4) = i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+            if (in)
+                store_streamed(reinterpret_cast<i32x4_t*>(row + (d + (kgrp & 1)) * 16 + (kgrp & 2) * 4),
+                               i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]}, stream);
         }
     }
 }
@@ -316,7 +318,7 @@ cross_bf16_kernel(CrossArgs a) {
             if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m[t] * c};
         } else {
             bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head);
-            cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp, row < a.rows);
+            cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp, row < a.rows, a.stream);
         }
     }
 }
@@ -457,7 +459,7 @@ cross_resident_kernel(CrossArgs a, int n) {
         for (int t = 0; t < QT; ++t) {
             const float sum = l[t][0];
             cross_store<NB>(ob + row_at(chunk, t, a.s.o_tok, a.s.o_head, o_lane, 0), acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp,
-                            chunk * BQ + t * 16 + l16 < a.rows);
+                            chunk * BQ + t * 16 + l16 < a.rows, a.stream);
         }
     }
 }
@@ -632,6 +634,7 @@ template <int HD>
 static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     const CrossPlan p = cross_plan_of(dtype, a);
     a.nsplit = p.nsplit;
+    a.stream = (size_t)a.batch * a.kv_heads * a.rows * HD * (dtype == PS_BF16 ? 2 : 4) > STREAM_BYTES;
     if constexpr (HD <= 64)
     if (p.resident) {
         // workgroups per head: two for every compute unit over the whole batch, a chunk for every wave at least

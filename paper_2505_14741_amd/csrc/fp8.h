@@ -16,6 +16,7 @@ struct Fp8Product {
     float* ws;                // fp32 sums of K pieces, or NULL
     size_t ws_bytes;
     int tiles_m, tiles_n, pieces;     // (set by the launcher)
+    bool stream;              // (the same: out is larger than STREAM_BYTES)
 };
 size_t fp8_product_workspace_bytes(int m, int n_out, int blocks);
 hipError_t launch_fp8_product(Fp8Product g, hipStream_t st);

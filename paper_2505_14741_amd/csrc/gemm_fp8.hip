@@ -301,8 +301,11 @@ gemm_fp8_kernel(Fp8Product g) {
                 const u32x2_t q = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, bf16x4_t));
                 const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
                 const int c = col + (kgrp & 1) * 16 + (kgrp & 2) * 4;
-                if (row < g.m && c < g.n_out)
-                    *reinterpret_cast<i32x4_t*>(g.out + (long)row * g.n_out + c) = i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+                const i32x4_t w = {(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+                if (row < g.m && c < g.n_out) {
+                    i32x4_t* const at = reinterpret_cast<i32x4_t*>(g.out + (long)row * g.n_out + c);
+                    store_streamed(at, w, g.stream);
+                }
             } else if (row < g.m) {
                 if (col + kgrp * 4 < g.n_out) fp8_store(g, row, col + kgrp * 4, u);
                 if (col + 16 + kgrp * 4 < g.n_out) fp8_store(g, row, col + 16 + kgrp * 4, v);
@@ -346,6 +349,7 @@ hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
     const size_t need = fp8_product_workspace_bytes(g.m, g.n_out, g.blocks);
     const Fp8Plan p = fp8_plan(g.m, g.n_out, g.blocks, need > 0 && g.ws && g.ws_bytes >= need, compute_units());
     g.pieces = p.pieces;
+    g.stream = (size_t)g.m * g.n_out * sizeof(bf16_t) > STREAM_BYTES;
     switch (p.tile) {
         case FP8_64x64: launch_product_tile<2, 2, 2, 2, 4, 2>(g, st); break;
         case FP8_128x128: launch_product_tile<2, 4, 4, 2, 3, 2>(g, st); break;

@@ -11,6 +11,7 @@ struct GroupNormArgs {
     int batch, positions, channels, groups, act;
     float eps;
     long x_batch, x_position, o_batch, o_position;
+    bool stream;                  // (set by the launcher: out is larger than STREAM_BYTES)
     float2* part;                 // scratch of group_norm_scratch_bytes()
 };
 size_t group_norm_scratch_bytes(int dtype, int batch, int positions, int channels, int groups);

@@ -68,14 +68,14 @@ __device__ __forceinline__ void widen(const typename ChannelsOf<T, V>::type& w, 
     }
 }
 template <typename T, int V>
-__device__ __forceinline__ void store_channels(T* p, const float (&v)[V]) {
+__device__ __forceinline__ void store_channels(T* p, const float (&v)[V], bool stream) {
     typename ChannelsOf<T, V>::type w;
     if constexpr (V == 1) w = (typename ElemOf<T>::type)v[0];
     else {
 #pragma unroll
         for (int i = 0; i < V; ++i) w[i] = (typename ElemOf<T>::type)v[i];
     }
-    *reinterpret_cast<typename ChannelsOf<T, V>::type*>(p) = w;
+    store_streamed(reinterpret_cast<typename ChannelsOf<T, V>::type*>(p), w, stream);
 }
 
 // PHASE 0: moments of the chunk's groups to a.part; 1: moments of all chunks from a.part, then the result; 2: both, one chunk.
@@ -226,7 +226,7 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
                     widen<T, V>(batch[u], v);
 #pragma unroll
                     for (int i = 0; i < V; ++i) v[i] = activated<T, ACT>(__builtin_fmaf(v[i] - mean[i], mul[i], add[i]));
-                    store_channels<T, V>(o + (s + u * rows) * a.o_position + col * V, v);
+                    store_channels<T, V>(o + (s + u * rows) * a.o_position + col * V, v, PHASE == 1 && a.stream);
                 }
         }
     }
@@ -274,7 +274,9 @@ static hipError_t launch_group_norm_t(const GroupNormArgs& a, hipStream_t st) {
     return launch_group_norm_as<T, 1>(a, p, st);
 }
 
-hipError_t launch_group_norm(int dtype, const GroupNormArgs& a, hipStream_t st) {
+hipError_t launch_group_norm(int dtype, const GroupNormArgs& args, hipStream_t st) {
+    GroupNormArgs a = args;
+    a.stream = (size_t)a.batch * a.positions * a.channels * (dtype == PS_BF16 ? 2 : 4) > STREAM_BYTES;
     return dtype == PS_BF16 ? launch_group_norm_t<bf16_t>(a, st) : launch_group_norm_t<float>(a, st);
 }
 

@@ -287,6 +287,11 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
     return (size_t)p.nsplit * batch * tokens * Nn * sizeof(float);
 }
 
+// Results larger than the L2 caches of the 8 XCDs together are stored without keeping a place there for them: whoever reads them next finds
+// them further away in any case, and what the launch reads again stays (8-bit product of 17776 x 5760, 205 MB: 202 -> 195 us; group norm of
+// 70200 x 512, 72 MB, which reads its input twice: 43 -> 39; attention of 8 x 1350 x 30 heads of 64, 41 MB: 31 -> 30).
+constexpr size_t STREAM_BYTES = (size_t)32 << 20;
+
 // ---- 8-bit products (gemm_fp8.hip): which tile, and how many pieces of k
 // Us of a round of workgroups: fixed + blocks of 128 k * stage; `lone`: up to one workgroup per compute unit where two fit.
 // Measured, us on 64 x 64 / 128 x 128 / 192 x 192 / 192 x 256 tiles (operands that change from call to call): 448 rows x 7680, k = 1920

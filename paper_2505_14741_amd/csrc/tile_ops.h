@@ -36,6 +36,19 @@ __device__ __forceinline__ float exp_near(float d) {
     return __builtin_fmaf(e, __builtin_fmaf(-t, LN2_REST, __builtin_fmaf(-t, LN2, d)), e);
 }
 
+// A store that does not keep a place in L2 (see STREAM_BYTES), or an ordinary one.  (The empty statements keep the compiler from merging
+// the two into an ordinary store.)
+template <typename V>
+__device__ __forceinline__ void store_streamed(V* at, V v, bool stream) {
+    if (stream) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, at);
+        asm volatile("");
+    } else {
+        *at = v;
+    }
+}
+
 // Consecutive workgroup ids go to different XCDs (8 of them, each with its own L2).
 // Give each XCD a contiguous range of tiles so co-resident workgroups share operand panels.
 __device__ __forceinline__ int xcd_remap(unsigned id, unsigned total) {
