@@ -215,7 +215,7 @@ PS_API int cross_attn(const void* q, const void* k, const void* v, const int32_t
  * s = scale[c / 128][r].
  *   q      DEVICE e4m3 bytes [rows][kp], kp = cols rounded up to a multiple of 128, filled up with zeros
  *   scale  DEVICE e8m0 bytes [kp / 128][pitch], pitch = rows rounded up to a multiple of 16, filled up with 0
- * fp8_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment, 16 bytes are fastest).  A block's scale is the
+ * fp8_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment).  A block's scale is the
  * least power of two >= 2^-127 under which its largest finite |x| is at most 448; values are rounded once, to nearest even; NaN and
  * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^28 blocks. */
 PS_API int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream);
@@ -234,7 +234,7 @@ PS_API int dit_linear_fp8(const void* a, const void* a_scale, const void* w, con
 /* Group norm over channels-last positions: a group is channels / groups neighbouring channels of a sample at all its positions,
  *   out = act((x - mean) / sqrt(var + eps) * gamma + beta),
  * var the mean squared deviation; act 0 none, 1 tanh-GELU, 2 SiLU.  x, out DEVICE [batch, positions, channels] in `dtype`, channels
- * contiguous, batch and position strides in elements (any alignment, 16 bytes are fastest; x's may be 0; ignored for an extent of 1);
+ * contiguous, batch and position strides in elements (any alignment; x's may be 0; ignored for an extent of 1);
  * out == x is allowed with equal strides, any other overlap is not.  gamma, beta DEVICE fp32 [channels], either may be NULL (1, 0).
  * Statistics in fp32, merged pairwise.  batch and positions may be 0; channels <= 65536.
  * workspace: DEVICE, 256-byte aligned, >= group_norm_workspace_bytes(...) (may be NULL when that is 0). */

@@ -8,8 +8,8 @@
 // Keys that do not count get a score of -infinity, and their V rows (K too in bf16) are zeros in LDS: what lies there is never multiplied.
 //
 // What binds: with few keys reading q and writing o (17550 x 226 keys, 30 heads of 64: 137 MB, 28 us at a device copy's rate) and the
-// vector instructions per score, about as long, which do not all run beside the matrix instructions; that case takes 50 us (2.7 TB/s,
-// 600 TFLOP/s).  With few rows, reading the keys: 32 tokens x 17776 keys (55 MB) 23 us and 6 to add the pieces.
+// vector instructions per score, about as long, which do not all run beside the matrix instructions; that case takes 48 us (2.9 TB/s,
+// 640 TFLOP/s).  With few rows, reading the keys: 32 tokens x 17776 keys (55 MB) 22 us and 6 to add the pieces.
 #include "cross_attention.h"
 #include "lane_sums.h"
 #include "plan.h"
@@ -323,7 +323,7 @@ cross_bf16_kernel(CrossArgs a) {
     }
 }
 
-// Short key sequences and many rows (a prompt's states under a video's tokens; 17550 x 226 keys 70 us on cross_bf16_kernel, 50 here): all keys and values of a (sample, key/value head) lie in LDS, and
+// Short key sequences and many rows (a prompt's states under a video's tokens; 17550 x 226 keys 70 us on cross_bf16_kernel, 48 here): all keys and values of a (sample, key/value head) lie in LDS, and
 // the 8 waves of a workgroup (four per SIMD of two workgroups) take QT * 16 rows each in turn, without a barrier.  n workgroups share a head.  A row's values depend on
 // the rows of its own chunk only, whatever n is.
 template <int HD, int QT>

@@ -99,7 +99,7 @@ hipError_t launch_fp8_quantize(int dtype, const void* x, void* q, void* scale, i
 // bits below 2^-13 of the power of two of the largest, and adds exactly enough from there on: 1.3e-5 of the result's norm for
 // Gaussian operands, whatever the 8-bit instruction.  The output is bf16.)  Rows of both operands are contiguous in k;
 // stages of one block (128 bytes of a row) go straight into an LDS ring, with the tile's scale bytes behind them.
-// 17776 x 5760, K = 1920: 199 us, 1.98 PFLOP/s; 4516 x 1920, K = 7680: 61 us, 2.18 (a library's 8-bit product of 8192^3 reaches 2.7); the tiles
+// 17776 x 5760, K = 1920: 194 us, 2.03 PFLOP/s; 4516 x 1920, K = 7680: 61 us, 2.18 (a library's 8-bit product of 8192^3 reaches 2.7); the tiles
 // and what each measured are in plan.h.
 // Slot p of LDS row r holds 16-byte chunk p ^ ((r >> 1) & 7), so that the 16 rows of a fragment read fall into different bank
 // groups.  A lane's 32 bytes of a fragment are chunks l / 16 and 4 + l / 16 of its row, of both operands alike (the instruction's

@@ -1,8 +1,8 @@
 // Group norm over channels-last positions with an activation: a group is channels / groups neighbouring channels of one sample over all
 // positions; y = (x - mean) / sqrt(var + eps) * gamma + beta, then none, tanh-GELU or SiLU.
 //
-// Reading x twice and writing it once is what binds.  70200 positions of 512 channels, 32 groups, SiLU, bf16 (72 MB): 15 us for the
-// moments (4.9 TB/s) and 26 for the result (5.5 TB/s, beyond a device copy's rate; the second read comes from the last-level cache).  2 x 345
+// Reading x twice and writing it once is what binds.  70200 positions of 512 channels, 32 groups, SiLU, bf16 (72 MB): 14 us for the
+// moments (5.2 TB/s) and 25 for the result (5.8 TB/s, beyond a device copy's rate; the second read comes from the last-level cache).  2 x 345
 // positions of 320 channels, fp32, in one launch 9 us, all of it latency.  A workgroup takes a slice of whole groups (about 64 channels, so that a position is
 // a whole cache line or two) over a chunk of positions.  Means and squared deviations are merged pairwise, (n, mean, M2) with
 // (n', mean', M2'), from single values on: exact where the mean is far larger than the deviations, whatever the first values are.
@@ -56,9 +56,20 @@ template <typename T, int ACT> __device__ __forceinline__ float activated(float 
     else return x;
 }
 
+// V channels, and the same in memory: at any element's address (element by element 17550 x 320 bf16 one element into rows of 321
+// took 30 us, so 19; aligned 18)
 template <typename T> struct ElemOf { typedef typename std::conditional<sizeof(T) == 4, float, __bf16>::type type; };
-template <typename T, int V> struct ChannelsOf { typedef __attribute__((ext_vector_type(V))) typename ElemOf<T>::type type; };
-template <typename T> struct ChannelsOf<T, 1> { typedef typename ElemOf<T>::type type; };
+template <typename T, int V> struct ChannelsOf;
+template <int V> struct ChannelsOf<float, V> {
+    typedef __attribute__((ext_vector_type(V))) float type;
+    typedef type mem __attribute__((aligned(4)));
+};
+template <int V> struct ChannelsOf<bf16_t, V> {
+    typedef __attribute__((ext_vector_type(V))) __bf16 type;
+    typedef type mem __attribute__((aligned(2)));
+};
+template <> struct ChannelsOf<float, 1> { typedef float type, mem; };
+template <> struct ChannelsOf<bf16_t, 1> { typedef __bf16 type, mem; };
 template <typename T, int V>
 __device__ __forceinline__ void widen(const typename ChannelsOf<T, V>::type& w, float (&v)[V]) {
     if constexpr (V == 1) v[0] = (float)w;
@@ -75,7 +86,7 @@ __device__ __forceinline__ void store_channels(T* p, const float (&v)[V], bool s
 #pragma unroll
         for (int i = 0; i < V; ++i) w[i] = (typename ElemOf<T>::type)v[i];
     }
-    store_streamed(reinterpret_cast<typename ChannelsOf<T, V>::type*>(p), w, stream);
+    store_streamed(reinterpret_cast<typename ChannelsOf<T, V>::mem*>(p), (typename ChannelsOf<T, V>::mem)w, stream);
 }
 
 // PHASE 0: moments of the chunk's groups to a.part; 1: moments of all chunks from a.part, then the result; 2: both, one chunk.
@@ -86,6 +97,7 @@ template <typename T, int V, int PHASE, int ACT, int U, int NT>      // U: posit
 __global__ void __launch_bounds__(NT)
 group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
     typedef typename ChannelsOf<T, V>::type vec_t;
+    typedef typename ChannelsOf<T, V>::mem mem_t;
     __shared__ float2 sums[PHASE == 1 ? 1 : NT * V + 2 * NT];     // mean, M2: rows of lanes * V channels and a fill (see p.fill)
     __shared__ float2 stats[GROUP_NORM_SLICE_GROUPS];    // mean, 1 / sqrt(var + eps)
     const int chunk = blockIdx.x, slice = blockIdx.y, b = blockIdx.z;
@@ -105,21 +117,22 @@ group_norm_kernel(GroupNormArgs a, GroupNormPlan p) {
         const T* at = q + s * a.x_position;
         if (s + (U - 1) * rows < s1) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const vec_t*>(at + u * step);
+            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const mem_t*>(at + u * step);
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const vec_t*>(q + min(s + u * rows, s1 - 1) * a.x_position);
+            for (int u = 0; u < U; ++u) batch[u] = *reinterpret_cast<const mem_t*>(q + min(s + u * rows, s1 - 1) * a.x_position);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     // what multiplies and follows a column of V channels, without the statistics
     typedef typename ChannelsOf<float, V>::type affine_t;
+    typedef typename ChannelsOf<float, V>::mem affine_mem_t;
     affine_t gamma, beta;
     auto fetch_affine = [&](int col) {
         gamma = affine_t{} + 1.f;
         beta = affine_t{};
-        if (a.gamma) gamma = *reinterpret_cast<const affine_t*>(a.gamma + c0 + col * V);
-        if (a.beta) beta = *reinterpret_cast<const affine_t*>(a.beta + c0 + col * V);
+        if (a.gamma) gamma = *reinterpret_cast<const affine_mem_t*>(a.gamma + c0 + col * V);
+        if (a.beta) beta = *reinterpret_cast<const affine_mem_t*>(a.beta + c0 + col * V);
     };
 
     Moments t{0.f, 0.f, 0.f};                            // of group tg
@@ -262,15 +275,10 @@ static hipError_t launch_group_norm_as(const GroupNormArgs& a, GroupNormPlan p, 
 template <typename T>
 static hipError_t launch_group_norm_t(const GroupNormArgs& a, hipStream_t st) {
     const GroupNormPlan p = group_norm_plan(a.positions, a.channels, a.groups, sizeof(T));
-    // the widest load that the slices' widths, the strides and the addresses allow (gamma and beta are read 4 channels at a time)
-    long bytes = (long)p.slice_groups * (a.channels / a.groups) * sizeof(T);
-    bytes |= (long)((uintptr_t)a.x | (uintptr_t)a.out) | (long)a.channels * sizeof(T);
-    if (a.positions > 1) bytes |= (a.x_position | a.o_position) * (long)sizeof(T);
-    if (a.batch > 1) bytes |= (a.x_batch | a.o_batch) * (long)sizeof(T);
-    const bool affine = (((uintptr_t)a.gamma | (uintptr_t)a.beta) & 15) == 0;
-    if (!affine) return launch_group_norm_as<T, 1>(a, p, st);
-    if (bytes % 16 == 0) return launch_group_norm_as<T, 16 / sizeof(T)>(a, p, st);
-    if (bytes % 8 == 0 && sizeof(T) == 2) return launch_group_norm_as<T, 4>(a, p, st);
+    // the widest load that divides a slice, the last one too
+    const int width = p.slice_groups * p.cpg | a.channels;
+    if (sizeof(T) == 2 && width % 8 == 0) return launch_group_norm_as<T, sizeof(T) == 2 ? 8 : 4>(a, p, st);
+    if (width % 4 == 0) return launch_group_norm_as<T, 4>(a, p, st);
     return launch_group_norm_as<T, 1>(a, p, st);
 }
 

@@ -366,7 +366,7 @@ struct GroupNormPlan {
 constexpr GroupNormPlan group_norm_plan(int positions, int channels, int groups, int elem_bytes) {
     const int cpg = channels / groups;
     const long bytes = (long)cpg * elem_bytes;
-    // a cache line of a position at least, and whole 16-byte loads if a few groups more give them
+    // a cache line of a position at least, and channels that 16-byte loads divide if a few groups more give them
     long k = (127 + bytes) / bytes;
     for (int more = 0; more < 8; ++more)
         if ((k + more) * bytes % 16 == 0) { k += more; break; }
