@@ -9,7 +9,7 @@
 //
 // What binds: with few keys reading q and writing o (17550 x 226 keys, 30 heads of 64: 137 MB, 28 us at a device copy's rate) and the
 // vector instructions per score, about as long, which do not all run beside the matrix instructions; that case takes 48 us (2.9 TB/s,
-// 640 TFLOP/s).  With few rows, reading the keys: 32 tokens x 17776 keys (55 MB) 22 us and 6 to add the pieces.
+// 640 TFLOP/s).  With few rows, reading the keys: 32 tokens x 17776 keys (55 MB) 23 us and 6 to add the pieces.
 #include "cross_attention.h"
 #include "lane_sums.h"
 #include "plan.h"
@@ -56,7 +56,10 @@ __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, lo
 // The reference of a row's exponents moves only where some score of a tile exceeds it by 8 in powers of two (probabilities
 // stay below 2^8, sums far from overflow): a tile then costs no rescaling and no maximum over lanes.
 constexpr float CROSS_AHEAD = 8.0f;
-constexpr float CROSS_SUM_MAX = 0x1p+100f;
+constexpr float CROSS_SUM_MAX = 0x1p+32f;                // (values up to 2^95 stay finite)
+// Exponents are c s - c m in one instruction; c m is rounded, by up to 2^-24 of itself, which all keys of a row share but two references
+// do not.  Beyond 2^10, where that is 2^-14, a row takes (s - m) c instead.
+constexpr float CROSS_FAR = 0x1p+10f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 __device__ __forceinline__ s16x4_t read_tr16(const bf16_t* p) {
@@ -166,18 +169,33 @@ __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_
         }
     }
 }
-// Probabilities, rounded to bf16 for the second product.
-template <int QT>
-__device__ __forceinline__ void cross_weights(const f32x4_t (&sc)[QT][4], const float (&m)[QT], float c, bf16x8_t (&pf)[QT][2]) {
+// Probabilities, rounded to bf16 for the second product (the scores are used up).  NEAR: no reference is beyond CROSS_FAR, or the caller looks for it afterwards.
+template <int QT, bool NEAR>
+__device__ __forceinline__ void cross_weights(f32x4_t (&sc)[QT][4], const float (&m)[QT], float c, bf16x8_t (&pf)[QT][2]) {
+    float mc[QT];
+    bool far = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        const float mc = m[t] == -INFINITY ? 0.f : m[t] * c;
+        mc[t] = m[t] == -INFINITY ? 0.f : m[t] * c;
+        far = far || fabsf(mc[t]) > CROSS_FAR;
+    }
+    if (!NEAR && __any(far)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const bool mine = fabsf(mc[t]) > CROSS_FAR;
+            const float ref = mine ? m[t] : 0.f;
+            mc[t] = mine ? 0.f : mc[t];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) sc[t][g] -= ref;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc));
-    }
+                pf[t][s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * s + e / 4][e % 4], c, -mc[t]));
 }
 // acc += V^T P^T, l += 1 P^T: the sums of the probabilities as they were rounded (one key alone has weight 1 exactly), for which the matrix
 // pipes have time and the vector ones have not.  Every lane has its row's whole sum.
@@ -303,7 +321,7 @@ cross_bf16_kernel(CrossArgs a) {
         }
         cross_softmax<QT, NB, false>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
-        cross_weights<QT>(sc, m, c, pf);
+        cross_weights<QT, false>(sc, m, c, pf);
         cross_values<HD, QT>(vf, pf, acc, l);
     }
 #pragma unroll
@@ -315,7 +333,7 @@ cross_bf16_kernel(CrossArgs a) {
             float* p = a.part + ((((long)it.b * a.kv_heads + it.g) * a.nsplit + it.piece) * a.rows + row) * (HD + 4);
 #pragma unroll
             for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[t][d];
-            if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m[t] * c};
+            if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m[t]};
         } else {
             bf16_t* p = (bf16_t*)a.o + it.b * a.s.o_batch + cross_row(a, it.g, min(row, a.rows - 1), a.s.o_tok, a.s.o_head);
             cross_store<NB>(p, acc[t], sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), kgrp, row < a.rows, a.stream);
@@ -323,9 +341,9 @@ cross_bf16_kernel(CrossArgs a) {
     }
 }
 
-// Short key sequences and many rows (a prompt's states under a video's tokens; 17550 x 226 keys 70 us on cross_bf16_kernel, 48 here): all keys and values of a (sample, key/value head) lie in LDS, and
-// the 8 waves of a workgroup (four per SIMD of two workgroups) take QT * 16 rows each in turn, without a barrier.  n workgroups share a head.  A row's values depend on
-// the rows of its own chunk only, whatever n is.
+// Short key sequences and many rows (a prompt's states under a video's tokens; 17550 x 226 keys 70 us on cross_bf16_kernel, 48 here): all keys and
+// values of a (sample, key/value head) lie in LDS, and the 8 waves of a workgroup (four per SIMD of two workgroups) take QT * 16 rows each in
+// turn, without a barrier.  n workgroups share a head.  A row's values depend on the rows of its own chunk only, whatever n is.
 template <int HD, int QT>
 __global__ void __launch_bounds__(CROSS_RESIDENT_WAVES * 64, CROSS_RESIDENT_WAVES / 2)
 cross_resident_kernel(CrossArgs a, int n) {
@@ -420,7 +438,7 @@ cross_resident_kernel(CrossArgs a, int n) {
         }
         if constexpr (FIRST || TRACKED) cross_softmax<QT, NB, FIRST>(sc, acc, m, l, c, ahead);
         bf16x8_t pf[QT][2];
-        cross_weights<QT>(sc, m, c, pf);
+        cross_weights<QT, !TRACKED>(sc, m, c, pf);
         CrossV<HD> vf;
         cross_read_v<HD, LDV>(v0 + j * (KT * LDV), vf);
         cross_values<HD, QT, FIRST>(vf, pf, acc, l);
@@ -429,14 +447,15 @@ cross_resident_kernel(CrossArgs a, int n) {
     const std::false_type no;
     for (; chunk < chunks; chunk += stride) {
         // Relative to the first tile's maximum, which is one of the row's scores, sums are at least 1; what they are at most is looked at
-        // behind the last tile, instead of every tile's maxima: rows whose later scores are so much larger are computed again.
+        // behind the last tile, instead of every tile's maxima: rows whose later scores are so much larger, or whose reference is
+        // beyond CROSS_FAR, are computed again.
         bool done = false;
         if (first_counts) {
             tile(0, yes, no);
             for (int j = 1; j < tiles; ++j) tile(j, no, no);
             bool fits = true;
 #pragma unroll
-            for (int t = 0; t < QT; ++t) fits = fits && l[t][0] < CROSS_SUM_MAX;
+            for (int t = 0; t < QT; ++t) fits = fits && l[t][0] < CROSS_SUM_MAX && !(fabsf(m[t] * c) > CROSS_FAR);
             done = __all(fits);
         }
         if (!done) {
@@ -464,14 +483,15 @@ cross_resident_kernel(CrossArgs a, int n) {
     }
 }
 
-// Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = 2^(ref_i - max); a piece without a key that counts has the reference
-// -infinity.  (fp32: references are natural, exponentials as exact as expf.)  A wave takes a row: HD / 4 lanes hold 4 adjacent values each, and
-// the wave's 256 / HD teams of them take a piece each in turn.
+// Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(scale * (ref_i - max)) for bf16, whose references are scores, and
+// exp(ref_i - max) for fp32, whose are scaled; a piece without a key that counts has the reference -infinity.  A wave takes a row: HD / 4 lanes
+// hold 4 adjacent values each, and the wave's 256 / HD teams of them take a piece each in turn.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256)
 cross_join_kernel(CrossArgs a, long lines) {
     constexpr int W = HD / 4, TEAMS = 64 / W;
     const int lane = threadIdx.x & 63, d = lane % W * 4, team = lane / W;
+    const float c = a.scale * CROSS_LOG2E;
     for (long line = (long)blockIdx.x * 4 + (threadIdx.x >> 6); line < lines; line += (long)gridDim.x * 4) {      // (whole waves)
         const long bg = line / a.rows;
         const int row = (int)(line - bg * a.rows), b = (int)(bg / a.kv_heads), g = (int)(bg - (long)b * a.kv_heads);
@@ -488,7 +508,7 @@ cross_join_kernel(CrossArgs a, long lines) {
         for (int i = team; i < a.nsplit; i += TEAMS) {
             const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-            const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(s[1] - ref) : expf(s[1] - ref);
+            const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f((s[1] - ref) * c) : expf(s[1] - ref);
             acc += v * w;
             l = __builtin_fmaf(s[0], w, l);
         }

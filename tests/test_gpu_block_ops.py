@@ -156,6 +156,34 @@ def test_cross_attention_large_scores(dtype, nq):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq,nk", [(5, 200), (40, 2600), (300, 200)])
+def test_cross_attention_of_huge_scores(dtype, nq, nk):
+    """Scores of 2^10 to 2^100 that are exact, so that the weights are: one key far ahead, wherever it stands, or two that share the first place;
+    and values of 2^60 under scores that grow by 40."""
+    g = gen(24)
+    v = randn(g, 1, nk, 1, 64).to(dtype)
+    for power in (10, 14, 24, 40, 100):
+        for best in ([0], [nk - 1], [70, nk - 3], [1, 2]):
+            q, k = torch.zeros(1, nq, 1, 64, device=DEV), torch.zeros(1, nk, 1, 64, device=DEV)
+            q[..., 0] = 2.0 ** (power // 2)
+            k[0, :, 0, 0] = 2.0 ** (power - power // 2) * (1.0 - 2.0 ** -2 * torch.rand(nk, generator=g, device=DEV).round().add(1.0))
+            k[0, best, 0, 0] = 2.0 ** (power - power // 2)
+            for sign in (1.0, -1.0):                             # (below zero: the best are the smallest in size)
+                kk = k.clone()
+                if sign < 0:
+                    kk[0, :, 0, 0] = -2.0 ** (power - power // 2) * 2
+                    kk[0, best, 0, 0] = -2.0 ** (power - power // 2)
+                out = B.cross_attn(q.to(dtype), kk.to(dtype), v, 1.0).double()
+                want = v.double()[:, best].mean(1, keepdim=True).expand_as(out)
+                # (at 2^10 the others are 2^8 behind: exp(-256) of the sum)
+                assert bool(((out - want).abs() <= 2 * U[dtype] * v.double()[:, best].abs().mean(1, keepdim=True) + 1e-6).all()), (power, best, sign)
+    q, k = torch.zeros(1, nq, 1, 64, device=DEV), torch.zeros(1, nk, 1, 64, device=DEV)
+    q[..., 0], k[0, 64:, 0, 0] = 1.0, 40.0
+    big = (v.float() * 2.0 ** 60).to(dtype)
+    check_cross(q.to(dtype), k.to(dtype), big, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_cross_attention_strides(dtype):
     """Halves of one projection, head-major tensors, operands that samples and heads share, an output inside a wider one whose other
     values stay."""
