@@ -55,7 +55,7 @@ __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, lo
 // ------------------------------------------------------------------------------------ bf16
 // The reference of a row's exponents moves only where some score of a tile exceeds it by 8 in powers of two (probabilities
 // stay below 2^8, sums far from overflow): a tile then costs no rescaling and no maximum over lanes.
-constexpr float CROSS_AHEAD = 8.0f;
+constexpr float CROSS_AHEAD = 8.0f;                      // (finite in units of the scores for every scale: -infinity plus it stays -infinity)
 constexpr float CROSS_SUM_MAX = 0x1p+32f;                // (values up to 2^95 stay finite)
 // Exponents are c s - c m in one instruction; c m is rounded, by up to 2^-24 of itself, which all keys of a row share but two references
 // do not.  Beyond 2^10, where that is 2^-14, a row takes (s - m) c instead.
@@ -231,7 +231,7 @@ cross_bf16_kernel(CrossArgs a) {
     int j0 = 0, j1 = tiles;
     if (a.nsplit > 1) { j0 = (int)((long)tiles * it.piece / a.nsplit); j1 = (int)((long)tiles * (it.piece + 1) / a.nsplit); }
     const int r0 = it.block * BQ + wave * QT * 16 + l16;
-    const float c = a.scale * CROSS_LOG2E, ahead = CROSS_AHEAD / c;
+    const float c = a.scale * CROSS_LOG2E, ahead = fminf(CROSS_AHEAD / c, 0x1p+127f);
 
     typedef __attribute__((ext_vector_type(4))) int chunk_t;
     chunk_t kn[LOADS], vn[LOADS];                        // the next tile; rows past the end are zeros
@@ -360,7 +360,7 @@ cross_resident_kernel(CrossArgs a, int n) {
     bf16_t* ob = (bf16_t*)a.o + b * a.s.o_batch;
     const int keys = cross_keys(a, b), tiles = (keys + KT - 1) / KT;
     const int chunks = (a.rows + BQ - 1) / BQ, stride = n * CROSS_RESIDENT_WAVES;
-    const float c = a.scale * CROSS_LOG2E, ahead = CROSS_AHEAD / c;
+    const float c = a.scale * CROSS_LOG2E, ahead = fminf(CROSS_AHEAD / c, 0x1p+127f);
 
     // offset of row t * 16 + l16 of a chunk: the lane's share of it is the same for all chunks that are whole, if heads share no keys
     const long q_lane = l16 * a.s.q_tok + kgrp * (HD == 16 ? 4 : 8), o_lane = l16 * a.s.o_tok;

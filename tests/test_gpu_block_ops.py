@@ -184,6 +184,13 @@ def test_cross_attention_of_huge_scores(dtype, nq, nk):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq,nk", [(5, 200), (40, 2600), (300, 200)])
+def test_cross_attention_of_a_tiny_scale(dtype, nq, nk):
+    g = gen(25)
+    check_cross(*(randn(g, 1, n, 1, 64).to(dtype) for n in (nq, nk, nk)), 1e-38)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_cross_attention_strides(dtype):
     """Halves of one projection, head-major tensors, operands that samples and heads share, an output inside a wider one whose other
     values stay."""
