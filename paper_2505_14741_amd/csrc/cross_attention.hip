@@ -409,12 +409,14 @@ cross_resident_kernel(CrossArgs a, int n) {
     }
     __syncthreads();
     unsigned whole = 0;                                  // tiles all of whose keys count
-    bool first_counts = false;                           // some key of the first tile does
+    bool first_counts = false, any_counts = false;       // some key of the first tile does, some key at all
     for (int j = 0; j < tiles; ++j) {
         const unsigned long long in = __ballot(Bs[j * KT + lane] == 0.f);
         whole |= (in == ~0ull ? 1u : 0u) << j;
         if (j == 0) first_counts = in != 0;
+        any_counts = any_counts || in != 0;
     }
+    const int tracked_tiles = any_counts ? tiles : 0;    // (zeros without a product: the query need not be finite)
 
     const bf16_t *const k0 = Ks + l16 * LDK + kgrp * (HD == 16 ? 4 : 8), *const v0 = Vs + (4 * kgrp + (l16 >> 2)) * LDV + (l16 & 3) * 4;
     f32x4_t acc[QT][NB], l[QT];
@@ -466,7 +468,7 @@ cross_resident_kernel(CrossArgs a, int n) {
 #pragma unroll
                 for (int d = 0; d < NB; ++d) acc[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
-            for (int j = 0; j < tiles; ++j) tile(j, no, yes);
+            for (int j = 0; j < tracked_tiles; ++j) tile(j, no, yes);
         }
         if (chunk + stride < chunks) fetch(chunk + stride);
         // the next queries' loads are waited for here: behind the stores, whose number the compiler cannot know, it would wait for these too

@@ -1,0 +1,56 @@
+"""Operators of a conditioned predictor block at the ends of their ranges: what is not finite, values and scores as large as their types
+hold, addresses on no border, the largest grids."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_14741_amd import binding as B
+from test_gpu_block_ops import DEV, NAN, U, check_cross, cross_ref, gen, randn
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------- cross attention
+# (few rows; rows whose keys are divided; all keys in LDS in bf16 up to heads of 64)
+SIZES = [(3, 100), (40, 2600), (300, 226)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("nq,nk", SIZES)
+def test_rows_without_a_key_are_zero_whatever_their_query_holds(dtype, d, nq, nk):
+    """An empty place of a padded batch, its queries never written: a mask of zeros, a length of zero.  Beside it a sample with the same
+    queries and all keys."""
+    print(f"cross_attn empty rows {dtype} d={d} q={nq} k={nk}", flush=True)
+    g = gen(nq + nk + d)
+    q, k, v = randn(g, 3, nq, 2, d).to(dtype), randn(g, 3, nk, 2, d).to(dtype), randn(g, 3, nk, 2, d).to(dtype)
+    junk = torch.tensor([NAN, float("inf"), -float("inf"), 1.0], device=DEV).to(dtype)
+    q[:2] = junk[torch.randint(0, 4, (2, nq, 2, d), generator=g, device=DEV)]
+    mask = torch.ones(3, nk, dtype=torch.bool, device=DEV)
+    mask[0] = False
+    lens = torch.tensor([nk, 0, nk], dtype=torch.int32, device=DEV)
+    out = B.cross_attn(q, k, v, 1.0 / math.sqrt(d), kv_lens=lens, key_mask=mask)
+    assert bool((out[:2] == 0).all())
+    assert torch.equal(out[2:], B.cross_attn(q[2:], k[2:], v[2:], 1.0 / math.sqrt(d), kv_lens=lens[2:], key_mask=mask[2:]))
+    check_cross(q[2:], k[2:], v[2:], 1.0 / math.sqrt(d))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq,nk", SIZES)
+def test_a_query_that_is_not_finite_spoils_its_own_row_only(dtype, nq, nk):
+    g = gen(nq + nk)
+    q, k, v = randn(g, 1, nq, 2, 64).to(dtype), randn(g, 1, nk, 2, 64).to(dtype), randn(g, 1, nk, 2, 64).to(dtype)
+    whole = torch.ones(1, nk, dtype=torch.bool, device=DEV)
+    ref, tol = cross_ref(q, k, v, 0.125, whole)
+    for mask in (None, torch.arange(nk, device=DEV)[None] >= 70):            # (nothing of the first 64 keys)
+        if mask is not None:
+            ref, tol = cross_ref(q, k, v, 0.125, mask)
+        for bad in (NAN, float("inf")):
+            p = q.clone()
+            p[0, 1, 0, 5] = bad
+            out = B.cross_attn(p, k, v, 0.125, key_mask=mask)
+            good = torch.ones(1, nq, 2, 64, dtype=torch.bool, device=DEV)
+            good[0, 1, 0] = False
+            assert bool(((out.double() - ref).abs() <= tol * 1.001)[good].all())
+            assert bool(torch.isnan(out[0, 1, 0]).all())
