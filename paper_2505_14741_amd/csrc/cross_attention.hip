@@ -56,7 +56,10 @@ __device__ __forceinline__ long cross_row(const CrossArgs& a, int g, int row, lo
 // The reference of a row's exponents moves only where some score of a tile exceeds it by 8 in powers of two (probabilities
 // stay below 2^8, sums far from overflow): a tile then costs no rescaling and no maximum over lanes.
 constexpr float CROSS_AHEAD = 8.0f;                      // (finite in units of the scores for every scale: -infinity plus it stays -infinity)
-constexpr float CROSS_SUM_MAX = 0x1p+32f;                // (values up to 2^95 stay finite)
+constexpr float CROSS_SUM_MAX = 0x1p+32f;
+// Sums up to here are no larger than 2^8 for each of the 65 keys or more of a row with a second tile: values overflow under them only where
+// they do with a reference that moves, too.
+constexpr float CROSS_SUM_NEAR = 0x1p+14f;
 // Exponents are c s - c m in one instruction; c m is rounded, by up to 2^-24 of itself, which all keys of a row share but two references
 // do not.  Beyond 2^10, where that is 2^-14, a row takes (s - m) c instead.
 constexpr float CROSS_FAR = 0x1p+10f;
@@ -449,15 +452,29 @@ cross_resident_kernel(CrossArgs a, int n) {
     const std::false_type no;
     for (; chunk < chunks; chunk += stride) {
         // Relative to the first tile's maximum, which is one of the row's scores, sums are at least 1; what they are at most is looked at
-        // behind the last tile, instead of every tile's maxima: rows whose later scores are so much larger, or whose reference is
-        // beyond CROSS_FAR, are computed again.
+        // behind the last tile, instead of every tile's maxima: rows whose later scores are so much larger (or somewhat larger, and the
+        // values so large that their sums are not finite), or whose reference is beyond CROSS_FAR, are computed again.
         bool done = false;
         if (first_counts) {
             tile(0, yes, no);
             for (int j = 1; j < tiles; ++j) tile(j, no, no);
             bool fits = true;
+            float sums = 0.f;                            // of the lane's rows: at least as large as each
 #pragma unroll
-            for (int t = 0; t < QT; ++t) fits = fits && l[t][0] < CROSS_SUM_MAX && !(fabsf(m[t] * c) > CROSS_FAR);
+            for (int t = 0; t < QT; ++t) {
+                sums += l[t][0];
+                fits = fits && !(fabsf(m[t] * c) > CROSS_FAR);
+            }
+            if (!__all(sums < CROSS_SUM_NEAR)) {
+                float zero = 0.f;                        // (NaN if a value is not finite)
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int d = 0; d < NB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(acc[t][d][i], 0.f, zero);
+                fits = fits && sums < CROSS_SUM_MAX && zero == 0.f;
+            }
             done = __all(fits);
         }
         if (!done) {

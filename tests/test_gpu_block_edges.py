@@ -54,3 +54,19 @@ def test_a_query_that_is_not_finite_spoils_its_own_row_only(dtype, nq, nk):
             good[0, 1, 0] = False
             assert bool(((out.double() - ref).abs() <= tol * 1.001)[good].all())
             assert bool(torch.isnan(out[0, 1, 0]).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [16, 64])
+@pytest.mark.parametrize("growth", [0.0, 11.0, 15.0, 30.0])
+@pytest.mark.parametrize("nq,nk", [(5, 200), (40, 2600), (300, 200), (300, 640)])
+def test_values_as_large_as_their_sums_allow(dtype, d, growth, nq, nk):
+    """|v| * keys * 2^8 below 2^128, under scores that grow by `growth` behind the first 64 keys (by 15: e^15 = 2^21.6 times 2^110)."""
+    print(f"cross_attn large values {dtype} d={d} q={nq} k={nk} growth={growth}", flush=True)
+    g = gen(26)
+    q, k = randn(g, 1, nq, 1, d) * 0.25, randn(g, 1, nk, 1, d) * 0.25
+    q[..., 0], k[0, :64, 0, 0], k[0, 64:, 0, 0] = 1.0, 0.0, growth
+    v = randn(g, 1, nk, 1, d)
+    v *= 2.0 ** (118 - math.ceil(math.log2(nk))) / v.abs().max()
+    assert float(v.abs().max()) * nk * 256 < 2.0 ** 128
+    assert bool(torch.isfinite(check_cross(q.to(dtype), k.to(dtype), v.to(dtype), 1.0)).all())
