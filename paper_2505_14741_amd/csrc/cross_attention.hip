@@ -144,6 +144,13 @@ __device__ __forceinline__ void cross_read_v(const bf16_t* vt, CrossV<HD>& v) {
         }
 }
 
+// 2^(c (a - b)) of two scores, b finite and a at most b, or -infinity (0).  Halves: the scores' difference itself may be beyond fp32 where
+// c times it is not (c times a finite score is finite).
+__device__ __forceinline__ float exp2_between(float a, float b, float c) {
+    const float half = (0.5f * a - 0.5f * b) * c;
+    return __builtin_amdgcn_exp2f(half + half);
+}
+
 // FIRST (a row's first tile, nothing has been summed): the reference is the maximum.  Else references move (in powers of two: times c)
 // where a score of the tile is ahead of one, and what has been summed with them.
 template <int QT, int NB, bool FIRST>
@@ -164,7 +171,7 @@ __device__ __forceinline__ void cross_softmax(const f32x4_t (&sc)[QT][4], f32x4_
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const float mn = fmaxf(m[t], max_xor32(max_xor16(top[t])));
-            const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f((m[t] - mn) * c);      // exp2(-inf) = 0 on the first tile
+            const float alpha = mn == m[t] ? 1.f : exp2_between(m[t], mn, c);        // 0 on the first tile
             m[t] = mn;
             l[t][0] *= alpha;                            // (the only one that is looked at)
 #pragma unroll
@@ -527,7 +534,7 @@ cross_join_kernel(CrossArgs a, long lines) {
         for (int i = team; i < a.nsplit; i += TEAMS) {
             const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-            const float w = sizeof(T) == 2 ? __builtin_amdgcn_exp2f((s[1] - ref) * c) : expf(s[1] - ref);
+            const float w = sizeof(T) == 2 ? exp2_between(s[1], ref, c) : expf(s[1] - ref);
             acc += v * w;
             l = __builtin_fmaf(s[0], w, l);
         }

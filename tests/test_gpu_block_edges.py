@@ -70,3 +70,22 @@ def test_values_as_large_as_their_sums_allow(dtype, d, growth, nq, nk):
     v *= 2.0 ** (118 - math.ceil(math.log2(nk))) / v.abs().max()
     assert float(v.abs().max()) * nk * 256 < 2.0 ** 128
     assert bool(torch.isfinite(check_cross(q.to(dtype), k.to(dtype), v.to(dtype), 1.0)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("first", [1, 64, 70])
+@pytest.mark.parametrize("nq,nk", [(5, 200), (40, 2600), (300, 200), (300, 640)])
+def test_scores_whose_difference_is_beyond_their_type(dtype, first, nq, nk):
+    """Scores of -1.75 * 2^127 and then 1.75 * 2^127 under a scale of 1e-38: 6 apart in the exponent, so that the first keys, whose values
+    alone are not zero, count for exp(-6) each."""
+    g = gen(27)
+    q, k = torch.zeros(1, nq, 1, 64, device=DEV), torch.zeros(1, nk, 1, 64, device=DEV)
+    q[..., 0], k[0, :first, 0, 0], k[0, first:, 0, 0] = 2.0 ** 63, -1.75 * 2.0 ** 64, 1.75 * 2.0 ** 64
+    v = randn(g, 1, nk, 1, 64) * 100.0
+    v[:, first:] = 0.0
+    for flip in (False, True):
+        kk, vv = (k.flip(1), v.flip(1)) if flip else (k, v)
+        mask = torch.ones(1, nk, dtype=torch.bool, device=DEV)
+        check_cross(q.to(dtype), kk.to(dtype).contiguous(), vv.to(dtype).contiguous(), 1e-38)
+        mask[0, 1 if first == 1 else 0] = False                  # (other paths where a key is out)
+        check_cross(q.to(dtype), kk.to(dtype).contiguous(), vv.to(dtype).contiguous(), 1e-38, key_mask=mask)
