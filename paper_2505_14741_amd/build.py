@@ -14,7 +14,9 @@ SOURCES = ["api.hip", "elementwise.hip", "gemm.hip", "gemm_mfma.hip", "gemm_few.
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-         "-Wno-unused-command-line-argument"]
+         "-Wno-unused-command-line-argument",
+         # an access wider than its address allows is an error: the hardware may take it, the compiler need not
+         "-Werror=align-mismatch"]
 
 
 # per-file additions: the attention loop is a long straight-line mix of matrix, vector and LDS instructions at the

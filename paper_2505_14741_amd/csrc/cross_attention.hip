@@ -86,8 +86,7 @@ __device__ __forceinline__ void cross_store(bf16_t* row, const f32x4_t (&acc)[NB
             const auto lo = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false), hi = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
             // even kgrp: block d, values 4 kgrp .. + 7; odd: block d + 1, values 4 (kgrp - 1) .. + 7
             if (in)
-                store_streamed(reinterpret_cast<i32x4_t*>(row + (d + (kgrp & 1)) * 16 + (kgrp & 2) * 4),
-                               i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]}, stream);
+                store_streamed<16>(row + (d + (kgrp & 1)) * 16 + (kgrp & 2) * 4, i32x4_t{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]}, stream);
         }
     }
 }

@@ -304,10 +304,7 @@ gemm_fp8_kernel(Fp8Product g) {
                 const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
                 const int c = col + (kgrp & 1) * 16 + (kgrp & 2) * 4;
                 const i32x4_t w = {(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
-                if (row < g.m && c < g.n_out) {
-                    i32x4_t* const at = reinterpret_cast<i32x4_t*>(g.out + (long)row * g.n_out + c);
-                    store_streamed(at, w, g.stream);
-                }
+                if (row < g.m && c < g.n_out) store_streamed<16>(g.out + (long)row * g.n_out + c, w, g.stream);
             } else if (row < g.m) {
                 if (col + kgrp * 4 < g.n_out) fp8_store(g, row, col + kgrp * 4, u);
                 if (col + 16 + kgrp * 4 < g.n_out) fp8_store(g, row, col + 16 + kgrp * 4, v);

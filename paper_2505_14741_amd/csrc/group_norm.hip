@@ -86,7 +86,7 @@ __device__ __forceinline__ void store_channels(T* p, const float (&v)[V], bool s
 #pragma unroll
         for (int i = 0; i < V; ++i) w[i] = (typename ElemOf<T>::type)v[i];
     }
-    store_streamed(reinterpret_cast<typename ChannelsOf<T, V>::mem*>(p), (typename ChannelsOf<T, V>::mem)w, stream);
+    store_streamed<sizeof(T)>(p, w, stream);
 }
 
 // PHASE 0: moments of the chunk's groups to a.part; 1: moments of all chunks from a.part, then the result; 2: both, one chunk.

@@ -36,10 +36,13 @@ __device__ __forceinline__ float exp_near(float d) {
     return __builtin_fmaf(e, __builtin_fmaf(-t, LN2_REST, __builtin_fmaf(-t, LN2, d)), e);
 }
 
-// A store that does not keep a place in L2 (see STREAM_BYTES), or an ordinary one.  (The empty statements keep the compiler from merging
-// the two into an ordinary store.)
-template <typename V>
-__device__ __forceinline__ void store_streamed(V* at, V v, bool stream) {
+// A store that does not keep a place in L2 (see STREAM_BYTES), or an ordinary one, at an address that is a multiple of ALIGN bytes.  (The
+// empty statements keep the compiler from merging the two into an ordinary store.  An alignment in the pointer's type would be lost where the
+// type is deduced: hence the argument.)
+template <int ALIGN, typename V>
+__device__ __forceinline__ void store_streamed(void* p, V v, bool stream) {
+    typedef V at_t __attribute__((aligned(ALIGN)));
+    at_t* const at = reinterpret_cast<at_t*>(p);
     if (stream) {
         asm volatile("");
         __builtin_nontemporal_store(v, at);

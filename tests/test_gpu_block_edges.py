@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2505_14741_amd import binding as B
-from test_gpu_block_ops import DEV, NAN, U, check_cross, cross_ref, gen, randn
+from test_gpu_block_ops import DEV, NAN, U, check_cross, check_gnorm, cross_ref, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +89,20 @@ def test_scores_whose_difference_is_beyond_their_type(dtype, first, nq, nk):
         check_cross(q.to(dtype), kk.to(dtype).contiguous(), vv.to(dtype).contiguous(), 1e-38)
         mask[0, 1 if first == 1 else 0] = False                  # (other paths where a key is out)
         check_cross(q.to(dtype), kk.to(dtype).contiguous(), vv.to(dtype).contiguous(), 1e-38, key_mask=mask)
+
+
+# ------------------------------------------------------------------------------------------------- group norm
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("off,channels", [(3, 256), (1, 324)])
+def test_group_norm_of_slices_on_no_border_beyond_the_caches(dtype, off, channels):
+    """Results over 32 MB, which are stored past L2, from and into channel slices at odd elements: loads and stores of 8 and 4 channels."""
+    positions = 70200
+    g = gen(28)
+    wide = torch.full((1, positions + 1, channels + 5), 9.0, dtype=dtype, device=DEV)
+    x = randn(g, 1, positions, channels + 7).to(dtype)[:, :, off:off + channels]
+    gamma, beta = randn(g, channels + 1)[1:], randn(g, channels + 1)[1:]
+    got = check_gnorm(x, 4, gamma, beta, act=2, out=wide[:, :-1, off:off + channels])
+    rest = torch.ones_like(wide, dtype=torch.bool)
+    rest[:, :-1, off:off + channels] = False
+    assert bool((wide[rest] == 9.0).all())
+    assert torch.equal(got, B.group_norm(x.contiguous(), 4, gamma.clone(), beta.clone(), act=2))
