@@ -217,7 +217,7 @@ PS_API int cross_attn(const void* q, const void* k, const void* v, const int32_t
  *   scale  DEVICE e8m0 bytes [kp / 128][pitch], pitch = rows rounded up to a multiple of 16, filled up with 0
  * fp8_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment).  A block's scale is the
  * least power of two >= 2^-127 under which its largest finite |x| is at most 448; values are rounded once, to nearest even; NaN and
- * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^28 blocks. */
+ * infinities become NaN.  q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, at most 2^28 - 16 blocks. */
 PS_API int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream);
 
 /* out[m, n_out] = act(a * w^T + bias) for operands in the format above, a of m rows and w of n_out rows, both of k columns; out DEVICE bf16, row-major; act 0 none, 1 tanh-GELU.  bias DEVICE fp32 [n_out].  All pointers

@@ -10,6 +10,7 @@
 #include "cross_attention.h"
 #include "fp8.h"
 #include "group_norm.h"
+#include "plan.h"
 #include "slim.h"
 
 using namespace ps;
@@ -565,7 +566,7 @@ int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_
     if (dtype != PS_F32 && dtype != PS_BF16) return PS_ERR_DTYPE;
     if (rows < 0 || cols < 1 || rows > (1 << 24) || cols > (1 << 22)) return PS_ERR_SHAPE;
     if (rows == 0) return PS_OK;
-    if ((long)rows * ((cols + 127) / 128) >= (1L << 28)) return PS_ERR_SHAPE;        // (threads of a launch stay below 2^32)
+    if (!grid_fits(quantize_workgroups(rows, cols), 256)) return PS_ERR_SHAPE;
     if (rows > 1 && (x_row < cols || x_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
     if (!x || !q || !scale) return PS_ERR_NULL;
     if (!aligned(x, dtype == PS_BF16 ? 2 : 4) || !aligned(q, 16) || !aligned(scale, 16) || q == x || scale == x || q == scale) return PS_ERR_SHAPE;

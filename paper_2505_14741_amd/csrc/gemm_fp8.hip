@@ -82,8 +82,7 @@ fp8_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsi
 template <typename T>
 static hipError_t launch_quantize_as(const T* x, unsigned char* q, unsigned char* scale, int rows, int cols, long x_row, hipStream_t st) {
     const int blocks = (cols + 127) / 128, pitch = (rows + 15) / 16 * 16;
-    const unsigned grid = (unsigned)(((long)rows * blocks + 15) / 16);
-    fp8_quantize_kernel<T><<<grid, 256, 0, st>>>(x, q, scale, rows, cols, x_row, blocks, pitch);
+    fp8_quantize_kernel<T><<<(unsigned)quantize_workgroups(rows, cols), 256, 0, st>>>(x, q, scale, rows, cols, x_row, blocks, pitch);
     return hipGetLastError();
 }
 

@@ -292,6 +292,12 @@ constexpr size_t few_workspace_bytes(bool bf16, const FewPlan& p, int batch, int
 // 70200 x 512, 72 MB, which reads its input twice: 43 -> 39; attention of 8 x 1350 x 30 heads of 64, 41 MB: 31 -> 30).
 constexpr size_t STREAM_BYTES = (size_t)32 << 20;
 
+// Threads of a launch in each dimension of its grid stay below 2^32.
+constexpr bool grid_fits(long workgroups, int threads) { return workgroups * threads < (1L << 32); }
+
+// ---- quantizer (gemm_fp8.hip): a workgroup of 256 threads takes 16 blocks
+constexpr long quantize_workgroups(int rows, int cols) { return ((long)rows * ((cols + 127) / 128) + 15) / 16; }
+
 // ---- 8-bit products (gemm_fp8.hip): which tile, and how many pieces of k
 // Us of a round of workgroups: fixed + blocks of 128 k * stage; `lone`: up to one workgroup per compute unit where two fit.
 // Measured, us on 64 x 64 / 128 x 128 / 192 x 192 / 192 x 256 tiles (operands that change from call to call): 448 rows x 7680, k = 1920

@@ -1,10 +1,33 @@
 """Operators of a conditioned predictor block, without a GPU: what the compiler is told of addresses, limits of launches, what is refused at the
 ends of the ranges."""
+import ctypes as C
 import os
 import re
 import subprocess
 
+import pytest
+
+from paper_2505_14741_amd import binding as B
 from paper_2505_14741_amd import build
+
+FAKE = 0x10000                                                   # never dereferenced: what is called with it is refused
+WRAPPERS = """
+#include "plan.h"
+extern "C" long quantize_workgroups(int rows, int cols) { return ps::quantize_workgroups(rows, cols); }
+extern "C" bool grid_fits(long workgroups, int threads) { return ps::grid_fits(workgroups, threads); }
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("edge_rules")
+    src, lib = os.path.join(d, "rules.cpp"), os.path.join(d, "rules.so")
+    with open(src, "w") as f:
+        f.write(WRAPPERS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", build.CSRC, src, "-o", lib], check=True)
+    r = C.CDLL(lib)
+    r.quantize_workgroups.restype, r.grid_fits.restype, r.grid_fits.argtypes = C.c_long, C.c_bool, [C.c_long, C.c_int]
+    return r
 
 
 def test_group_norm_accesses_promise_no_alignment_beyond_an_element():
@@ -23,3 +46,14 @@ def test_group_norm_accesses_promise_no_alignment_beyond_an_element():
     for kind, count, elem, streamed in [(k, n, e, s) for n, e in (("8", "bfloat"), ("4", "bfloat"), ("4", "float"))
                                         for k, s in (("load", False), ("store", False), ("store", True))]:
         assert (kind, count, elem, streamed) in seen
+
+
+def test_quantizer_launches_fit(rules):
+    """Blocks are rounded up to whole workgroups of 16; their threads stay below 2^32, the sizes that would not are refused."""
+    fits = lambda rows, blocks: rules.grid_fits(rules.quantize_workgroups(rows, blocks * 128), 256)  # noqa: E731
+    assert rules.quantize_workgroups(1, 1) == 1 and rules.quantize_workgroups(16, 128) == 1 and rules.quantize_workgroups(17, 128) == 2
+    assert rules.quantize_workgroups((1 << 24) - 1, 2048) * 256 == (1 << 32) - 256
+    for rows, blocks, ok in (((1 << 24) - 1, 16, True), (1 << 24, 15, True), (16384, 16383, True), (16385, 16383, False), (1 << 24, 16, False)):
+        assert fits(rows, blocks) == ok
+        if not ok:
+            assert B.lib().fp8_quantize(FAKE, 2 * FAKE, 3 * FAKE, rows, blocks * 128, blocks * 128, 1, None) == -2
