@@ -527,7 +527,7 @@ int cross_args(const cross_attn_shape* s, CrossArgs& a) {
         !strides_ok(s->batch, s->q_len, s->heads, s->o_batch, s->o_token, s->o_head, es, true) || s->mask_batch < 0)
         return PS_ERR_SHAPE;
     const long share = s->heads / s->kv_heads, rows = s->q_len * share;
-    if (rows > (1L << 30) || (rows + 15) / 16 * s->batch * s->kv_heads > (1L << 25)) return PS_ERR_SHAPE;    // (threads of a launch stay below 2^32)
+    if (!cross_rows_fit(s->batch, rows, s->kv_heads)) return PS_ERR_SHAPE;
     a = CrossArgs{};
     a.mask_batch = s->mask_batch;
     a.batch = s->batch; a.rows = (int)rows; a.share = (int)share; a.kv_len = s->kv_len; a.kv_heads = s->kv_heads;

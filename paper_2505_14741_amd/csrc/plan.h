@@ -345,6 +345,14 @@ struct CrossPlan { int block, nsplit; bool resident; };
 constexpr int cross_v_pitch(int head_dim) { return head_dim == 16 ? 24 : head_dim + 16; }
 constexpr int cross_resident_key_bytes(int head_dim) { return 2 * (head_dim + 8 + cross_v_pitch(head_dim)) + 4; }
 
+// The most rows: 2^25 times 16 over all samples and key heads.  The grid is key heads x blocks of 64 rows at least in x (x pieces where that is
+// not much) and samples in z; each dimension's threads stay below 2^32, and a launch may have more of them in all.  In x: heads of up to 64
+// rows are at most 65535 workgroups; of n > 1 started blocks, 2.5 n times 16 rows at least, so at most 2^25 / 2.5.  (512 samples x 65535 heads
+// of one row, 2^33 threads, 52 ms.)
+constexpr bool cross_rows_fit(int batch, long rows, int kv_heads) {
+    return rows <= (1L << 30) && (rows + 15) / 16 * batch * kv_heads <= (1L << 25);
+}
+
 constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, int head_dim, int cus) {
     CrossPlan p{};
     // bf16: 64, 128 or 192 rows, whichever of the last two wastes less; more registers than heads of 128 leave spill (16 heads, 4290 rows x 512

@@ -2,6 +2,7 @@
 ends of the ranges."""
 import ctypes as C
 import os
+import random
 import re
 import subprocess
 
@@ -14,6 +15,11 @@ FAKE = 0x10000                                                   # never derefer
 WRAPPERS = """
 #include "plan.h"
 extern "C" long quantize_workgroups(int rows, int cols) { return ps::quantize_workgroups(rows, cols); }
+extern "C" bool cross_rows_fit(int batch, long rows, int kv_heads) { return ps::cross_rows_fit(batch, rows, kv_heads); }
+extern "C" long cross_x(int bf16, int rows, int kv_len, int kv_heads, int head_dim) {
+    const ps::CrossPlan p = ps::cross_plan(bf16 != 0, rows, kv_len, kv_heads, head_dim, 256);
+    return (long)kv_heads * p.nsplit * ((rows + (long)p.block - 1) / p.block);
+}
 extern "C" bool grid_fits(long workgroups, int threads) { return ps::grid_fits(workgroups, threads); }
 """
 
@@ -27,6 +33,7 @@ def rules(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", build.CSRC, src, "-o", lib], check=True)
     r = C.CDLL(lib)
     r.quantize_workgroups.restype, r.grid_fits.restype, r.grid_fits.argtypes = C.c_long, C.c_bool, [C.c_long, C.c_int]
+    r.cross_rows_fit.restype, r.cross_rows_fit.argtypes, r.cross_x.restype = C.c_bool, [C.c_int, C.c_long, C.c_int], C.c_long
     return r
 
 
@@ -57,3 +64,28 @@ def test_quantizer_launches_fit(rules):
         assert fits(rows, blocks) == ok
         if not ok:
             assert B.lib().fp8_quantize(FAKE, 2 * FAKE, 3 * FAKE, rows, blocks * 128, blocks * 128, 1, None) == -2
+
+
+def test_cross_attention_launches_fit(rules):
+    """Every shape that is accepted has fewer than 2^32 threads in x, and at most 65535 samples in z; the last accepted and first refused."""
+    r = random.Random(4)
+    for batch, rows, kv_heads, ok in ((512, 1, 65535, True), (513, 1, 65535, False), (1, 1 << 29, 1, True), (1, (1 << 29) + 1, 1, False), (1, 8192, 65535, True),
+                                      (1, 8193, 65535, False), (65535, 1, 512, True), (65535, 16, 512, True), (65535, 17, 512, False)):
+        assert rules.cross_rows_fit(batch, rows, kv_heads) == ok
+        if not ok and rows < 1 << 24:
+            width = kv_heads * 16
+            s = B._CrossShape(batch=batch, q_len=rows, kv_len=1, heads=kv_heads, kv_heads=kv_heads, head_dim=16, dtype=1, scale=1.0, q_batch=rows * width,
+                              q_token=width, q_head=16, k_batch=width, k_token=width, k_head=16, v_batch=width, v_token=width, v_head=16, o_batch=rows * width,
+                              o_token=width, o_head=16)
+            assert B.lib().cross_attn(FAKE, 2 * FAKE, 3 * FAKE, None, None, 4 * FAKE, C.byref(s), None, 0, None) == -2
+    tried = 0
+    while tried < 3000:
+        kv_heads, batch = int(2 ** r.uniform(0, 16)) & 65535 or 1, int(2 ** r.uniform(0, 10))
+        rows = max(1, int((1 << 29) / kv_heads / batch * 2 ** r.uniform(-1, 0.1))) if r.random() < 0.5 else int(2 ** r.uniform(0, 30))
+        if not rules.cross_rows_fit(batch, rows, kv_heads):
+            continue
+        tried += 1
+        for bf16 in (0, 1):
+            for d in (16, 64, 128):
+                kv_len = int(2 ** r.uniform(0, 24))
+                assert rules.grid_fits(rules.cross_x(bf16, rows, kv_len, kv_heads, d), 256), (rows, kv_heads, kv_len, d)

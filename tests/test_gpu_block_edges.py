@@ -91,6 +91,19 @@ def test_scores_whose_difference_is_beyond_their_type(dtype, first, nq, nk):
         check_cross(q.to(dtype), kk.to(dtype).contiguous(), vv.to(dtype).contiguous(), 1e-38, key_mask=mask)
 
 
+@pytest.mark.parametrize("batch,heads,nq", [(512, 65535, 1), (1, 65535, 8192)])
+def test_cross_attention_on_the_largest_grids(batch, heads, nq):
+    """The most samples x heads x tokens, one key each: the result is its value.  2^25 workgroups over samples, and 2^22 of 128 rows in one."""
+    print(f"cross_attn batch={batch} heads={heads} q={nq}", flush=True)
+    g = gen(29)
+    v = torch.randn(batch, 1, heads, 16, generator=g, device=DEV, dtype=torch.bfloat16)
+    q = torch.ones(1, 1, 1, 16, device=DEV, dtype=torch.bfloat16).expand(batch, nq, heads, 16)
+    out = B.cross_attn(q, v, v, 0.25)
+    for at in range(0, nq, 1024):
+        part = out[:, at:at + 1024]
+        assert torch.equal(part, v.expand_as(part))
+
+
 # ------------------------------------------------------------------------------------------------- group norm
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("off,channels", [(3, 256), (1, 324)])
