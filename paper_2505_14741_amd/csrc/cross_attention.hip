@@ -693,9 +693,11 @@ static hipError_t launch_cross_hd(int dtype, CrossArgs a, hipStream_t st) {
     }
     const dim3 grid((unsigned)(a.kv_heads * p.nsplit) * (unsigned)((a.rows + p.block - 1) / p.block), 1, a.batch);
     if (dtype != PS_BF16) cross_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
-    else if (p.block == 64) cross_bf16_kernel<HD, 1><<<grid, 256, 0, st>>>(a);
-    else if (p.block == 128) cross_bf16_kernel<HD, 2><<<grid, 256, 0, st>>>(a);
-    else if constexpr (HD <= 64) cross_bf16_kernel<HD, 3><<<grid, 256, 0, st>>>(a);
+    else if (HD > 64 || p.block == 64) cross_bf16_kernel<HD, 1><<<grid, 256, 0, st>>>(a);      // (heads of 128 always: see cross_plan)
+    else if constexpr (HD <= 64) {
+        if (p.block == 128) cross_bf16_kernel<HD, 2><<<grid, 256, 0, st>>>(a);
+        else cross_bf16_kernel<HD, 3><<<grid, 256, 0, st>>>(a);
+    }
     if (p.nsplit > 1) {
         const long lines = (long)a.batch * a.kv_heads * a.rows;
         const unsigned wgs = (unsigned)((lines + 3) / 4 < (1L << 22) ? (lines + 3) / 4 : 1L << 22);

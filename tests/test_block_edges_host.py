@@ -16,6 +16,9 @@ WRAPPERS = """
 #include "plan.h"
 extern "C" long quantize_workgroups(int rows, int cols) { return ps::quantize_workgroups(rows, cols); }
 extern "C" bool cross_rows_fit(int batch, long rows, int kv_heads) { return ps::cross_rows_fit(batch, rows, kv_heads); }
+extern "C" void cross(int rows, int kv_len, int kv_heads, int head_dim, int* out) {
+    out[0] = ps::cross_plan(true, rows, kv_len, kv_heads, head_dim, 256).block;
+}
 extern "C" long cross_x(int bf16, int rows, int kv_len, int kv_heads, int head_dim) {
     const ps::CrossPlan p = ps::cross_plan(bf16 != 0, rows, kv_len, kv_heads, head_dim, 256);
     return (long)kv_heads * p.nsplit * ((rows + (long)p.block - 1) / p.block);
@@ -89,3 +92,18 @@ def test_cross_attention_launches_fit(rules):
             for d in (16, 64, 128):
                 kv_len = int(2 ** r.uniform(0, 24))
                 assert rules.grid_fits(rules.cross_x(bf16, rows, kv_len, kv_heads, d), 256), (rows, kv_heads, kv_len, d)
+
+
+def test_the_library_holds_the_attention_kernels_that_the_rule_picks(rules):
+    """Rows per workgroup of the bf16 kernel by head size, over all sizes: each one's kernel is built, and no other."""
+    out, picked = (C.c_int * 5)(), set()
+    for d in (16, 32, 64, 128):
+        for rows in list(range(1, 800)) + [1 << n for n in range(10, 30)]:
+            for kv_len in (64, 4096):
+                rules.cross(rows, kv_len, 30, d, out)
+                picked.add((d, out[0] // 64))
+    with open(build.LIB, "rb") as f:
+        lib = f.read()
+    for d in (16, 32, 64, 128):
+        for tiles in (1, 2, 3, 4):
+            assert (b"cross_bf16_kernelILi%dELi%dEE" % (d, tiles) in lib) == ((d, tiles) in picked), (d, tiles)
