@@ -12,6 +12,14 @@ from paper_2505_14741_amd import binding as B
 from paper_2505_14741_amd import build
 
 FAKE = 0x10000                                                   # never dereferenced: what is called with it is refused
+# 8-bit products (rows, columns, k) for each tile: last tiles that are partial in either direction, columns that no 16-byte store divides, one
+# block of k, two, three, a last one that is partial, and many.  test_gpu_block_edges.py computes them.
+PRODUCTS = {
+    (64, 64): [(1, 65, 100), (70, 1004, 129), (129, 257, 300), (112, 2050, 1920), (33, 130, 7680)],
+    (128, 128): [(1100, 1920, 100), (1100, 1921, 129), (4600, 516, 300), (1037, 1924, 1920), (1100, 1920, 7680)],
+    (192, 192): [(2500, 2052, 100), (2500, 2050, 129), (4600, 1920, 300), (4516, 1917, 1920), (4600, 1908, 7680)],
+    (192, 256): [(4600, 2052, 100), (4600, 2300, 129), (4600, 2052, 256), (4600, 2301, 300), (4600, 2300, 500), (3500, 5760, 1920), (9000, 1003, 1920)],
+}
 WRAPPERS = """
 #include "plan.h"
 extern "C" long quantize_workgroups(int rows, int cols) { return ps::quantize_workgroups(rows, cols); }
@@ -23,6 +31,11 @@ extern "C" long cross_x(int bf16, int rows, int kv_len, int kv_heads, int head_d
     const ps::CrossPlan p = ps::cross_plan(bf16 != 0, rows, kv_len, kv_heads, head_dim, 256);
     return (long)kv_heads * p.nsplit * ((rows + (long)p.block - 1) / p.block);
 }
+extern "C" void fp8(int m, int n, int blocks, int* out) {
+    const ps::Fp8Plan p = ps::fp8_plan(m, n, blocks, false, 256);
+    out[0] = ps::kFp8Tiles[p.tile].bm; out[1] = ps::kFp8Tiles[p.tile].bn;
+}
+extern "C" int fp8_tiles() { return ps::FP8_TILES; }
 extern "C" bool grid_fits(long workgroups, int threads) { return ps::grid_fits(workgroups, threads); }
 """
 
@@ -107,3 +120,12 @@ def test_the_library_holds_the_attention_kernels_that_the_rule_picks(rules):
     for d in (16, 32, 64, 128):
         for tiles in (1, 2, 3, 4):
             assert (b"cross_bf16_kernelILi%dELi%dEE" % (d, tiles) in lib) == ((d, tiles) in picked), (d, tiles)
+
+
+def test_tested_products_take_every_tile(rules):
+    assert len(PRODUCTS) == rules.fp8_tiles()
+    out = (C.c_int * 2)()
+    for tile, shapes in PRODUCTS.items():
+        for m, n, k in shapes:
+            rules.fp8(m, n, (k + 127) // 128, out)
+            assert tuple(out) == tile, (m, n, k)

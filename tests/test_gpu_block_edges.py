@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from paper_2505_14741_amd import binding as B
-from test_gpu_block_ops import DEV, NAN, U, check_cross, check_gnorm, cross_ref, gen, randn
+from test_block_edges_host import PRODUCTS
+from test_gpu_block_ops import DEV, NAN, U, check_cross, check_gnorm, cross_ref, fp8_ref, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -102,6 +103,33 @@ def test_cross_attention_on_the_largest_grids(batch, heads, nq):
     for at in range(0, nq, 1024):
         part = out[:, at:at + 1024]
         assert torch.equal(part, v.expand_as(part))
+
+
+# ------------------------------------------------------------------------------------------------- 8-bit products
+@pytest.mark.parametrize("rows,n_out,k", [s for shapes in PRODUCTS.values() for s in shapes])
+@pytest.mark.parametrize("act", [0, 1])
+def test_products_of_every_tile(rows, n_out, k, act):
+    """The bounds of test_product_of_blocks; what lies behind the last row stays; a row has the same bits on the tiles of few rows."""
+    print(f"dit_linear_fp8 {rows}x{n_out}x{k} act={act}", flush=True)
+    g = gen(rows + n_out + k)
+    a, a_scale = B.fp8_quantize(randn(g, rows, k) * torch.exp(2 * randn(g, rows, 1)) * torch.exp(randn(g, k)))
+    w, w_scale = B.fp8_quantize(randn(g, n_out, k) / math.sqrt(k))
+    bias = randn(g, n_out)
+    buf = torch.full((rows + 3, n_out), 5.0, dtype=torch.bfloat16, device=DEV)
+    out = B.dit_linear_fp8(a, a_scale, w, w_scale, bias, act=act, out=buf[:rows], use_workspace=False)
+    ref, off = fp8_ref(a, a_scale, w, w_scale, bias, act)
+    tol = 1.13 * off + U[torch.bfloat16] * ref.abs() + (2.0 ** -20 * (ref.abs() + 1.0) if act else 0.0) + 1e-30
+    assert bool(((out.double() - ref).abs() <= tol).all()), float(((out.double() - ref).abs() / tol).max())
+    assert bool((buf[rows:] == 5.0).all())
+    few = min(rows, 48)
+    assert torch.equal(B.dit_linear_fp8(a[-few:], scales_of_last(a_scale, rows, few), w, w_scale, bias, act=act, use_workspace=False), out[-few:])
+
+
+def scales_of_last(scale, rows, few):
+    """The scales of the last `few` rows as an operand of their own: [blocks, few rounded up to 16], filled up with zeros."""
+    s = torch.zeros(scale.shape[0], (few + 15) // 16 * 16, dtype=torch.uint8, device=DEV)
+    s[:, :few] = scale.view(torch.uint8)[:, rows - few:rows]
+    return s.view(scale.dtype)
 
 
 # ------------------------------------------------------------------------------------------------- group norm
