@@ -194,7 +194,7 @@ PS_API int dit_linear(const void* a, const void* w, const float* bias, void* out
  * k and v kv_heads (a divisor): query heads h * (heads / kv_heads) .. share key head h.  head_dim in {16, 32, 64, 128}, its
  * elements contiguous; every other stride is free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0 to repeat
  * an operand; of an extent of 1 they are ignored), so k and v may be the halves of one projection.  Pointers 16-byte aligned; o
- * must not overlap the inputs.  batch and heads <= 65535, q_len and kv_len <= 2^24, and at most 2^25 times 16 query rows (q_len * heads / kv_heads
+ * must not overlap the inputs, nor its heads each other (refused where one stride or two of them make them).  batch and heads <= 65535, q_len and kv_len <= 2^24, and at most 2^25 times 16 query rows (q_len * heads / kv_heads
  * of each sample and key head, rounded up to 16).  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).  Scores times scale * log2(e) must be
  * finite in fp32, and so must be the largest |v| times kv_len (in bf16 times 2^8 more: the sums in front of the division can be as large).
  * bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32; fp32: everything in fp32.
@@ -235,7 +235,7 @@ PS_API int dit_linear_fp8(const void* a, const void* a_scale, const void* w, con
  *   out = act((x - mean) / sqrt(var + eps) * gamma + beta),
  * var the mean squared deviation; act 0 none, 1 tanh-GELU, 2 SiLU.  x, out DEVICE [batch, positions, channels] in `dtype`, channels
  * contiguous, batch and position strides in elements (any alignment; x's may be 0; ignored for an extent of 1);
- * out == x is allowed with equal strides, any other overlap is not.  gamma, beta DEVICE fp32 [channels], either may be NULL (1, 0).
+ * out == x is allowed with equal strides, any other overlap is not, nor one of out's positions.  gamma, beta DEVICE fp32 [channels], either may be NULL (1, 0).
  * Statistics in fp32, merged pairwise.  batch and positions may be 0; channels <= 65536.
  * workspace: DEVICE, 256-byte aligned, >= group_norm_workspace_bytes(...) (may be NULL when that is 0). */
 typedef struct {

@@ -504,11 +504,11 @@ int dit_linear(const void* a, const void* w, const float* bias, void* out, int m
 namespace {
 
 // strides of a [batch, token, head, head_dim] operand that 16-byte accesses can follow; an extent of one has no stride
-bool strides_ok(long n_batch, long n_token, long n_head, int64_t batch, int64_t token, int64_t head, int esize, bool written) {
+bool strides_ok(long n_batch, long n_token, long n_head, int64_t batch, int64_t token, int64_t head, int esize) {
     const int64_t unit = 16 / esize, st[3] = {batch, token, head};
     const long n[3] = {n_batch, n_token, n_head};
     for (int i = 0; i < 3; ++i)
-        if (n[i] > 1 && (st[i] < 0 || st[i] % unit || st[i] > ((int64_t)1 << 40) || (written && st[i] == 0))) return false;
+        if (n[i] > 1 && (st[i] < 0 || st[i] % unit || st[i] > ((int64_t)1 << 40))) return false;
     return true;
 }
 
@@ -521,10 +521,13 @@ int cross_args(const cross_attn_shape* s, CrossArgs& a) {
     if (s->batch > 65535 || s->heads > 65535 || s->q_len > (1 << 24) || s->kv_len > (1 << 24)) return PS_ERR_SHAPE;
     if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return PS_ERR_SHAPE;
     const int es = s->dtype == PS_BF16 ? 2 : 4;
-    if (!strides_ok(s->batch, s->q_len, s->heads, s->q_batch, s->q_token, s->q_head, es, false) ||
-        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->k_batch, s->k_token, s->k_head, es, false) ||
-        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->v_batch, s->v_token, s->v_head, es, false) ||
-        !strides_ok(s->batch, s->q_len, s->heads, s->o_batch, s->o_token, s->o_head, es, true) || s->mask_batch < 0)
+    if (!strides_ok(s->batch, s->q_len, s->heads, s->q_batch, s->q_token, s->q_head, es) ||
+        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->k_batch, s->k_token, s->k_head, es) ||
+        !strides_ok(s->batch, s->kv_len, s->kv_heads, s->v_batch, s->v_token, s->v_head, es) ||
+        !strides_ok(s->batch, s->q_len, s->heads, s->o_batch, s->o_token, s->o_head, es) || s->mask_batch < 0)
+        return PS_ERR_SHAPE;
+    if (pieces_meet(s->o_batch, s->batch, s->o_token, s->q_len, s->head_dim) || pieces_meet(s->o_batch, s->batch, s->o_head, s->heads, s->head_dim) ||
+        pieces_meet(s->o_token, s->q_len, s->o_head, s->heads, s->head_dim))
         return PS_ERR_SHAPE;
     const long share = s->heads / s->kv_heads, rows = s->q_len * share;
     if (!cross_rows_fit(s->batch, rows, s->kv_heads)) return PS_ERR_SHAPE;
@@ -614,7 +617,7 @@ int group_norm(const void* x, const float* gamma, const float* beta, void* out, 
         if (s->batch > 1 && (st < 0 || st > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
     for (int64_t st : {s->x_position, s->out_position})
         if (s->positions > 1 && (st < 0 || st > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
-    if ((s->batch > 1 && s->out_batch < s->channels) || (s->positions > 1 && s->out_position < s->channels)) return PS_ERR_SHAPE;
+    if (pieces_meet(s->out_batch, s->batch, s->out_position, s->positions, s->channels)) return PS_ERR_SHAPE;
     if (s->batch == 0 || s->positions == 0) return PS_OK;
     if (!x || !out) return PS_ERR_NULL;
     const size_t esize = s->dtype == PS_BF16 ? 2 : 4;

@@ -295,6 +295,21 @@ constexpr size_t STREAM_BYTES = (size_t)32 << 20;
 // Threads of a launch in each dimension of its grid stay below 2^32.
 constexpr bool grid_fits(long workgroups, int threads) { return workgroups * threads < (1L << 32); }
 
+// Whether pieces of `width` elements at i * a + j * b, 0 <= i < n, 0 <= j < m, overlap (an extent of one has no stride; one of n and m is at most
+// 65536, strides at most 2^40).
+constexpr bool pieces_meet(long a, long n, long b, long m, long width) {
+    if (n > m) { const long s = a, e = n; a = b; n = m; b = s; m = e; }
+    if ((n > 1 && a < width) || (m > 1 && b < width)) return true;
+    if (n < 2 || (n - 1) * a + width <= b) return false;         // (all of i between two neighbours of j)
+    for (long i = 1; i < n; ++i) {
+        const long p = i * a, j = p / b, r = p - j * b;          // the neighbours of p among j * b are j and j + 1
+        if (j > m) return false;
+        if (j < m && r < width) return true;
+        if (j + 1 < m && b - r < width) return true;
+    }
+    return false;
+}
+
 // ---- quantizer (gemm_fp8.hip): a workgroup of 256 threads takes 16 blocks
 constexpr long quantize_workgroups(int rows, int cols) { return ((long)rows * ((cols + 127) / 128) + 15) / 16; }
 

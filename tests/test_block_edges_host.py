@@ -36,6 +36,7 @@ extern "C" void fp8(int m, int n, int blocks, int* out) {
     out[0] = ps::kFp8Tiles[p.tile].bm; out[1] = ps::kFp8Tiles[p.tile].bn;
 }
 extern "C" int fp8_tiles() { return ps::FP8_TILES; }
+extern "C" bool pieces_meet(long a, long n, long b, long m, long width) { return ps::pieces_meet(a, n, b, m, width); }
 extern "C" bool grid_fits(long workgroups, int threads) { return ps::grid_fits(workgroups, threads); }
 """
 
@@ -50,6 +51,7 @@ def rules(tmp_path_factory):
     r = C.CDLL(lib)
     r.quantize_workgroups.restype, r.grid_fits.restype, r.grid_fits.argtypes = C.c_long, C.c_bool, [C.c_long, C.c_int]
     r.cross_rows_fit.restype, r.cross_rows_fit.argtypes, r.cross_x.restype = C.c_bool, [C.c_int, C.c_long, C.c_int], C.c_long
+    r.pieces_meet.restype, r.pieces_meet.argtypes = C.c_bool, [C.c_long] * 5
     return r
 
 
@@ -129,3 +131,37 @@ def test_tested_products_take_every_tile(rules):
         for m, n, k in shapes:
             rules.fp8(m, n, (k + 127) // 128, out)
             assert tuple(out) == tile, (m, n, k)
+
+
+def test_pieces_that_meet(rules):
+    """Against the pieces counted one by one; and at extents and strides as large as they may be, which take no time."""
+    r = random.Random(5)
+    met = 0
+    for _ in range(20000):
+        width, n, m = r.randint(1, 6), r.randint(1, 7), r.randint(1, 7)
+        a, b = r.randint(0, 40), r.randint(0, 40)
+        at = sorted(i * a + j * b for i in range(n) for j in range(m))
+        want = any(y - x < width for x, y in zip(at, at[1:]))
+        met += want
+        assert rules.pieces_meet(a, n, b, m, width) == want, (a, n, b, m, width)
+    assert 2000 < met < 18000
+    far = 1 << 40
+    for a, n, b, m, width, want in ((far, 65535, 64, 1 << 24, 64, False), (far, 65535, far, 1 << 24, 64, True), (far, 65535, far - 64, 1 << 24, 128, True),
+                                    (64, 65535, 64 * 65535, 1 << 24, 64, False), (64, 65535, 64 * 65534, 1 << 24, 64, True)):
+        assert rules.pieces_meet(a, n, b, m, width) == want and rules.pieces_meet(b, m, a, n, width) == want
+
+
+@pytest.mark.parametrize("over", [dict(o_head=32), dict(o_token=128), dict(o_token=64, o_head=64), dict(o_batch=256, o_token=256), dict(o_batch=64),
+                                  dict(o_batch=128, o_token=640, o_head=160), dict(q_len=1, o_batch=192)])
+def test_cross_attention_refuses_an_output_whose_heads_overlap(over):
+    s = dict(batch=2, q_len=5, kv_len=7, heads=4, kv_heads=2, head_dim=64, dtype=1, scale=0.125, q_batch=1280, q_token=256, q_head=64, k_batch=896, k_token=128, k_head=64,
+             v_batch=896, v_token=128, v_head=64, o_batch=1280, o_token=256, o_head=64)
+    s.update(over)
+    assert B.lib().cross_attn(FAKE, 2 * FAKE, 3 * FAKE, None, None, 4 * FAKE, C.byref(B._CrossShape(**s)), None, 0, None) == -2
+
+
+@pytest.mark.parametrize("over", [dict(out_batch=64), dict(out_batch=128, out_position=64), dict(out_batch=64, out_position=64), dict(out_batch=128, out_position=160)])
+def test_group_norm_refuses_an_output_whose_positions_overlap(over):
+    s = dict(batch=2, positions=5, channels=64, groups=8, act=0, dtype=1, eps=1e-5, x_batch=320, x_position=64, out_batch=320, out_position=64)
+    s.update(over)
+    assert B.lib().group_norm(FAKE, None, None, 2 * FAKE, C.byref(B._GroupNormShape(**s)), None, 0, None) == -2

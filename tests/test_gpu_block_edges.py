@@ -147,3 +147,27 @@ def test_group_norm_of_slices_on_no_border_beyond_the_caches(dtype, off, channel
     rest[:, :-1, off:off + channels] = False
     assert bool((wide[rest] == 9.0).all())
     assert torch.equal(got, B.group_norm(x.contiguous(), 4, gamma.clone(), beta.clone(), act=2))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_outputs_that_interleave(dtype):
+    """Samples between the heads of a token, tokens between samples, positions between samples: no overlap, and every other value stays."""
+    g = gen(30)
+    q, k = randn(g, 2, 70, 4, 64).to(dtype), randn(g, 2, 90, 4, 64).to(dtype)
+    for strides in ((64, 640, 160), (64, 128, 2 * 70 * 64), (4 * 64, 2 * 4 * 64, 64)):
+        buf = torch.full((2 * 70 * 640,), 7.0, dtype=dtype, device=DEV)
+        out = buf.as_strided((2, 70, 4, 64), (*strides, 1))
+        check_cross(q, k, k, 0.125, out=out)
+        kept = out.clone()
+        out.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        assert torch.equal(kept, B.cross_attn(q, k, k, 0.125))
+    x = randn(g, 2, 300, 64).to(dtype)
+    for strides in ((96, 160), (64, 128)):
+        buf = torch.full((300 * 160 + 200,), 7.0, dtype=dtype, device=DEV)
+        out = buf.as_strided((2, 300, 64), (*strides, 1))
+        check_gnorm(x, 8, out=out)
+        kept = out.clone()
+        out.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        assert torch.equal(kept, B.group_norm(x, 8))
