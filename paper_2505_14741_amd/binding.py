@@ -279,6 +279,11 @@ def _need(ok: bool, where: str, what: str, status: int = PS_ERR_SHAPE):
         raise PsError(status, f"{where}: {what}")
 
 
+def _need_extents(where: str, *extents: int):
+    """The library's sizes are 32-bit integers, into which ctypes would cut larger ones."""
+    _need(max(extents) < 1 << 31, where, "extents must be below 2^31")
+
+
 def _need_here(where: str, first: torch.Tensor, *others: Optional[torch.Tensor]):
     """Kernels run on the current device and its current stream, on memory of that device."""
     dev = first.get_device()
@@ -299,6 +304,7 @@ def _cross_plan(dtypes, q, qs, k, ks, v, vs, o, os_, lens, mask, scale, device):
     _need(k[0] == B and k[3] == d, w, "k and v must have q's batch and head_dim")
     dt = _CODE.get(dtypes[0])
     _need(dt is not None and dtypes[1] == dtypes[0] and dtypes[2] == dtypes[0], w, "float32 or bfloat16, the same for q, k and v", PS_ERR_DTYPE)
+    _need_extents(w, *q, *k)
     _need(o == q, w, "out must have q's shape")
     _need(dtypes[3] == dtypes[0], w, "out must have q's type", PS_ERR_DTYPE)
     _need(qs[3] == ks[3] == vs[3] == os_[3] == 1, w, "the elements of a head must be contiguous")
@@ -339,6 +345,7 @@ def fp8_quantize(x: torch.Tensor):
     dt = _CODE.get(x.dtype)
     _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
     rows, cols = x.shape
+    _need_extents(w, rows, cols)
     _need(x.stride(1) == 1 or cols == 1, w, "the elements of a row must be contiguous")
     _need_here(w, x)
     blocks = (cols + 127) // 128
@@ -354,6 +361,7 @@ def _fp8_plan(dtypes, a, a_scale, w, w_scale, bias, out, use_workspace, device):
     _need(len(a) == 2 and len(w) == 2 and a[1] == w[1] and a[1] % 128 == 0 and a[1] > 0, f, "a [M, kp] and w [n_out, kp], kp a multiple of 128")
     M, K = a
     Nn = w[0]
+    _need_extents(f, M, K, Nn)
     _need(dtypes[:4] == (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float8_e4m3fn, torch.float8_e8m0fnu), f,
           "values in float8_e4m3fn, scales in float8_e8m0fnu", PS_ERR_DTYPE)
     _need(dtypes[4] == torch.float32, f, "bias must be float32", PS_ERR_DTYPE)
@@ -368,6 +376,7 @@ def dit_linear_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_sc
                    out: Optional[torch.Tensor] = None, use_workspace: bool = True) -> torch.Tensor:
     """act(a w^T + bias) of operands from fp8_quantize: a of [M, K] and w of [n_out, K]; bias float32 [n_out], out bfloat16."""
     f = "dit_linear_fp8"
+    _need(0 <= act <= 1, f, "act 0 or 1")
     if out is None:
         _need(a.dim() == 2 and w.dim() == 2, f, "a [M, kp] and w [n_out, kp]")
         out = torch.empty((a.shape[0], w.shape[0]), dtype=torch.bfloat16, device=a.device)
@@ -388,6 +397,8 @@ def _gnorm_plan(dtypes, x, xs, o, os_, affine, groups, eps, act, device):
     _need(len(x) == 3 and x[2] >= 1, w, "x must be [B, positions, C]")
     dt = _CODE.get(dtypes[0])
     _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    _need_extents(w, *x)
+    _need(1 <= groups <= x[2] and 0 <= act <= 2, w, "1 to C groups, act 0, 1 or 2")
     _need(o == x, w, "out must have x's shape")
     _need(dtypes[1] == dtypes[0], w, "out must have x's type", PS_ERR_DTYPE)
     _need(x[2] == 1 or (xs[2] == 1 and os_[2] == 1), w, "channels must be contiguous")

@@ -165,3 +165,25 @@ def test_group_norm_refuses_an_output_whose_positions_overlap(over):
     s = dict(batch=2, positions=5, channels=64, groups=8, act=0, dtype=1, eps=1e-5, x_batch=320, x_position=64, out_batch=320, out_position=64)
     s.update(over)
     assert B.lib().group_norm(FAKE, None, None, 2 * FAKE, C.byref(B._GroupNormShape(**s)), None, 0, None) == -2
+
+
+def test_binding_refuses_sizes_that_do_not_fit_the_library():
+    """Extents, groups and activations of 2^31 and more, which ctypes would cut to 32 bits (tensors without memory)."""
+    import torch
+    far = (1 << 32) + 5
+    meta = lambda *s, dtype=torch.bfloat16: torch.empty(1, dtype=dtype, device="meta").as_strided(s, (8 * far,) * (len(s) - 1) + (1,))  # noqa: E731
+    q, x, bias = meta(1, 4, 2, 64), torch.empty(1, 4, 64, device="meta"), torch.empty(4, device="meta")
+    e4, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    q8 = lambda rows, k: (torch.empty(rows, k, dtype=e4, device="meta"), torch.empty(k // 128, (rows + 15) // 16 * 16, dtype=e8, device="meta"))  # noqa: E731
+    calls = [(lambda: B.cross_attn(q, meta(1, far, 2, 64), meta(1, far, 2, 64), 1.0), "2\\^31"),
+             (lambda: B.cross_attn(meta(1, far, 2, 64), q, q, 1.0), "2\\^31"),
+             (lambda: B.fp8_quantize(meta(1, far)), "2\\^31"), (lambda: B.fp8_quantize(meta(far, 64)), "2\\^31"),
+             (lambda: B.dit_linear_fp8(*q8(4, 1 << 33), *q8(4, 1 << 33), bias), "2\\^31"),
+             (lambda: B.dit_linear_fp8(*q8(1 << 32, 128), *q8(4, 128), bias), "2\\^31"),
+             (lambda: B.dit_linear_fp8(*q8(4, 128), *q8(4, 128), bias, act=1 << 32), "act"),
+             (lambda: B.group_norm(torch.empty(1, far, 64, device="meta"), 8), "2\\^31"),
+             (lambda: B.group_norm(x, (1 << 32) + 8), "groups"), (lambda: B.group_norm(x, 8, act=1 << 32), "act")]
+    for i, (call, why) in enumerate(calls):
+        with pytest.raises(B.PsError, match=why) as e:
+            call()
+        assert e.value.status == -2, i
