@@ -195,8 +195,9 @@ PS_API int dit_linear(const void* a, const void* w, const float* bias, void* out
  * elements contiguous; every other stride is free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0 to repeat
  * an operand; of an extent of 1 they are ignored), so k and v may be the halves of one projection.  Pointers 16-byte aligned; o
  * must not overlap the inputs, nor its heads each other (refused where one stride or two of them make them).  batch and heads <= 65535, q_len and kv_len <= 2^24, and at most 2^25 times 16 query rows (q_len * heads / kv_heads
- * of each sample and key head, rounded up to 16).  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).  Scores times scale * log2(e) must be
- * finite in fp32, and so must be the largest |v| times kv_len (in bf16 times 2^8 more: the sums in front of the division can be as large).
+ * of each sample and key head, rounded up to 16).  batch, q_len and kv_len may be 0 (kv_len 0: o = 0).
+ * Finite in fp32 must be: scale * log2(e) (refused else); in bf16 q . k, and that times scale * log2(e); in fp32 scale * q, which is rounded
+ * first, and its products with k; the largest |v| times kv_len (in bf16 times 2^8 more: the sums in front of the division can be as large).
  * bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32; fp32: everything in fp32.
  * workspace: DEVICE, 256-byte aligned, >= cross_attn_workspace_bytes(...) (may be NULL when that is 0): where the rows of a sample
  * do not fill the chip its keys are divided among workgroups, and their partial sums pass through it. */

@@ -519,7 +519,7 @@ int cross_args(const cross_attn_shape* s, CrossArgs& a) {
     if (s->head_dim != 16 && s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return PS_ERR_SHAPE;
     if (s->batch < 0 || s->q_len < 0 || s->kv_len < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads) return PS_ERR_SHAPE;
     if (s->batch > 65535 || s->heads > 65535 || s->q_len > (1 << 24) || s->kv_len > (1 << 24)) return PS_ERR_SHAPE;
-    if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return PS_ERR_SHAPE;
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale * CROSS_LOG2E)) return PS_ERR_SHAPE;
     const int es = s->dtype == PS_BF16 ? 2 : 4;
     if (!strides_ok(s->batch, s->q_len, s->heads, s->q_batch, s->q_token, s->q_head, es) ||
         !strides_ok(s->batch, s->kv_len, s->kv_heads, s->k_batch, s->k_token, s->k_head, es) ||

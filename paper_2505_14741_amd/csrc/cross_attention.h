@@ -4,6 +4,8 @@
 
 namespace ps {
 
+constexpr float CROSS_LOG2E = 1.4426950408889634f;       // scores times it and the scale are exponents of two
+
 // A key/value head's query rows are its (token, query head of the group) pairs, row = token * share + head of the group.
 struct CrossArgs {
     const void *q, *k, *v;

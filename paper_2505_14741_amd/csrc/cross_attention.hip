@@ -19,7 +19,6 @@
 namespace ps {
 
 constexpr int CROSS_RESIDENT_WAVES = 8;
-constexpr float CROSS_LOG2E = 1.4426950408889634f;
 
 // the sample's keys, and which of the 64 keys from kv0 on count (wave-uniform)
 __device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {

@@ -187,3 +187,12 @@ def test_binding_refuses_sizes_that_do_not_fit_the_library():
         with pytest.raises(B.PsError, match=why) as e:
             call()
         assert e.value.status == -2, i
+
+
+def test_cross_attention_scale():
+    """A scale is refused from where its product with log2(e) is not finite in fp32: a score of zero would be NaN under it."""
+    s = lambda scale: B._CrossShape(batch=1, q_len=1, kv_len=100000, heads=1, kv_heads=1, head_dim=64, dtype=1, scale=scale, q_batch=64, q_token=64, q_head=64,  # noqa: E731
+                                    k_batch=64, k_token=64, k_head=64, v_batch=64, v_token=64, v_head=64, o_batch=64, o_token=64, o_head=64)
+    for scale, ok in ((2.0 ** -149, True), (2.358e38, True), (2.359e38, False), (3.4e38, False)):
+        assert (B.lib().cross_attn_workspace_bytes(C.byref(s(scale))) > 0) == ok, scale
+        assert B.lib().cross_attn(FAKE, 2 * FAKE, 3 * FAKE, None, None, 4 * FAKE, C.byref(s(scale)), None, 0, None) == (-4 if ok else -2)

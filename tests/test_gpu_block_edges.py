@@ -171,3 +171,14 @@ def test_outputs_that_interleave(dtype):
         out.fill_(7.0)
         assert bool((buf == 7.0).all())
         assert torch.equal(kept, B.group_norm(x, 8))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq,nk", SIZES)
+def test_cross_attention_of_the_largest_scale(dtype, nq, nk):
+    """Scores of 0 to 3 under a scale of 2^127, from queries of 2^-60 and keys of 2^-67 times small whole numbers (exact products)."""
+    g = gen(31)
+    q, k = torch.zeros(1, nq, 2, 64, device=DEV), torch.zeros(1, nk, 2, 64, device=DEV)
+    q[..., 3] = 2.0 ** -60 * torch.randint(0, 2, (1, nq, 2), generator=g, device=DEV)
+    k[..., 3] = 2.0 ** -67 * torch.randint(0, 4, (1, nk, 2), generator=g, device=DEV)
+    check_cross(q.to(dtype), k.to(dtype), randn(g, 1, nk, 2, 64).to(dtype), 2.0 ** 127)
