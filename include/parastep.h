@@ -237,7 +237,7 @@ PS_API int dit_linear_fp8(const void* a, const void* a_scale, const void* w, con
  * var the mean squared deviation; act 0 none, 1 tanh-GELU, 2 SiLU.  x, out DEVICE [batch, positions, channels] in `dtype`, channels
  * contiguous, batch and position strides in elements (any alignment; x's may be 0; ignored for an extent of 1);
  * out == x is allowed with equal strides, any other overlap is not, nor one of out's positions.  gamma, beta DEVICE fp32 [channels], either may be NULL (1, 0).
- * Statistics in fp32, merged pairwise.  batch and positions may be 0; channels <= 65536.
+ * Statistics in fp32, merged pairwise: the sum of a group's squared deviations must be finite there.  batch and positions may be 0; channels <= 65536.
  * workspace: DEVICE, 256-byte aligned, >= group_norm_workspace_bytes(...) (may be NULL when that is 0). */
 typedef struct {
     int batch, positions, channels, groups, act, dtype;

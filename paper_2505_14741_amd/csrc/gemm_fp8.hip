@@ -31,9 +31,7 @@ __global__ void __launch_bounds__(256)
 fp8_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsigned char* __restrict__ scale, int rows, int cols,
                     long x_row, int blocks, int pitch) {
     const unsigned item = blockIdx.x * 16u + (threadIdx.x >> 4), l16 = threadIdx.x & 15;
-    if (item >= (unsigned)rows * (unsigned)blocks) {     // whole groups of 16 lanes; then the fill of the scales' rows
-        return;
-    }
+    if (item >= (unsigned)rows * (unsigned)blocks) return;       // (whole groups of 16 lanes)
     const int row = (int)(item / (unsigned)blocks), b = (int)(item - (unsigned)row * (unsigned)blocks);
     const int col = b * 128 + (int)l16 * 8;
     const T* p = x + row * x_row + col;
@@ -76,6 +74,7 @@ fp8_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsi
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
     *reinterpret_cast<int2*>(q + (long)row * blocks * 128 + col) = make_int2(lo, hi);
     if (l16 == 0) scale[(long)b * pitch + row] = (unsigned char)s;
+    // (the fill of the scales' rows: at most 15, by the last row's lanes)
     if (row == rows - 1 && rows + (int)l16 < pitch) scale[(long)b * pitch + rows + l16] = 0;
 }
 

@@ -7,7 +7,8 @@ import torch
 
 from paper_2505_14741_amd import binding as B
 from test_block_edges_host import PRODUCTS
-from test_gpu_block_ops import DEV, NAN, U, check_cross, check_gnorm, cross_ref, fp8_ref, gen, randn
+from test_gpu_block_ops import (DEV, NAN, U, block_data, check_cross, check_gnorm, check_quantize, conditioned_block, cross_ref, fp8_ref, gen,
+                                randn)
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +183,100 @@ def test_cross_attention_of_the_largest_scale(dtype, nq, nk):
     q[..., 3] = 2.0 ** -60 * torch.randint(0, 2, (1, nq, 2), generator=g, device=DEV)
     k[..., 3] = 2.0 ** -67 * torch.randint(0, 4, (1, nk, 2), generator=g, device=DEV)
     check_cross(q.to(dtype), k.to(dtype), randn(g, 1, nk, 2, 64).to(dtype), 2.0 ** 127)
+
+
+# ------------------------------------------------------------------------------------------------- the largest sizes
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq", [1, 40])
+def test_cross_attention_over_the_most_keys(dtype, nq):
+    """2^24 keys of equal scores, values 0 and 1: every sum is a whole number up to 2^24, exact in fp32, so the result is their quotient, rounded;
+    with a length that ends inside a tile and garbage behind it."""
+    nk = 1 << 24
+    g = gen(32)
+    q, k = torch.zeros(1, nq, 1, 16, dtype=dtype, device=DEV), torch.ones(1, 1, 1, 16, dtype=dtype, device=DEV).expand(1, nk, 1, 16)
+    v = torch.randint(0, 2, (1, nk, 1, 16), generator=g, device=DEV, dtype=torch.int8).to(dtype)
+    for n in (nk, nk - 37):
+        v[:, n:] = NAN
+        out = B.cross_attn(q, k, v, 1.0, kv_lens=torch.tensor([n], dtype=torch.int32, device=DEV))
+        want = v[0, :n, 0].sum(0, dtype=torch.float64) / n
+        assert bool(((out[0, :, 0].double() - want).abs() <= (U[dtype] + 4 * 2.0 ** -24) * want).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_cross_attention_of_the_most_tokens(dtype):
+    g = gen(33)
+    q, k, v = torch.randn(1, 1 << 24, 1, 16, generator=g, device=DEV, dtype=dtype), randn(g, 1, 3, 1, 16).to(dtype), randn(g, 1, 3, 1, 16).to(dtype)
+    out = B.cross_attn(q, k, v, 0.25)
+    for at in (0, 1 << 23, (1 << 24) - 1000):
+        ref, tol = cross_ref(q[:, at:at + 1000], k, v, 0.25, torch.ones(1, 3, dtype=torch.bool, device=DEV))
+        assert bool(((out[:, at:at + 1000].double() - ref).abs() <= tol * 1.001).all())
+
+
+@pytest.mark.parametrize("use_workspace", [True, False])
+@pytest.mark.parametrize("rows,n_out", [(3, 5), (70, 300)])
+def test_products_of_the_most_columns(rows, n_out, use_workspace):
+    """k = 2^22, values -1, 0 and 1: whole sums, exact in fp32."""
+    k = 1 << 22
+    g = gen(34)
+    x, w = (torch.randint(-1, 2, (n, k), generator=g, device=DEV, dtype=torch.int8).float() for n in (rows, n_out))
+    out = B.dit_linear_fp8(*B.fp8_quantize(x), *B.fp8_quantize(w.bfloat16()), torch.zeros(n_out, device=DEV), use_workspace=use_workspace)
+    want = x.double() @ w.double().t().contiguous()
+    assert bool(((out.double() - want).abs() <= U[torch.bfloat16] * want.abs()).all())
+
+
+def test_products_of_the_most_rows():
+    """2^24 rows of one column against one, as the operand of many rows and as that of many columns."""
+    n = 1 << 24
+    g = gen(35)
+    x = torch.randint(-16, 17, (n, 1), generator=g, device=DEV).bfloat16()
+    q, s = B.fp8_quantize(x)
+    w = B.fp8_quantize(torch.full((1, 1), 3.0, device=DEV))
+    assert torch.equal(B.dit_linear_fp8(q, s, *w, torch.zeros(1, device=DEV)), 3.0 * x)
+    assert torch.equal(B.dit_linear_fp8(*w, q, s, torch.zeros(n, device=DEV)), (3.0 * x).t())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("batch,positions,groups", [(1, 1, 1), (2, 3, 32), (1, 50, 1), (1, 600, 65536), (1, 40, 16384)])
+def test_group_norm_of_the_most_channels(dtype, batch, positions, groups):
+    print(f"group_norm {dtype} {batch}x{positions}x65536/{groups}", flush=True)
+    g = gen(36)
+    x = (randn(g, batch, positions, 65536) * torch.exp(randn(g, 65536)) + randn(g, 65536)).to(dtype)
+    check_gnorm(x, groups, randn(g, 65536), randn(g, 65536), act=2)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("positions", [20, 5000])
+def test_group_norm_keeps_what_is_not_finite_in_its_group(dtype, positions):
+    g = gen(37)
+    x = randn(g, 2, positions, 96).to(dtype)
+    want = B.group_norm(x, 12)
+    for bad in (NAN, float("inf")):
+        y = x.clone()
+        y[1, positions - 1, 17] = bad                            # group 2 of the second sample
+        out = B.group_norm(y, 12)
+        spoilt = torch.zeros_like(out, dtype=torch.bool)
+        spoilt[1, :, 16:24] = True
+        assert bool(torch.isnan(out[spoilt]).all()) and torch.equal(out[~spoilt], want[~spoilt])
+
+
+# ------------------------------------------------------------------------------------------------- together
+def check_linear(x, w, bias):
+    """Quantization exact, the product within its bound (see test_product_of_blocks); the result."""
+    a, a_scale = check_quantize(x)
+    ref, off = fp8_ref(a, a_scale, *w, bias, 0)
+    out = B.dit_linear_fp8(a, a_scale, *w, bias)
+    assert bool(((out.double() - ref).abs() <= off + U[torch.bfloat16] * ref.abs() + 1e-30).all())
+    return out
+
+
+def test_a_conditioned_block_step_by_step():
+    """Each operator on what the one before it gave, within its own bound; the block in one go has the same bits."""
+    x, states, lens, p, _ = block_data(38)
+    Bn, N, D = x.shape
+    L, heads = states.shape[1], 5
+    h = check_gnorm(x, 32, p["gamma"], p["beta"], act=2)
+    q = check_linear(h.view(Bn * N, D), p["wq"], p["bq"]).view(Bn, N, heads, D // heads)
+    kv = check_linear(states.view(Bn * L, -1), p["wkv"], p["bkv"]).view(Bn, L, 2, heads, D // heads)
+    o = check_cross(q, kv[:, :, 0], kv[:, :, 1], 1.0 / math.sqrt(D // heads), kv_lens=lens)
+    y = x + check_linear(o.view(Bn * N, D), p["wo"], p["bo"]).view(Bn, N, D)
+    assert torch.equal(y, conditioned_block(x, states, lens, p, heads))
