@@ -280,3 +280,13 @@ def test_a_conditioned_block_step_by_step():
     o = check_cross(q, kv[:, :, 0], kv[:, :, 1], 1.0 / math.sqrt(D // heads), kv_lens=lens)
     y = x + check_linear(o.view(Bn * N, D), p["wo"], p["bo"]).view(Bn, N, D)
     assert torch.equal(y, conditioned_block(x, states, lens, p, heads))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nq,nk", SIZES)
+def test_cross_attention_of_the_smallest_scale(dtype, nq, nk):
+    """Below the normal range: the weights are equal; and with scores of 2^126, which such a scale leaves as small."""
+    g = gen(39)
+    q, k, v = randn(g, 1, nq, 2, 64), randn(g, 1, nk, 2, 64), randn(g, 1, nk, 2, 64).to(dtype)
+    for size in (1.0, 2.0 ** 59):
+        check_cross((q * size).to(dtype), (k * size).to(dtype), v, 2.0 ** -149)
