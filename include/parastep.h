@@ -35,7 +35,7 @@
  * with K % 64 == 0 and at least 64 outputs and fp32 with K % 32 == 0 (projections, outputs
  * a multiple of 4) and every attention shape (bf16 products at head_dim 64, fp32 otherwise);
  * every other accepted projection runs on a generic fp32-FMA kernel.
- * (The operators of a conditioned predictor block name their own limits.)
+ * (The operators of a conditioned predictor block and of self-attention on packed samples name their own limits.)
  */
 #ifndef PARASTEP_H
 #define PARASTEP_H
@@ -247,6 +247,89 @@ typedef struct {
 PS_API size_t group_norm_workspace_bytes(int batch, int positions, int channels, int groups, int dtype);
 PS_API int group_norm(const void* x, const float* gamma, const float* beta, void* out, const group_norm_shape* shape, void* workspace,
                size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------- operators of self-attention on packed samples
+ * What a predictor block runs whose samples differ in length (resolutions, frame counts, prompts) and lie behind each other along one token axis:
+ * projections in 4 bits, norms of queries and keys for each head with the rotation by their positions, and attention inside each sample
+ * (Section 1's 3D attention, where a batch is not a rectangle), also of the tokens that are appended to a sample whose keys are kept.
+ *
+ * 4-bit floating point with a power-of-two scale for each block of 32 columns of a row: x[r, c] = q[r, c] * 2^(s - 127) with
+ * s = scale[c / 32][r].
+ *   q      DEVICE e2m1 codes [rows][kp / 2] bytes, the even column in the low four bits, kp = cols rounded up to a multiple of 128,
+ *          filled up with zeros
+ *   scale  DEVICE e8m0 bytes [kp / 32][pitch], pitch = rows rounded up to a multiple of 16, filled up with 0
+ * fp4_quantize: x DEVICE [rows, cols] in `dtype`, rows x_row elements apart (>= cols; any alignment).  A block's scale is the
+ * least power of two >= 2^-127 under which its largest |x| is at most 6; values are rounded once, to nearest even (0 0.5 1 1.5 2 3 4 6).  A block
+ * with a value that is not finite has the scale 255, NaN, and zeros.
+ * fp4_dequantize: out DEVICE [rows, cols] in `dtype`, rows out_row elements apart (>= cols; any alignment): the values, exactly (beyond the
+ * type's largest number: that); NaN under the scale 255.
+ * q and scale 16-byte aligned; rows may be 0; cols <= 2^22, rows <= 2^24, fewer than 2^24 tiles of 16 x 512. */
+PS_API int fp4_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream);
+PS_API int fp4_dequantize(const void* q, const void* scale, void* out, int rows, int cols, int64_t out_row, int dtype, void* hip_stream);
+
+/* dit_linear_fp8 for operands in this format: out[m, n_out] = act(a * w^T + bias), the same arguments and limits.  Products and sums are as exact
+ * as in fp32; out bf16.  Summed whole, a row's result does not depend on the rows beside it; with the workspace, which shapes are summed in pieces
+ * of k depends on m. */
+PS_API size_t dit_linear_fp4_workspace_bytes(int m, int n_out, int k);
+PS_API int dit_linear_fp4(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m,
+                   int n_out, int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Rotary positions on several axes (frame, row, column, ...): table[t, p] = (cos, sin) of positions[t, axis of p] * theta[axis]^(-2 i / d),
+ * axis_dims[axis] = d values of a head turn with that axis, pair i of d / 2; pairs in the axes' order.  Angles in 64 bits.
+ *   positions  DEVICE fp32 [tokens][axes], rows position_row elements apart (0: one for all; fractions allowed)
+ *   axis_dims, theta  HOST [axes]; 1 <= axes <= 4, d even and >= 2, 256 in all at most, theta finite and > 0
+ *   table      DEVICE fp32 [tokens][rotated / 2][2], rotated the sum of axis_dims; 8-byte aligned.  tokens <= 2^24, may be 0. */
+PS_API int rope_table(const float* positions, int64_t position_row, int axes, const int* axis_dims, const double* theta, float* table, int tokens,
+               void* hip_stream);
+
+/* Queries and keys of a projection, normalised over each head and turned: out = rotate(norm(x) * gamma + beta),
+ *   norm 0: x (gamma and beta are not looked at);  1: x / sqrt(mean x^2 + eps);  2: (x - mean) / sqrt(mean (x - mean)^2 + eps);
+ *   pair p of the first `rotated` values of a head turns by table[token, p]: (c, e) -> (c cos - e sin, e cos + c sin), the values 2p and
+ *   2p + 1, or with halves = 1 the values p and p + rotated / 2; the others stay.
+ * q [batch, tokens, heads, head_dim] and k [batch, tokens, kv_heads, head_dim] DEVICE in `dtype`, elements of a head contiguous, every other stride free (elements,
+ * >= 0, those of an input may be 0; any alignment; ignored for an extent of 1).  Outputs may be their inputs (with equal strides), so that both turn where they lie in the
+ * projection; no other overlap.  kv_heads may be 0: then k, k_out and their norm are not looked at.  gamma, beta DEVICE fp32 [head_dim], each may be NULL (1, 0).
+ * table DEVICE fp32 [tokens][rotated / 2][2], table_batch floats from one sample's to the next (0: one for all); may be NULL iff rotated is 0.
+ * head_dim a multiple of 8, at most 256; rotated a multiple of 8 (halves: of 16), at most head_dim.  Statistics in fp32: the sum of a head's squares must be
+ * finite there.  batch and tokens may be 0; tokens <= 2^24, batch and heads <= 65535, at most 2^25 tokens in all. */
+typedef struct {
+    int batch, tokens, heads, kv_heads, head_dim, rotated, norm, halves, dtype;
+    float eps;
+    int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, q_out_batch, q_out_token, q_out_head, k_out_batch, k_out_token, k_out_head, table_batch;
+} qk_norm_rope_shape;
+PS_API int qk_norm_rope(const void* q, const void* k, const float* table, const float* gamma_q, const float* beta_q, const float* gamma_k,
+                 const float* beta_k, void* q_out, void* k_out, const qk_norm_rope_shape* shape, void* hip_stream);
+
+/* Attention inside samples that lie packed along one token axis.  Sample s has the query tokens q_offsets[s] .. q_offsets[s + 1] - 1 and the key tokens
+ * kv_offsets[s] .. kv_offsets[s + 1] - 1 (DEVICE int32 [samples + 1], rising; what is outside the axis is clamped; of offsets that fall results are
+ * unspecified, reads and writes stay inside the tensors).  With own_offsets = 0, kv_offsets is NULL, the keys' offsets are the queries' and
+ * kv_tokens = q_tokens.  A sample's nq queries are the last of its nk tokens: query t stands at i = nk - nq + t.  The first P =
+ * prefix_lens[s] tokens (DEVICE int32 [samples], clamped to 0 .. nk; NULL: 0) are the prefix, the others lie in frames of `frame` tokens, f(i) = floor((i - P) / frame).
+ *   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(x_ij - max),  over the keys j of the sample that i sees;
+ *   causal 0: all;  1: those of the prefix, and for i >= P those with f(j) <= f(i) (frame 1: j <= i)
+ *   x_ij = scale * q_i . k_j;  cap > 0: cap * tanh(x_ij / cap);  less slopes[head] * |f(i) - f(j)| where i, j >= P (slopes DEVICE fp32 [heads]; NULL: 0)
+ * A query that sees no key gets zeros.  What lies in k and v of other samples, and at keys that a query does not see, does not count for it, NaN and infinity included.
+ * Rows of o outside all samples stay as they were.
+ * q and o [q_tokens, heads, head_dim], k and v [kv_tokens, kv_heads, head_dim] DEVICE in `dtype`; kv_heads divides heads: query heads h * (heads / kv_heads) .. share key head h.
+ * head_dim in {16, 32, 64, 128}, its elements contiguous; token and head strides are free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0; of an
+ * extent of 1 they are ignored).  Pointers 16-byte aligned; o must not overlap the inputs, nor its heads each other.  samples, q_tokens and
+ * kv_tokens may be 0; samples and heads <= 65535, tokens <= 2^24, q_tokens * heads / kv_heads <= 2^30 and, divided by 128 (fp32: 64) plus samples, fewer than 2^24 /
+ * kv_heads.  frame >= 1; cap >= 0, and scale / cap must be finite.
+ * Finite in fp32 must be, with what a query sees: scale * log2(e) (refused else), q . k and that times scale * log2(e); cap and slope * distance, times log2(e);
+ * the largest |v| times the keys (in bf16 times 2^8 more).  bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32; fp32:
+ * everything in fp32.  A sample's result does not depend on the others.
+ * workspace: DEVICE, 256-byte aligned, >= packed_attn_workspace_bytes(...) (may be NULL when that is 0): few queries' keys are divided among workgroups, and
+ * their partial sums pass through it. */
+typedef struct {
+    int samples, q_tokens, kv_tokens, heads, kv_heads, head_dim, dtype;
+    int own_offsets;                             /* 1: the keys have offsets of their own */
+    int causal, frame;
+    float scale, cap;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
+} packed_attn_shape;
+PS_API size_t packed_attn_workspace_bytes(const packed_attn_shape* shape);
+PS_API int packed_attn(const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* prefix_lens,
+                const float* slopes, void* o, const packed_attn_shape* shape, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------- scheduler and metric
  * Fused DDIM update  x_out = a*x + b*eps  (the element-wise Scheduler of the paper's

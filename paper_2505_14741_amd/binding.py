@@ -56,6 +56,16 @@ class _GroupNormShape(C.Structure):
         (n, C.c_int64) for n in ("x_batch", "x_position", "out_batch", "out_position")]
 
 
+class _QkNormShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("batch", "tokens", "heads", "kv_heads", "head_dim", "rotated", "norm", "halves", "dtype")] + [("eps", C.c_float)] + [
+        (f"{t}_{n}", C.c_int64) for t in ("q", "k", "q_out", "k_out") for n in ("batch", "token", "head")] + [("table_batch", C.c_int64)]
+
+
+class _PackedShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("samples", "q_tokens", "kv_tokens", "heads", "kv_heads", "head_dim", "dtype", "own_offsets", "causal", "frame")] + [
+        ("scale", C.c_float), ("cap", C.c_float)] + [(f"{t}_{n}", C.c_int64) for t in "qkvo" for n in ("token", "head")]
+
+
 class SamplerState(C.Structure):
     """Host part of a run's state between two steps (`sampler_state`); plain data, may be stored."""
     _fields_ = [("step", C.c_int32), ("cycle", C.c_int32), ("round", C.c_int32), ("toggle", C.c_int32),
@@ -94,6 +104,14 @@ def lib():
         "dit_linear_fp8": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
         "group_norm_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
         "group_norm": (i32, [vp, vp, vp, vp, C.POINTER(_GroupNormShape), vp, sz, vp]),
+        "fp4_quantize": (i32, [vp, vp, vp, i32, i32, C.c_int64, i32, vp]),
+        "fp4_dequantize": (i32, [vp, vp, vp, i32, i32, C.c_int64, i32, vp]),
+        "dit_linear_fp4_workspace_bytes": (sz, [i32, i32, i32]),
+        "dit_linear_fp4": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
+        "rope_table": (i32, [vp, C.c_int64, i32, C.POINTER(i32), C.POINTER(C.c_double), vp, i32, vp]),
+        "qk_norm_rope": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, C.POINTER(_QkNormShape), vp]),
+        "packed_attn_workspace_bytes": (sz, [C.POINTER(_PackedShape)]),
+        "packed_attn": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, C.POINTER(_PackedShape), vp, sz, vp]),
         "sampler_step_workspace_bytes": (sz, [sz]),
         "sampler_step": (i32, [vp, vp, vp, vp, C.c_double, C.c_double, sz, vp, vp, sz, vp]),
         "sampler_step_noalloc": (i32, [vp, vp, vp, vp, C.c_double, C.c_double, sz, vp, vp]),
@@ -124,7 +142,8 @@ EXPORTED = ("ps_strerror", "ps_mfma_probe", "dit_set_kernel_path", "dit_get_kern
             "rel_mae_workspace_bytes", "rel_mae", "ddim_coefficients", "euler_discrete_coefficients",
             "flow_euler_coefficients", "sampler_workspace_bytes", "sampler_run", "sampler_state_bytes",
             "sampler_run_steps", "cross_attn_workspace_bytes", "cross_attn", "fp8_quantize", "dit_linear_fp8_workspace_bytes",
-            "dit_linear_fp8", "group_norm_workspace_bytes", "group_norm")
+            "dit_linear_fp8", "group_norm_workspace_bytes", "group_norm", "fp4_quantize", "fp4_dequantize", "dit_linear_fp4_workspace_bytes",
+            "dit_linear_fp4", "rope_table", "qk_norm_rope", "packed_attn_workspace_bytes", "packed_attn")
 
 
 def _check(status: int, where: str):
@@ -421,6 +440,202 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
     _need_here("group_norm", x, out, gamma, beta)
     ws = _workspace(n, x.device)
     _check(lib().group_norm(x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), shape, _ptr(ws), n, _stream()), "group_norm")
+    return out
+
+
+# ------------------------------------- operators of self-attention on packed samples
+def fp4_quantize(x: torch.Tensor):
+    """x [rows, cols], float32 or bfloat16, rows any distance apart -> (q uint8 [rows, kp / 2], two e2m1 codes to a byte, scale float8_e8m0fnu
+    [kp / 32, pitch]): kp is cols rounded up to 128, pitch is rows rounded up to 16, both filled up as include/parastep.h says."""
+    w = "fp4_quantize"
+    _need(x.dim() == 2 and x.shape[1] >= 1, w, "x must be [rows, cols]")
+    dt = _CODE.get(x.dtype)
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    rows, cols = x.shape
+    _need_extents(w, rows, cols)
+    _need(x.stride(1) == 1 or cols == 1, w, "the elements of a row must be contiguous")
+    _need_here(w, x)
+    kp = (cols + 127) // 128 * 128
+    q = torch.empty((rows, kp // 2), dtype=torch.uint8, device=x.device)
+    scale = torch.empty((kp // 32, (rows + 15) // 16 * 16), dtype=torch.float8_e8m0fnu, device=x.device)
+    _check(lib().fp4_quantize(x.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, x.stride(0), dt, _stream()), w)
+    return q, scale
+
+
+def fp4_dequantize(q: torch.Tensor, scale: torch.Tensor, cols: Optional[int] = None, dtype: torch.dtype = torch.bfloat16,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values [rows, cols] of fp4_quantize's result (cols: all kp), float32 or bfloat16; NaN where a block was not finite."""
+    w = "fp4_dequantize"
+    _need(q.dim() == 2 and q.shape[1] % 64 == 0 and q.shape[1] > 0, w, "q must be [rows, kp / 2], kp a multiple of 128")
+    _need(q.dtype == torch.uint8 and scale.dtype == torch.float8_e8m0fnu, w, "codes in uint8, scales in float8_e8m0fnu", PS_ERR_DTYPE)
+    rows, kp = q.shape[0], 2 * q.shape[1]
+    cols = kp if cols is None else int(cols)
+    _need_extents(w, rows, kp)
+    _need(kp - 128 < cols <= kp, w, "cols must be what kp is rounded up from")
+    _need(scale.shape == (kp // 32, (rows + 15) // 16 * 16), w, "scale must be [kp / 32, rows rounded up to 16]")
+    _need(q.is_contiguous() and scale.is_contiguous(), w, "q and scale must be contiguous")
+    if out is None:
+        _need(dtype in _CODE, w, "float32 or bfloat16", PS_ERR_DTYPE)
+        out = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    dt = _CODE.get(out.dtype)
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    _need(out.shape == (rows, cols) and (out.stride(1) == 1 or cols == 1), w, "out must be [rows, cols], rows contiguous")
+    _need_here(w, q, scale, out)
+    _check(lib().fp4_dequantize(q.data_ptr(), scale.data_ptr(), out.data_ptr(), rows, cols, out.stride(0), dt, _stream()), w)
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _fp4_plan(dtypes, a, a_scale, w, w_scale, bias, out, use_workspace, device):
+    f = "dit_linear_fp4"
+    _need(len(a) == 2 and len(w) == 2 and a[1] == w[1] and a[1] % 64 == 0 and a[1] > 0, f, "a [M, kp / 2] and w [n_out, kp / 2], kp a multiple of 128")
+    M, K = a[0], 2 * a[1]
+    Nn = w[0]
+    _need_extents(f, M, K, Nn)
+    _need(dtypes[:4] == (torch.uint8, torch.float8_e8m0fnu, torch.uint8, torch.float8_e8m0fnu), f, "codes in uint8, scales in float8_e8m0fnu", PS_ERR_DTYPE)
+    _need(dtypes[4] == torch.float32, f, "bias must be float32", PS_ERR_DTYPE)
+    _need(a_scale == (K // 32, (M + 15) // 16 * 16) and w_scale == (K // 32, (Nn + 15) // 16 * 16), f, "scales [kp / 32, rows rounded up to 16]")
+    _need(bias == (Nn,), f, "bias must be [n_out]")
+    _need(out == (M, Nn), f, "out must be [M, n_out]")
+    _need(dtypes[5] == torch.bfloat16, f, "out must be bfloat16", PS_ERR_DTYPE)
+    return M, Nn, K, lib().dit_linear_fp4_workspace_bytes(M, Nn, K) if use_workspace else 0
+
+
+def dit_linear_fp4(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor, act: int = 0,
+                   out: Optional[torch.Tensor] = None, use_workspace: bool = True) -> torch.Tensor:
+    """act(a w^T + bias) of operands from fp4_quantize: a of [M, K] and w of [n_out, K]; bias float32 [n_out], out bfloat16."""
+    f = "dit_linear_fp4"
+    _need(0 <= act <= 1, f, "act 0 or 1")
+    if out is None:
+        _need(a.dim() == 2 and w.dim() == 2, f, "a [M, kp / 2] and w [n_out, kp / 2]")
+        out = torch.empty((a.shape[0], w.shape[0]), dtype=torch.bfloat16, device=a.device)
+    M, Nn, K, nb = _fp4_plan((a.dtype, a_scale.dtype, w.dtype, w_scale.dtype, bias.dtype, out.dtype), a.shape, a_scale.shape, w.shape, w_scale.shape,
+                             bias.shape, out.shape, use_workspace, a.get_device())
+    _need(a.is_contiguous() and a_scale.is_contiguous() and w.is_contiguous() and w_scale.is_contiguous() and bias.is_contiguous() and
+          out.is_contiguous(), f, "operands must be contiguous")
+    _need_here(f, a, a_scale, w, w_scale, bias, out)
+    ws = _workspace(nb, a.device)
+    _check(lib().dit_linear_fp4(a.data_ptr(), a_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), bias.data_ptr(), out.data_ptr(), M, Nn, K, int(act),
+                                _ptr(ws), nb, _stream()), f)
+    return out
+
+
+def rope_table(positions: torch.Tensor, axis_dims: Sequence[int], theta=10000.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """positions float32 [tokens, axes] -> float32 [tokens, sum(axis_dims) / 2, 2] of (cos, sin); theta one number, or one for each axis."""
+    w = "rope_table"
+    n = len(axis_dims)
+    _need(positions.dim() == 2 and 1 <= n <= 4 and positions.shape[1] == n, w, "positions must be [tokens, axes], 1 to 4 axes of axis_dims")
+    _need(positions.dtype == torch.float32, w, "positions must be float32", PS_ERR_DTYPE)
+    thetas = [float(t) for t in theta] if isinstance(theta, (list, tuple)) else [float(theta)] * n
+    _need(len(thetas) == n, w, "theta must be one number, or one for each axis")
+    dims = [int(d) for d in axis_dims]
+    _need(all(0 < d <= 256 and d % 2 == 0 for d in dims), w, "axis_dims must be even, 256 in all at most")
+    _need_extents(w, positions.shape[0])
+    _need(n == 1 or positions.stride(1) == 1 or positions.shape[0] == 0, w, "a token's positions must be contiguous")
+    shape = (positions.shape[0], sum(dims) // 2, 2)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=positions.device)
+    _need(out.dtype == torch.float32, w, "out must be float32", PS_ERR_DTYPE)
+    _need(out.shape == shape and out.is_contiguous(), w, "out must be [tokens, sum(axis_dims) / 2, 2], contiguous")
+    _need_here(w, positions, out)
+    _check(lib().rope_table(positions.data_ptr(), positions.stride(0), n, (C.c_int * n)(*dims), (C.c_double * n)(*thetas), out.data_ptr(), shape[0], _stream()), w)
+    return out
+
+
+def _like(t: Optional[torch.Tensor]):
+    return None if t is None else (t.dtype, t.shape, t.stride())
+
+
+@functools.lru_cache(maxsize=1024)
+def _qk_plan(q, k, qo, ko, table, affine, norm, eps, halves, device):
+    w = "qk_norm_rope"
+    _need(len(q[1]) == 4, w, "q must be [B, N, H, d]")
+    B, N, H, d = q[1]
+    dt = _CODE.get(q[0])
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    _need((k is None) == (ko is None), w, "k_out goes with k")
+    _need(k is None or (len(k[1]) == 4 and k[1][:2] == (B, N) and k[1][3] == d and k[1][2] >= 1), w, "k must be [B, N, Hkv, d]")
+    _need(qo[1] == q[1] and (k is None or ko[1] == k[1]), w, "outputs must have their inputs' shapes")
+    for t in (k, qo, ko):
+        _need(t is None or t[0] == q[0], w, "one type for all", PS_ERR_DTYPE)
+    for t in (q, k, qo, ko):
+        _need(t is None or t[2][3] == 1, w, "the elements of a head must be contiguous")
+    _need(0 <= norm <= 2, w, "norm 0, 1 or 2")
+    _need_extents(w, B, N, H, d, k[1][2] if k else 0)
+    for t in affine:
+        _need(t is None or t[0] == torch.float32, w, "gamma and beta must be float32", PS_ERR_DTYPE)
+        _need(t is None or (t[1] == (d,) and t[2] == (1,)), w, "gamma and beta must be [d], contiguous")
+    rotated = table_batch = 0
+    if table is not None:
+        _need(table[0] == torch.float32, w, "table must be float32", PS_ERR_DTYPE)
+        shape, stride = (table[1], table[2]) if len(table[1]) == 4 else ((B,) + tuple(table[1]), (0,) + tuple(table[2]))
+        _need(len(shape) == 4 and shape[0] == B and shape[1] == N and shape[3] == 2 and 1 <= shape[2] <= 128, w, "table must be [N, pairs, 2] or [B, N, pairs, 2]")
+        rotated, table_batch = 2 * shape[2], stride[0] if B > 1 else 0
+        _need(stride[3] == 1 and (shape[2] == 1 or stride[2] == 2) and (N <= 1 or stride[1] == rotated), w, "a sample's table must be contiguous")
+    none = (None, (0, 0, 0), (0, 0, 0))
+    kk, oo = k or none, ko or none
+    s = _QkNormShape(B, N, H, k[1][2] if k else 0, d, rotated, norm, int(halves), dt, eps, *q[2][:3], *kk[2][:3], *qo[2][:3], *oo[2][:3], table_batch)
+    return C.byref(s)
+
+
+def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: Optional[torch.Tensor], gamma_q: Optional[torch.Tensor] = None,
+                 gamma_k: Optional[torch.Tensor] = None, beta_q: Optional[torch.Tensor] = None, beta_k: Optional[torch.Tensor] = None, norm: int = 1,
+                 eps: float = 1e-6, halves: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """q [B, N, H, d] and k [B, N, Hkv, d] (or None), elements of a head contiguous, normalised over each head (norm 0 none, 1 by the root of the mean
+    square, 2 by mean and deviation; gamma, beta float32 [d]) and turned by table, [N, pairs, 2] or [B, N, pairs, 2] from rope_table (None: not
+    turned): neighbouring values, or with halves the first pairs values with the next.  Returns (q_out, k_out), which may be q and k."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    shape = _qk_plan(_like(q), _like(k), _like(q_out), _like(k_out), _like(table), (_like(gamma_q), _like(beta_q), _like(gamma_k), _like(beta_k)),
+                     int(norm), float(eps), bool(halves), q.get_device())
+    _need_here("qk_norm_rope", q, k, q_out, k_out, table, gamma_q, gamma_k, beta_q, beta_k)
+    _check(lib().qk_norm_rope(q.data_ptr(), _ptr(k), _ptr(table), _ptr(gamma_q), _ptr(beta_q), _ptr(gamma_k), _ptr(beta_k), q_out.data_ptr(), _ptr(k_out),
+                              shape, _stream()), "qk_norm_rope")
+    return q_out, k_out
+
+
+@functools.lru_cache(maxsize=1024)
+def _packed_plan(q, k, v, o, q_offsets, kv_offsets, prefix_lens, slopes, scale, frame, causal, cap, device):
+    w = "packed_attn"
+    _need(len(q[1]) == 3 and len(k[1]) == 3 and v[1] == k[1], w, "q [Tq, H, d], k and v [Tk, Hkv, d]")
+    T, H, d = q[1]
+    _need(k[1][2] == d, w, "k and v must have q's head_dim")
+    dt = _CODE.get(q[0])
+    _need(dt is not None and k[0] == q[0] and v[0] == q[0], w, "float32 or bfloat16, the same for q, k and v", PS_ERR_DTYPE)
+    _need(o[1] == q[1], w, "out must have q's shape")
+    _need(o[0] == q[0], w, "out must have q's type", PS_ERR_DTYPE)
+    _need(q[2][2] == k[2][2] == v[2][2] == o[2][2] == 1, w, "the elements of a head must be contiguous")
+    _need(len(q_offsets[1]) == 1 and q_offsets[1][0] >= 1, w, "q_offsets must be [samples + 1]")
+    n = q_offsets[1][0] - 1
+    _need_extents(w, T, H, d, *k[1], n, frame)
+    for t, m in ((q_offsets, n + 1), (kv_offsets, n + 1), (prefix_lens, n)):
+        _need(t is None or t[0] == torch.int32, w, "offsets and prefix_lens must be int32", PS_ERR_DTYPE)
+        _need(t is None or (t[1] == (m,) and (m <= 1 or t[2] == (1,))), w, "kv_offsets must be [samples + 1] and prefix_lens [samples], contiguous")
+    _need(slopes is None or slopes[0] == torch.float32, w, "slopes must be float32", PS_ERR_DTYPE)
+    _need(slopes is None or (slopes[1] == (H,) and (H == 1 or slopes[2] == (1,))), w, "slopes must be [H], contiguous")
+    _need(kv_offsets is not None or k[1][0] == T, w, "without kv_offsets, keys must be as many as queries")
+    s = _PackedShape(n, T, k[1][0], H, k[1][1], d, dt, int(kv_offsets is not None), int(causal), frame, scale, cap, *q[2][:2], *k[2][:2], *v[2][:2], *o[2][:2])
+    return C.byref(s), lib().packed_attn_workspace_bytes(C.byref(s))
+
+
+def packed_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, q_offsets: torch.Tensor, kv_offsets: Optional[torch.Tensor] = None,
+                prefix_lens: Optional[torch.Tensor] = None, frame: int = 1, causal: bool = False, cap: float = 0.0,
+                slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [Tq, H, d]; k, v [Tk, Hkv, d], any strides whose elements of a head are contiguous; sample s has the queries q_offsets[s] .. q_offsets[s + 1] - 1
+    (int32 [samples + 1]) and the keys of kv_offsets (None: the queries'), its queries being its last tokens.  Behind the sample's first prefix_lens[s]
+    tokens (int32 [samples]) tokens lie in frames of `frame`; causal: a query sees the prefix and the frames up to its own; slopes (float32 [H]):
+    scores less slope * distance in frames; cap: scores capped by cap * tanh(score / cap).  A query that sees no key gets zeros; rows of out
+    outside all samples are not written."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape, n = _packed_plan(_like(q), _like(k), _like(v), _like(out), _like(q_offsets), _like(kv_offsets), _like(prefix_lens), _like(slopes), float(scale),
+                            int(frame), bool(causal), float(cap), q.get_device())
+    _need_here("packed_attn", q, k, v, out, q_offsets, kv_offsets, prefix_lens, slopes)
+    ws = _workspace(n, q.device)
+    _check(lib().packed_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_offsets.data_ptr(), _ptr(kv_offsets), _ptr(prefix_lens), _ptr(slopes),
+                             out.data_ptr(), shape, _ptr(ws), n, _stream()), "packed_attn")
     return out
 
 

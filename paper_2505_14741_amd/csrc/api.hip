@@ -8,8 +8,11 @@
 
 #include "common.h"
 #include "cross_attention.h"
+#include "fp4.h"
 #include "fp8.h"
 #include "group_norm.h"
+#include "packed_attention.h"
+#include "qk_norm.h"
 #include "plan.h"
 #include "slim.h"
 
@@ -577,13 +580,11 @@ int fp8_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_
                ? PS_OK : PS_ERR_HIP;
 }
 
-size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k) {
-    if (m < 1 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22)) return 0;
-    return align256(fp8_product_workspace_bytes(m, n_out, (k + 127) / 128));
-}
+namespace {
 
-int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out,
-                   int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream) {
+// PS_OK and the launcher's arguments of a product of operands with block scales, or why not
+int scaled_product_args(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out, int k,
+                        int act, void* workspace, size_t workspace_bytes, ScaledProduct& g) {
     if (m < 0 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22) || (act != 0 && act != 1)) return PS_ERR_SHAPE;
     if (((m + 63L) / 64) * ((n_out + 63L) / 64) >= (1L << 24)) return PS_ERR_SHAPE;  // (the same)
     if (m == 0) return PS_OK;
@@ -592,12 +593,26 @@ int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void
         out == a || out == w)
         return PS_ERR_SHAPE;
     if (workspace && !aligned(workspace, 256)) return PS_ERR_WORKSPACE;
-    Fp8Product g{};
     g.a = a; g.w = w; g.a_scale = a_scale; g.w_scale = w_scale; g.bias = bias; g.out = (bf16_t*)out;
     g.m = m; g.n_out = n_out; g.blocks = (k + 127) / 128; g.act = act;
     g.a_pitch = (m + 15) / 16 * 16; g.w_pitch = (n_out + 15) / 16 * 16;
     g.ws = (float*)workspace;
     g.ws_bytes = workspace ? workspace_bytes : 0;
+    return PS_OK;
+}
+
+}  // namespace
+
+size_t dit_linear_fp8_workspace_bytes(int m, int n_out, int k) {
+    if (m < 1 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22)) return 0;
+    return align256(fp8_product_workspace_bytes(m, n_out, (k + 127) / 128));
+}
+
+int dit_linear_fp8(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out,
+                   int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    ScaledProduct g{};
+    const int rc = scaled_product_args(a, a_scale, w, w_scale, bias, out, m, n_out, k, act, workspace, workspace_bytes, g);
+    if (rc != PS_OK || m == 0) return rc;
     return launch_fp8_product(g, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
 }
 
@@ -631,6 +646,162 @@ int group_norm(const void* x, const float* gamma, const float* beta, void* out, 
     a.x_batch = (long)s->x_batch; a.x_position = (long)s->x_position; a.o_batch = (long)s->out_batch; a.o_position = (long)s->out_position;
     a.part = (float2*)workspace;
     return launch_group_norm(s->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+int fp4_quantize(const void* x, void* q, void* scale, int rows, int cols, int64_t x_row, int dtype, void* hip_stream) {
+    if (dtype != PS_F32 && dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (rows < 0 || cols < 1 || rows > (1 << 24) || cols > (1 << 22)) return PS_ERR_SHAPE;
+    if (rows == 0) return PS_OK;
+    if (!grid_fits(fp4_workgroups(rows, cols), 256)) return PS_ERR_SHAPE;
+    if (rows > 1 && (x_row < cols || x_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    if (!x || !q || !scale) return PS_ERR_NULL;
+    if (!aligned(x, dtype == PS_BF16 ? 2 : 4) || !aligned(q, 16) || !aligned(scale, 16) || q == x || scale == x || q == scale) return PS_ERR_SHAPE;
+    return launch_fp4_quantize(dtype, x, q, scale, rows, cols, rows > 1 ? (long)x_row : cols, (hipStream_t)hip_stream) == hipSuccess
+               ? PS_OK : PS_ERR_HIP;
+}
+
+int fp4_dequantize(const void* q, const void* scale, void* out, int rows, int cols, int64_t out_row, int dtype, void* hip_stream) {
+    if (dtype != PS_F32 && dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (rows < 0 || cols < 1 || rows > (1 << 24) || cols > (1 << 22)) return PS_ERR_SHAPE;
+    if (rows == 0) return PS_OK;
+    if (!grid_fits(fp4_workgroups(rows, cols), 256)) return PS_ERR_SHAPE;
+    if (rows > 1 && (out_row < cols || out_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    if (!q || !scale || !out) return PS_ERR_NULL;
+    if (!aligned(out, dtype == PS_BF16 ? 2 : 4) || !aligned(q, 16) || !aligned(scale, 16) || out == q || out == scale) return PS_ERR_SHAPE;
+    return launch_fp4_dequantize(dtype, q, scale, out, rows, cols, rows > 1 ? (long)out_row : cols, (hipStream_t)hip_stream) == hipSuccess
+               ? PS_OK : PS_ERR_HIP;
+}
+
+size_t dit_linear_fp4_workspace_bytes(int m, int n_out, int k) {
+    if (m < 1 || n_out < 1 || k < 1 || m > (1 << 24) || n_out > (1 << 24) || k > (1 << 22)) return 0;
+    return align256(fp4_product_workspace_bytes(m, n_out, (k + 127) / 128));
+}
+
+int dit_linear_fp4(const void* a, const void* a_scale, const void* w, const void* w_scale, const float* bias, void* out, int m, int n_out,
+                   int k, int act, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    ScaledProduct g{};
+    const int rc = scaled_product_args(a, a_scale, w, w_scale, bias, out, m, n_out, k, act, workspace, workspace_bytes, g);
+    if (rc != PS_OK || m == 0) return rc;
+    return launch_fp4_product(g, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+int rope_table(const float* positions, int64_t position_row, int axes, const int* axis_dims, const double* theta, float* table, int tokens,
+               void* hip_stream) {
+    if (axes < 1 || axes > ROPE_MAX_AXES || tokens < 0 || tokens > (1 << 24)) return PS_ERR_SHAPE;
+    if (!axis_dims || !theta) return PS_ERR_NULL;
+    RopeAxes r;
+    r.pairs = 0;
+    for (int a = 0; a < axes; ++a) {
+        if (axis_dims[a] < 2 || axis_dims[a] % 2 || axis_dims[a] / 2 > ROPE_MAX_PAIRS - r.pairs || !(theta[a] > 0) || !std::isfinite(theta[a])) return PS_ERR_SHAPE;
+        for (int i = 0; i < axis_dims[a] / 2; ++i) {
+            r.axis[r.pairs] = (unsigned char)a;
+            r.freq[r.pairs++] = std::pow(theta[a], -2.0 * i / axis_dims[a]);
+        }
+    }
+    if (tokens > 1 && (position_row < 0 || position_row > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    if (tokens == 0) return PS_OK;
+    if (!positions || !table) return PS_ERR_NULL;
+    if (!aligned(positions, 4) || !aligned(table, 8) || (const float*)table == positions) return PS_ERR_SHAPE;
+    return launch_rope_table(positions, tokens > 1 ? (long)position_row : 0, r, table, tokens, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+namespace {
+
+// one side of qk_norm_rope: strides of any alignment, an output that does not overlap itself and is its input only where it lies alike
+bool qk_side_ok(const qk_norm_rope_shape* s, const QkSide& q) {
+    const long n[3] = {s->batch, s->tokens, q.heads}, x[3] = {q.x_batch, q.x_tok, q.x_head}, o[3] = {q.o_batch, q.o_tok, q.o_head};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (x[i] < 0 || x[i] > (1L << 40) || o[i] < 0 || o[i] > (1L << 40) || (q.x == q.out && q.x && x[i] != o[i]))) return false;
+    return !pieces_meet(o[0], n[0], o[1], n[1], s->head_dim) && !pieces_meet(o[0], n[0], o[2], n[2], s->head_dim) &&
+           !pieces_meet(o[1], n[1], o[2], n[2], s->head_dim);
+}
+
+}  // namespace
+
+int qk_norm_rope(const void* q, const void* k, const float* table, const float* gamma_q, const float* beta_q, const float* gamma_k,
+                 const float* beta_k, void* q_out, void* k_out, const qk_norm_rope_shape* s, void* hip_stream) {
+    if (!s) return PS_ERR_NULL;
+    if (s->dtype != PS_F32 && s->dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (s->batch < 0 || s->tokens < 0 || s->heads < 1 || s->kv_heads < 0 || s->batch > 65535 || s->tokens > (1 << 24) || s->heads > 65535 || s->kv_heads > 65535 ||
+        (long)s->batch * s->tokens > (1L << 25))
+        return PS_ERR_SHAPE;
+    if (s->head_dim < 8 || s->head_dim % 8 || s->head_dim > 256 || s->norm < 0 || s->norm > 2 || s->halves < 0 || s->halves > 1) return PS_ERR_SHAPE;
+    if (s->rotated < 0 || s->rotated > s->head_dim || s->rotated % (s->halves ? 16 : 8)) return PS_ERR_SHAPE;
+    if (s->norm && (!(s->eps >= 0.f) || !std::isfinite(s->eps))) return PS_ERR_SHAPE;
+    if (s->batch > 1 && (s->table_batch < 0 || s->table_batch > ((int64_t)1 << 40))) return PS_ERR_SHAPE;
+    QkNormArgs a{};
+    a.side[0] = QkSide{q, q_out, gamma_q, beta_q, s->heads, (long)s->q_batch, (long)s->q_token, (long)s->q_head, (long)s->q_out_batch, (long)s->q_out_token,
+                       (long)s->q_out_head};
+    a.side[1] = QkSide{k, k_out, gamma_k, beta_k, s->kv_heads, (long)s->k_batch, (long)s->k_token, (long)s->k_head, (long)s->k_out_batch, (long)s->k_out_token,
+                       (long)s->k_out_head};
+    if (!qk_side_ok(s, a.side[0]) || (s->kv_heads && !qk_side_ok(s, a.side[1]))) return PS_ERR_SHAPE;
+    if (s->batch == 0 || s->tokens == 0) return PS_OK;
+    if (!q || !q_out || (s->kv_heads && (!k || !k_out)) || (s->rotated && !table)) return PS_ERR_NULL;
+    const size_t es = s->dtype == PS_BF16 ? 2 : 4;
+    if (!aligned(q, es) || !aligned(q_out, es) || !aligned(table, 4) || !aligned(gamma_q, 4) || !aligned(beta_q, 4)) return PS_ERR_SHAPE;
+    if (s->kv_heads && (!aligned(k, es) || !aligned(k_out, es) || !aligned(gamma_k, 4) || !aligned(beta_k, 4) || q_out == k || k_out == q || q_out == k_out))
+        return PS_ERR_SHAPE;
+    a.table = table;
+    a.table_batch = s->batch > 1 ? (long)s->table_batch : 0;
+    a.batch = s->batch; a.tokens = s->tokens; a.head_dim = s->head_dim; a.pairs = s->rotated / 2; a.norm = s->norm; a.halves = s->halves && s->rotated; a.eps = s->eps;
+    return launch_qk_norm_rope(s->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
+}
+
+namespace {
+
+// PS_OK and the launcher's arguments (kv_offsets: whether there are any), or why not
+int packed_args(const packed_attn_shape* s, PackedArgs& a) {
+    if (!s) return PS_ERR_NULL;
+    if (s->dtype != PS_F32 && s->dtype != PS_BF16) return PS_ERR_DTYPE;
+    if (s->head_dim != 16 && s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return PS_ERR_SHAPE;
+    if (s->samples < 0 || s->q_tokens < 0 || s->kv_tokens < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads) return PS_ERR_SHAPE;
+    if (s->samples > 65535 || s->heads > 65535 || s->q_tokens > (1 << 24) || s->kv_tokens > (1 << 24)) return PS_ERR_SHAPE;
+    if (s->own_offsets < 0 || s->own_offsets > 1 || (!s->own_offsets && s->kv_tokens != s->q_tokens)) return PS_ERR_SHAPE;
+    if (s->causal < 0 || s->causal > 1 || s->frame < 1) return PS_ERR_SHAPE;
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale * PACKED_LOG2E)) return PS_ERR_SHAPE;
+    if (!(s->cap >= 0.f) || !std::isfinite(s->cap * PACKED_LOG2E) || (s->cap > 0.f && !std::isfinite(2.0f * (s->scale * PACKED_LOG2E) / s->cap))) return PS_ERR_SHAPE;
+    const int es = s->dtype == PS_BF16 ? 2 : 4;
+    if (!strides_ok(1, s->q_tokens, s->heads, 0, s->q_token, s->q_head, es) || !strides_ok(1, s->kv_tokens, s->kv_heads, 0, s->k_token, s->k_head, es) ||
+        !strides_ok(1, s->kv_tokens, s->kv_heads, 0, s->v_token, s->v_head, es) || !strides_ok(1, s->q_tokens, s->heads, 0, s->o_token, s->o_head, es))
+        return PS_ERR_SHAPE;
+    if (pieces_meet(s->o_token, s->q_tokens, s->o_head, s->heads, s->head_dim)) return PS_ERR_SHAPE;
+    const int share = s->heads / s->kv_heads;
+    if ((long)s->q_tokens * share > (1L << 30)) return PS_ERR_SHAPE;
+    if (!grid_fits((long)packed_slots(s->q_tokens, share, s->samples, s->dtype == PS_BF16 ? 128 : 64) * s->kv_heads, 256)) return PS_ERR_SHAPE;
+    a = PackedArgs{};
+    a.samples = s->samples; a.q_tokens = s->q_tokens; a.kv_tokens = s->kv_tokens; a.kv_heads = s->kv_heads; a.share = share; a.head_dim = s->head_dim;
+    a.frame = s->frame; a.causal = s->causal; a.scale = s->scale; a.cap = s->cap;
+    a.q_tok = (long)s->q_token; a.q_head = (long)s->q_head; a.k_tok = (long)s->k_token; a.k_head = (long)s->k_head;
+    a.v_tok = (long)s->v_token; a.v_head = (long)s->v_head; a.o_tok = (long)s->o_token; a.o_head = (long)s->o_head;
+    a.own_offsets = s->own_offsets != 0;
+    return PS_OK;
+}
+
+}  // namespace
+
+size_t packed_attn_workspace_bytes(const packed_attn_shape* shape) {
+    PackedArgs a;
+    if (packed_args(shape, a) != PS_OK || a.samples == 0 || a.q_tokens == 0) return 0;
+    return align256(packed_workspace_bytes(shape->dtype, a));
+}
+
+int packed_attn(const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* prefix_lens,
+                const float* slopes, void* o, const packed_attn_shape* shape, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    PackedArgs a;
+    const int rc = packed_args(shape, a);
+    if (rc != PS_OK) return rc;
+    if (a.samples == 0 || a.q_tokens == 0) return PS_OK;
+    if (!q || !o || !q_offsets || (a.kv_tokens > 0 && (!k || !v)) || (a.own_offsets && !kv_offsets)) return PS_ERR_NULL;
+    if (!a.own_offsets && kv_offsets) return PS_ERR_SHAPE;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(q_offsets, 4) || !aligned(kv_offsets, 4) ||
+        !aligned(prefix_lens, 4) || !aligned(slopes, 4) || o == q || o == k || o == v)
+        return PS_ERR_SHAPE;
+    const size_t need = packed_attn_workspace_bytes(shape);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PS_ERR_WORKSPACE;
+    a.q = q; a.k = k; a.v = v; a.o = o;
+    a.q_offsets = q_offsets; a.kv_offsets = kv_offsets; a.prefix = prefix_lens; a.slopes = slopes;
+    a.part = (float*)workspace;
+    return launch_packed_attention(shape->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
 }
 
 size_t sampler_step_workspace_bytes(size_t n) { return align256(reduce_workspace_bytes(n)); }

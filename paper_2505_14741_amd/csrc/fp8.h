@@ -7,7 +7,7 @@ namespace ps {
 hipError_t launch_fp8_quantize(int dtype, const void* x, void* q, void* scale, int rows, int cols, long x_row, hipStream_t st);
 
 // out[m, n_out] = act(A * W^T + bias): operands of `blocks` blocks of 128 columns, scales [block][pitch]
-struct Fp8Product {
+struct ScaledProduct {
     const void *a, *w;
     const void *a_scale, *w_scale;
     const float* bias;
@@ -19,6 +19,6 @@ struct Fp8Product {
     bool stream;              // (the same: out is larger than STREAM_BYTES)
 };
 size_t fp8_product_workspace_bytes(int m, int n_out, int blocks);
-hipError_t launch_fp8_product(Fp8Product g, hipStream_t st);
+hipError_t launch_fp8_product(ScaledProduct g, hipStream_t st);
 
 }  // namespace ps

@@ -4,10 +4,9 @@
 // scale byte s (2^(s - 127)) for each row and block of 128 columns, scale[Kp / 128][pitch], pitch = R filled up to a multiple of
 // 16: block after block, so that a tile's scales of one block are neighbours.
 #include "fp8.h"
-#include "few_epilogue.h"
 #include "lane_sums.h"
 #include "plan.h"
-#include "tile_ops.h"
+#include "scaled_product.h"
 #include <type_traits>
 
 namespace ps {
@@ -17,15 +16,6 @@ namespace ps {
 // e4m3: with amax = 1.f * 2^x, e = x - 8 where 1.f <= 1.75 and x - 7 above (448 = 1.75 * 2^8).  Multiplying by 2^-e is exact, so
 // each value is rounded once, to the nearest e4m3.  What is not finite becomes NaN and does not count for the scale.
 // Memory binds: 16 lanes take a block, 8 values each, a 16-byte load of bf16.  17776 x 7680 bf16 (410 MB) 73 us, 5.6 TB/s.
-typedef __attribute__((ext_vector_type(8))) float f32x8_t;
-// 16-byte loads from any element's address (element by element, 17776 rows of 1919 bf16 take 44 us)
-typedef bf16x8_t any_bf16x8_t __attribute__((aligned(2)));
-typedef f32x4_t any_f32x4_t __attribute__((aligned(4)));
-
-__device__ __forceinline__ unsigned max_u32(unsigned a, unsigned b) { return a > b ? a : b; }
-template <int CTRL>
-__device__ __forceinline__ unsigned dpp_u32(unsigned v) { return __builtin_amdgcn_update_dpp(0u, v, CTRL, 0xf, 0xf, true); }
-
 template <typename T>
 __global__ void __launch_bounds__(256)
 fp8_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsigned char* __restrict__ scale, int rows, int cols,
@@ -36,23 +26,7 @@ fp8_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsi
     const int col = b * 128 + (int)l16 * 8;
     const T* p = x + row * x_row + col;
     float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (col + 8 <= cols) {
-        if constexpr (sizeof(T) == 2) {
-            const f32x8_t w = __builtin_convertvector(*reinterpret_cast<const any_bf16x8_t*>(p), f32x8_t);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = w[i];
-        } else {
-            const f32x4_t a = *reinterpret_cast<const any_f32x4_t*>(p), c = *reinterpret_cast<const any_f32x4_t*>(p + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = c[i]; }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) v[i] = to_f32(p[i]);
-    }
+    load_eight(v, p, col, cols);
     unsigned amax = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -103,43 +77,6 @@ hipError_t launch_fp8_quantize(int dtype, const void* x, void* q, void* scale, i
 // groups.  A lane's 32 bytes of a fragment are chunks l / 16 and 4 + l / 16 of its row, of both operands alike (the instruction's
 // own order of k inside a block does not matter then).
 // W fragments are the first operand: a lane holds 4 adjacent output columns (4 * (l / 16) ..) of row l % 16.
-typedef __attribute__((ext_vector_type(8))) int i32x8_t;
-typedef __attribute__((ext_vector_type(4))) int i32x4_t;
-
-__device__ __forceinline__ void lds_dma4_base(unsigned voff, const void* sbase, unsigned lds_addr) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "s"(lds_addr)
-                 : "memory", "m0");
-}
-
-template <int N>
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-
-// 4 adjacent columns of a row, behind the bias
-__device__ __forceinline__ f32x4_t fp8_finish(const Fp8Product& g, f32x4_t x) {
-    if (g.act) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = gelu_fast(x[i]);
-    }
-    return x;
-}
-__device__ __forceinline__ f32x4_t fp8_bias(const Fp8Product& g, int col) {
-    if (g.n_out % 4 == 0) return *reinterpret_cast<const f32x4_t*>(g.bias + min(col, g.n_out - 4));
-    f32x4_t b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = g.bias[min(col + i, g.n_out - 1)];
-    return b;
-}
-__device__ __forceinline__ void fp8_store(const Fp8Product& g, int row, int col, f32x4_t x) {
-    bf16_t* out = g.out + (long)row * g.n_out + col;
-    if (g.n_out % 4 == 0) {                              // a lane's 4 columns are inside or outside together
-        store_quad(out, x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (col + i < g.n_out) out[i] = from_f32<bf16_t>(x[i]);
-    }
-}
-
 // WR x WC waves of TM x TN blocks of 16 x 16 outputs (rows x columns).  A ring of NST stages of one block of k.
 // A stage has two halves of TM / 2 row blocks.  The first goes row block by row block: as soon as the products of one are issued, its
 // registers are read again with the one TM / 2 further down.  Then the next stage's data are waited for and the slot of this one, all of
@@ -147,7 +84,7 @@ __device__ __forceinline__ void fp8_store(const Fp8Product& g, int row, int col,
 // in its last column the next stage's first A fragments.  So one set of registers per operand is enough.
 template <int TM, int TN, int WR, int WC, int NST, int OCC>
 __global__ void __launch_bounds__(WR * WC * 64, OCC)
-gemm_fp8_kernel(Fp8Product g) {
+gemm_fp8_kernel(ScaledProduct g) {
     constexpr int NW = WR * WC, BM = WR * TM * 16, BN = WC * TN * 16, H = TM / 2;
     static_assert((BM + BN) % (8 * NW) == 0 && BM % 8 == 0 && BM <= 256 && BN <= 256 && TM % 2 == 0 && NST >= 2 && NST <= 4, "tile");
     constexpr int GPW = (BM + BN) / 8 / NW, DATA = (BM + BN) * 128, STAGE = DATA + 1024;   // scales: 256 bytes of A, 256 of W
@@ -269,68 +206,11 @@ gemm_fp8_kernel(Fp8Product g) {
     if (kt + 1 < nkt) stage(kt++, std::integral_constant<int, 1>{});
     stage(kt, std::integral_constant<int, 0>{});
     // (every load has landed: the last hand-over waited for all)
-    if (g.pieces > 1) {                                  // [piece][row][column], rows of n_out rounded up to 4
-        const int ldn = (g.n_out + 3) & ~3;
-#pragma unroll
-        for (int x = 0; x < TM; ++x) {
-            const int row = m0 + (wm * TM + x) * 16 + l16;
-            if (row >= g.m) continue;
-#pragma unroll
-            for (int y = 0; y < TN; ++y) {
-                const int col = n0 + (wn * TN + y) * 16 + kgrp * 4;
-                if (col < g.n_out) *reinterpret_cast<f32x4_t*>(g.ws + ((long)piece * g.m + row) * ldn + col) = acc[y][x];
-            }
-        }
-        return;
-    }
-    f32x4_t bias[TN];
-#pragma unroll
-    for (int y = 0; y < TN; ++y) bias[y] = fp8_bias(g, n0 + (wn * TN + y) * 16 + kgrp * 4);
-    const bool wide = g.n_out % 8 == 0;
-#pragma unroll
-    for (int x = 0; x < TM; ++x) {
-        const int row = m0 + (wm * TM + x) * 16 + l16;
-#pragma unroll
-        for (int y = 0; y + 1 < TN; y += 2) {
-            const f32x4_t u = fp8_finish(g, acc[y][x] + bias[y]), v = fp8_finish(g, acc[y + 1][x] + bias[y + 1]);
-            const int col = n0 + (wn * TN + y) * 16;
-            if (wide) {
-                // lanes of neighbouring kgrp swap quads of two column blocks: 8 adjacent columns each, 64 bytes of a row by four lanes
-                typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
-                const u32x2_t p = __builtin_bit_cast(u32x2_t, __builtin_convertvector(u, bf16x4_t));
-                const u32x2_t q = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, bf16x4_t));
-                const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
-                const int c = col + (kgrp & 1) * 16 + (kgrp & 2) * 4;
-                const i32x4_t w = {(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
-                if (row < g.m && c < g.n_out) store_streamed<16>(g.out + (long)row * g.n_out + c, w, g.stream);
-            } else if (row < g.m) {
-                if (col + kgrp * 4 < g.n_out) fp8_store(g, row, col + kgrp * 4, u);
-                if (col + 16 + kgrp * 4 < g.n_out) fp8_store(g, row, col + 16 + kgrp * 4, v);
-            }
-        }
-        if constexpr (TN % 2) {
-            const int col = n0 + (wn * TN + TN - 1) * 16 + kgrp * 4;
-            if (row < g.m && col < g.n_out) fp8_store(g, row, col, fp8_finish(g, acc[TN - 1][x] + bias[TN - 1]));
-        }
-    }
-}
-
-// Adds the pieces of 4 adjacent columns in order.
-__global__ void __launch_bounds__(256)
-gemm_fp8_join_kernel(Fp8Product g, long quads) {
-    const long id = (long)blockIdx.x * 256 + threadIdx.x;
-    if (id >= quads) return;
-    const int per_row = (g.n_out + 3) / 4;
-    const long row = id / per_row;
-    const int col = (int)(id - row * per_row) * 4;
-    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int p = 0; p < g.pieces; ++p) s += *reinterpret_cast<const f32x4_t*>(g.ws + ((long)p * g.m + row) * (per_row * 4) + col);
-    fp8_store(g, (int)row, col, fp8_finish(g, s + fp8_bias(g, col)));
+    scaled_results<TM, TN>(g, acc, m0, n0, piece, wm, wn, l16, kgrp);
 }
 
 template <int TM, int TN, int WR, int WC, int NST, int OCC>
-static void launch_product_tile(Fp8Product g, hipStream_t st) {
+static void launch_product_tile(ScaledProduct g, hipStream_t st) {
     constexpr int BM = WR * TM * 16, BN = WC * TN * 16;
     g.tiles_m = (g.m + BM - 1) / BM;
     g.tiles_n = (g.n_out + BN - 1) / BN;
@@ -342,7 +222,7 @@ size_t fp8_product_workspace_bytes(int m, int n_out, int blocks) {
     return p.pieces > 1 ? (size_t)p.pieces * m * ((n_out + 3) / 4 * 4) * sizeof(float) : 0;
 }
 
-hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
+hipError_t launch_fp8_product(ScaledProduct g, hipStream_t st) {
     const size_t need = fp8_product_workspace_bytes(g.m, g.n_out, g.blocks);
     const Fp8Plan p = fp8_plan(g.m, g.n_out, g.blocks, need > 0 && g.ws && g.ws_bytes >= need, compute_units());
     g.pieces = p.pieces;
@@ -355,7 +235,7 @@ hipError_t launch_fp8_product(Fp8Product g, hipStream_t st) {
     }
     if (p.pieces > 1) {
         const long quads = (long)g.m * ((g.n_out + 3) / 4);
-        gemm_fp8_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, quads);
+        scaled_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, quads);
     }
     return hipGetLastError();
 }

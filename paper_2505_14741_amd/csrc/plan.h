@@ -352,6 +352,16 @@ constexpr Fp8Plan fp8_plan(int m, int n_out, int blocks, bool split, int cus) {
     return p;
 }
 
+// ---- 4-bit blocks (gemm_fp4.hip): a workgroup of the quantizer, or of reading back, takes 16 rows x 512 columns
+constexpr long fp4_workgroups(int rows, int cols) { return (((long)rows + 15) / 16) * (((long)cols + 511) / 512); }
+
+struct Fp4Plan { int tile, pieces; };
+constexpr Fp4Plan fp4_plan(int m, int n_out, int blocks, bool split, int cus) {
+    Fp4Plan p{};
+    p.pieces = 1;
+    return p;
+}
+
 // ---- cross attention: query rows per workgroup, and pieces of the keys.  A function of the sample's shape only, never of the batch.
 // resident: all keys in LDS (bf16), which has to hold two such workgroups.
 struct CrossPlan { int block, nsplit; bool resident; };
@@ -382,6 +392,29 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
     p.nsplit = n < 2 ? 1 : (int)n;
     p.resident = bf16 && head_dim <= 64 && p.nsplit == 1 && rows >= 256 && tiles * 64 * cross_resident_key_bytes(head_dim) <= 80 * 1024;
     return p;
+}
+
+// ---- attention of packed samples (packed_attention.hip): blocks of rows are found on the GPU; what follows is a function of one sample's shape.
+constexpr int PACKED_SLOTS = 512;                        // most (key head, piece, block) of a sample that is divided along its keys
+constexpr int PACKED_KEYS = 1280;                        // least keys of such a sample
+constexpr int PACKED_ROWS = 1024;                        // most rows of one; fewer than the keys, so samples that attend to themselves never are
+// Pieces of 256 keys at least, as many as bring the workgroups to two per compute unit of 256.
+constexpr int packed_pieces(int block, int rows, int keys, int kv_heads) {
+    if (rows > PACKED_ROWS || keys < PACKED_KEYS) return 1;
+    const int items = (rows + block - 1) / block * kv_heads, n = PACKED_SLOTS / items, most = keys / 256;
+    return n < 2 ? 1 : n < most ? n : most;
+}
+// bounds over all samples, of which the host knows the sums only
+constexpr int packed_most_pieces(bool keys_of_their_own, int kv_tokens, int kv_heads) {
+    if (!keys_of_their_own || kv_tokens < PACKED_KEYS) return 1;
+    const int n = PACKED_SLOTS / kv_heads, most = kv_tokens / 256;
+    return n < 2 ? 1 : n < most ? n : most;
+}
+constexpr int packed_slots(int q_tokens, int share, int samples, int block) { return (int)((long)q_tokens * share / block) + samples; }
+// regions of scratch: one per sample, or per PACKED_KEYS keys, in which at most one divided sample begins
+constexpr int packed_regions(int samples, int kv_tokens) {
+    const int n = kv_tokens / PACKED_KEYS + 1;
+    return samples < n ? samples : n;
 }
 
 // ---- group norm: `slices` slices of slice_groups whole groups (the last may have fewer), each over `chunks` chunks of positions.
