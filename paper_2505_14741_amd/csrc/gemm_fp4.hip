@@ -138,8 +138,7 @@ gemm_fp4_kernel(ScaledProduct g) {
     typedef Fp4Strips<BM> SA;
     typedef Fp4Strips<BN> SW;
     static_assert((BM + BN) % (8 * NW) == 0 && BM % 8 == 0 && BM <= 256 && BN <= 256 && TM % 2 == 0 && NST >= 2 && NST <= 4, "tile");
-    static_assert((SA::LOADS + SW::LOADS) % NW == 0, "every wave requests as many strips");
-    constexpr int GPW = (BM + BN) / 8 / NW, SPW = (SA::LOADS + SW::LOADS) / NW, LOADS = GPW + SPW;
+    constexpr int GPW = (BM + BN) / 8 / NW, STRIPS = SA::LOADS + SW::LOADS, SPW = (STRIPS + NW - 1) / NW, LOADS = GPW + SPW;
     constexpr int DATA = (BM + BN) * 128, STAGE = (DATA + SA::BYTES + SW::BYTES + 1023) / 1024 * 1024;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[NST * STAGE];
     const int stages = (g.blocks + 1) / 2;
@@ -179,7 +178,7 @@ gemm_fp4_kernel(ScaledProduct g) {
             const unsigned o = half ? off[i] - (unsigned)(chunk & 4) * 16 : off[i];
             lds_dma16_base(o, base[i] + (long)kt * 128, __builtin_amdgcn_readfirstlane(lds_base + slot * STAGE + group * 1024));
         } else {
-            const int n = wave * SPW + i - GPW;
+            const int n = (wave * SPW + i - GPW) % STRIPS;       // (every wave requests as many: some twice)
             const bool of_a = n < SA::LOADS;
             const int l = of_a ? n : n - SA::LOADS, per = of_a ? SA::PER : SW::PER, r = of_a ? BM : BN, pitch = of_a ? g.a_pitch : g.w_pitch, s0 = of_a ? m0 : n0;
             int strip = l * per + (per > 1 ? lane * 4 / r : 0);
@@ -302,7 +301,13 @@ hipError_t launch_fp4_product(ScaledProduct g, hipStream_t st) {
     const Fp4Plan p = fp4_plan(g.m, g.n_out, g.blocks, need > 0 && g.ws && g.ws_bytes >= need, compute_units());
     g.pieces = p.pieces;
     g.stream = (size_t)g.m * g.n_out * sizeof(bf16_t) > STREAM_BYTES;
-    launch_product_tile<2, 2, 2, 2, 4, 2>(g, st);
+    switch (p.tile) {
+        case FP4_64x64: launch_product_tile<2, 2, 2, 2, 4, 2>(g, st); break;
+        case FP4_128x128: launch_product_tile<2, 4, 4, 2, 3, 2>(g, st); break;
+        case FP4_128x128_PAIR: launch_product_tile<4, 4, 2, 2, 2, 2>(g, st); break;
+        case FP4_192x192: launch_product_tile<6, 3, 2, 4, 3, 2>(g, st); break;
+        default: launch_product_tile<6, 4, 2, 4, 2, 2>(g, st); break;
+    }
     if (p.pieces > 1) {
         const long quads = (long)g.m * ((g.n_out + 3) / 4);
         scaled_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, quads);

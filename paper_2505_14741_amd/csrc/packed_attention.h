@@ -17,10 +17,11 @@ struct PackedArgs {
     long q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
     float* part;                  // scratch of packed_workspace_bytes()
     int slots, most_pieces;       // (set by the launcher)
+    long region_rows;             // (the same)
     bool by_sample;               // (the same)
     bool own_offsets;             // whether kv_offsets are given, for the sizes
 };
-size_t packed_workspace_bytes(int dtype, const PackedArgs& a);
+size_t packed_workspace_bytes(const PackedArgs& a);
 hipError_t launch_packed_attention(int dtype, PackedArgs a, hipStream_t st);
 
 }  // namespace ps

@@ -6,8 +6,7 @@
 // tile of 64 keys is whole for a wave's rows, cut by their reach, or behind it, and only those that are cut look at single keys.
 //
 // Query heads that share a key head are rows of one product, row = token * share + head of the group.  Blocks of BQ rows of one (sample, key head)
-// are found on the GPU, from the offsets: sample s owns the block slots from rows_before(s) / BQ + s on, which leaves room for its last, partial block
-// (and at most one slot of a sample is empty), so that a slot's sample is a search in a rising sequence.
+// are found on the GPU, from the offsets (packed_item); the host knows how many there are at most.
 #include "packed_attention.h"
 #include "lane_sums.h"
 #include "plan.h"
@@ -34,31 +33,65 @@ struct PackedItem {
         return min((long)keys, prefix + ((long)((unsigned)(pos - prefix) / (unsigned)a.frame) + 1) * a.frame);
     }
 };
+// Which key head and slot a workgroup takes.  Workgroup ids go to the 8 XCDs in turn, each with an L2 of its own: an XCD has kv_heads / 8 key heads to itself and
+// every eighth item of the others', over 8 slots as many as all XCDs; low slots, which are long, first.
+__device__ __forceinline__ void packed_place(int kv_heads, int& g, int& slot) {
+    const unsigned x = blockIdx.x & 7, n = blockIdx.x >> 3, own = (unsigned)kv_heads / 8, rest = (unsigned)kv_heads % 8;
+    const unsigned period = n / (unsigned)kv_heads, i = n - period * (unsigned)kv_heads;
+    if (i < 8 * own) {
+        slot = (int)(period * 8 + i / own);
+        g = (int)(x * own + i % own);
+    } else {
+        const unsigned u = (period * rest + i - 8 * own) * 8 + x;
+        slot = (int)(u / rest);
+        g = (int)(8 * own + u % rest);
+    }
+}
+// The block's sample and rows.  Up to 64 samples: those with more keys first, each with its own blocks.  More: sample s has the slots from rows_before(s) / BQ + s
+// on, which leaves room for its last, partial block (and at most one slot of a sample is empty), so that a slot's sample is a search in a rising sequence.
+// A sample's last blocks, whose rows see most, come first.
 template <int BQ>
 __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane) {
     PackedItem t;
-    const int id = a.most_pieces > 1 ? (int)blockIdx.x : xcd_remap(blockIdx.x, gridDim.x);
-    t.g = (int)((unsigned)id / (unsigned)a.slots);
-    const int slot = a.slots - 1 - (id - t.g * a.slots);             // (a sample's last queries see most)
+    int slot, first;                                     // first: the sample's first slot
+    packed_place(a.kv_heads, t.g, slot);
     t.piece = blockIdx.y;
     t.any = false;
-    const auto first_slot = [&](int s) { return (int)((unsigned)within(a.q_offsets[s], 0, a.q_tokens) * (unsigned)a.share / BQ) + s; };
-    int s = 0, n = a.samples, step;
-    do {
-        step = (n + 63) / 64;
-        const int i = lane * step;
-        const unsigned long long below = __ballot(i < n && first_slot(s + min(i, n - 1)) <= slot);
-        if (below == 0) return t;
-        const int c = (__popcll(below) - 1) * step;
-        s += c;
-        n = min(step, n - c);
-    } while (step > 1);
+    int s = 0;
+    if (a.samples <= 64) {
+        const int at = min(lane, a.samples - 1);
+        const int32_t* of = a.kv_offsets ? a.kv_offsets : a.q_offsets;
+        const int q0 = within(a.q_offsets[at], 0, a.q_tokens), nq = within(a.q_offsets[at + 1], q0, a.q_tokens) - q0;
+        const int keys = max(of[at + 1], 0) - max(of[at], 0), blocks = lane < a.samples ? (nq * a.share + BQ - 1) / BQ : 0;
+        int before = 0;                                  // blocks of the samples in front
+        for (int i = 0; i < a.samples; ++i) {
+            const int k = __builtin_amdgcn_readlane(keys, i), n = __builtin_amdgcn_readlane(blocks, i);
+            before += k > keys || (k == keys && i < lane) ? n : 0;
+        }
+        const unsigned long long here = __ballot(slot >= before && slot < before + blocks);
+        if (here == 0) return t;
+        s = __builtin_ctzll(here);
+        first = uniform(__shfl(before, s));
+    } else {
+        const auto first_slot = [&](int s) { return (int)((unsigned)within(a.q_offsets[s], 0, a.q_tokens) * (unsigned)a.share / BQ) + s; };
+        int n = a.samples, step;
+        do {
+            step = (n + 63) / 64;
+            const int i = lane * step;
+            const unsigned long long below = __ballot(i < n && first_slot(s + min(i, n - 1)) <= slot);
+            if (below == 0) return t;
+            const int c = (__popcll(below) - 1) * step;
+            s += c;
+            n = min(step, n - c);
+        } while (step > 1);
+        first = uniform(first_slot(s));
+    }
     t.sample = uniform(s);
     t.q0 = uniform(within(a.q_offsets[t.sample], 0, a.q_tokens));
     const int nq = uniform(within(a.q_offsets[t.sample + 1], t.q0, a.q_tokens)) - t.q0;
     t.rows = nq * a.share;
-    t.r0 = uniform((slot - first_slot(t.sample)) * BQ);
-    if (t.r0 >= t.rows) return t;
+    t.r0 = ((t.rows + BQ - 1) / BQ - 1 - (slot - first)) * BQ;
+    if (t.r0 < 0) return t;
     t.k0 = t.q0;
     t.keys = nq;
     if (a.kv_offsets) {
@@ -67,15 +100,15 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane)
     }
     t.ahead = t.keys - nq;
     t.prefix = a.prefix ? uniform(within(a.prefix[t.sample], 0, t.keys)) : 0;
-    t.pieces = a.most_pieces > 1 ? packed_pieces(BQ, t.rows, t.keys, a.kv_heads) : 1;
+    t.pieces = a.most_pieces > 1 ? packed_pieces(t.rows, t.keys, a.kv_heads) : 1;
     t.any = t.piece < t.pieces;
     return t;
 }
-// where the partial sums of a piece's row lie: a region of PACKED_SLOTS blocks for each sample that is divided
-template <int BQ, int HD>
-__device__ __forceinline__ float* packed_part(const PackedArgs& a, const PackedItem& t, int piece) {
-    const int region = a.by_sample ? t.sample : t.k0 / PACKED_KEYS, block_rows = min(BQ, a.q_tokens * a.share), blocks = (t.rows + BQ - 1) / BQ;
-    return a.part + (((long)region * PACKED_SLOTS + (t.g * t.pieces + piece) * blocks + t.r0 / BQ) * block_rows) * (HD + 4);
+// where the partial sums of a piece's row lie: a region of PACKED_PART_ROWS rows for each sample that is divided
+template <int HD>
+__device__ __forceinline__ float* packed_part(const PackedArgs& a, const PackedItem& t, int piece, int row) {
+    const int region = a.by_sample ? t.sample : t.k0 / PACKED_KEYS;
+    return a.part + (region * a.region_rows + (long)(t.g * t.pieces + piece) * t.rows + row) * (HD + 4);
 }
 
 // offset of a row of the sample in q or o
@@ -107,6 +140,8 @@ __device__ __forceinline__ float packed_bias(const PackedRow& r, float frame) {
     return far == far ? r.slope * far : 0.f;
 }
 
+__device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ float exp2_between(float a, float b, float c) {
     const float half = (0.5f * a - 0.5f * b) * c;
     return __builtin_amdgcn_exp2f(half + half);
@@ -115,154 +150,182 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 // ------------------------------------------------------------------------------------ bf16
 // Tiles are transposed: S^T = K Q^T leaves a query in lane % 32 and keys 8 (i / 4) + 4 (lane / 32) + i % 4 of every 32 in register i, which, rounded to
 // bf16, are the second operand of O^T = V^T P^T as they stand (its k in the order of the registers; V fragments follow).
-// The reference of a row's exponents moves only where some score of a tile exceeds it by 8 in powers of two (probabilities stay below 2^8, sums
-// far from overflow).  Exponents are c s - c m in one instruction; beyond 2^10, where the rounding of c m is 2^-14, a row takes (s - m) c.
+//
+// What binds is the vector unit (an exponential, a multiply-add and half a conversion for each score) next to the matrix unit, so the loop goes
+// over halves of 32 keys in three parts that do not depend on each other: the scores of the next half, the weights of this one, the values of the last one.
+// K and V go straight into LDS, K a tile ahead of its use and V with it, three slots each and one hand-over per tile; rows of a tile are permuted in chunks
+// of 16 bytes so that fragment reads meet different banks.
+//
+// A row's exponents are relative to the largest score of its first 32 keys (without the distance bias, which is not positive where slopes are not
+// negative), instead of a maximum that moves: what the sums became is looked at behind the last key.  Rows whose sum is not within 2^-40 .. 2^32, or
+// above 2^14 with outputs that are not finite, or whose reference is beyond 2^10 (where the rounding of scale * score is 2^-14), are computed again by
+// packed_tracked(), their whole wave with them: a reference that moves where a score exceeds it by 8 in powers of two, and is subtracted first where it is large.
 constexpr float PACKED_AHEAD = 8.0f, PACKED_FAR = 0x1p+10f;
-constexpr int PACKED_BQ = 128, PACKED_BQ_F32 = 64;
+constexpr float PACKED_SUM_MIN = 0x1p-40f, PACKED_SUM_MAX = 0x1p+32f, PACKED_SUM_NEAR = 0x1p+14f;
+constexpr int PACKED_BQ_F32 = 64;
 
-__device__ __forceinline__ s16x4_t packed_read_tr16(const bf16_t* p) {
+__device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
 }
 
-template <int HD, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, HD > 64 ? 2 : 3)
-packed_bf16_kernel(PackedArgs a) {
-    constexpr int KT = 64, LDK = HD + 8, LDV = HD + 16, NB = HD < 32 ? 1 : HD / 32, QS = HD / 16, CH = HD / 8, LOADS = (KT * CH + 255) / 256;
-    __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * LDK], Vs[KT * LDV];
-    __shared__ float Fs[KT];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l32 = lane & 31, hi = lane >> 5;
-    const PackedItem it = packed_item<PACKED_BQ>(a, lane);
-    if (!it.any) return;                                 // (the whole workgroup)
-    const bf16_t *kb = (const bf16_t*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const bf16_t*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
+template <int HD, int QT, bool CAP, bool BIAS>
+struct PackedBf16 {
+    static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
+    static constexpr int NB = HD < 32 ? 1 : HD / 32, QS = HD / 16, ROW = HD * 2, TILE = U * ROW;
+    static constexpr int LOADS = 2 * TILE / 1024 / 4;                // 1 KB loads per wave: K's by the first waves, V's by the others
+    static_assert(LOADS * 4 * 1024 == 2 * TILE, "every wave requests as many");
 
-    const int w0 = it.r0 + wave * 32, wl = min(w0 + 31, it.rows - 1), bl = min(it.r0 + PACKED_BQ, it.rows) - 1, row = min(w0 + l32, it.rows - 1);
-    const bool mine = w0 < it.rows;                      // (the wave has rows)
-    const int least = mine ? it.reach(a, it.ahead + w0 / a.share) : 0, most = mine ? it.reach(a, it.ahead + wl / a.share) : 0;
-    const int tiles_all = (it.keys + KT - 1) / KT, tiles = (it.reach(a, it.ahead + bl / a.share) + KT - 1) / KT;
-    const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
-    PackedRow me = packed_query(a, it, row);
-    me.slope *= PACKED_LOG2E;
+    const PackedArgs& a;
+    const PackedItem& it;
+    unsigned char *const kl, *const vl;                              // three tiles each
+    float* const fl;                                                 // frames of three tiles' keys
+    const bf16_t *kb, *vb;
+    int lane, wave, l32, hi;
+    PackedRow me[QT];
+    float c0, cap2, into, m[QT], mc[QT];                             // m: the reference, a score (capped or biased: in powers of two); mc: in powers of two
+    int koff[QS], voff[NB];
+    bf16x8_t qf[QT][QS];
+    f32x16_t acc[QT][NB];
+    float l[QT];                                                     // of the lane's keys
 
-    i32x4_t kn[LOADS], vn[LOADS];
-    float fn = 0.f;
-    auto fetch = [&](int kv0) {                          // keys behind the sample's last one are zeros
+    // chunk of a row -> its place
+    __device__ __forceinline__ static int k_place(int r) { return HD == 16 ? 0 : HD == 32 ? (r >> 2) & 3 : r & 7; }
+    __device__ __forceinline__ static int v_place(int r) { return HD <= 32 ? 0 : HD == 64 ? (r & 3) | (r & 2) << 1 : (r & 3) << 2; }
+
+    __device__ __forceinline__ PackedBf16(const PackedArgs& a_, const PackedItem& it_, unsigned char* lds, float* frames)
+        : a(a_), it(it_), kl(lds), vl(lds + 3 * TILE), fl(frames) {}
+
+    __device__ __forceinline__ void start(int w0) {
+        kb = (const bf16_t*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head;
+        vb = (const bf16_t*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
+        c0 = a.scale * PACKED_LOG2E;
+        cap2 = a.cap * PACKED_LOG2E;
+        into = CAP ? 2.0f * c0 / a.cap : 0.f;
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int e = threadIdx.x + 256 * u, r = e / CH, key = kv0 + r;
-            kn[u] = vn[u] = i32x4_t{0, 0, 0, 0};
-            if (r < KT && key < it.keys) {
-                kn[u] = *reinterpret_cast<const i32x4_t*>(kb + key * a.k_tok + e % CH * 8);
-                vn[u] = *reinterpret_cast<const i32x4_t*>(vb + key * a.v_tok + e % CH * 8);
-            }
+        for (int q = 0; q < QT; ++q) {
+            const int row = min(w0 + q * 32 + l32, it.rows - 1);
+            me[q] = packed_query(a, it, row);
+            me[q].slope *= PACKED_LOG2E;
+            const bf16_t* p = (const bf16_t*)a.q + packed_row(a, it, row, a.q_tok, a.q_head) + hi * 8;      // second operand of S^T: 8 consecutive d of row l32
+#pragma unroll
+            for (int s = 0; s < QS; ++s) qf[q][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 16);
         }
-        if constexpr (BIAS) fn = packed_frame(a, it, kv0 + (threadIdx.x & 63));
-    };
-    bf16x8_t qf[QS];                                     // second operand of S^T: 8 consecutive d of row l32
-    {
-        const bf16_t* p = (const bf16_t*)a.q + packed_row(a, it, row, a.q_tok, a.q_head) + hi * 8;
 #pragma unroll
-        for (int s = 0; s < QS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(p + s * 16);
+        for (int s = 0; s < QS; ++s) koff[s] = l32 * ROW + ((2 * s + hi) ^ k_place(l32)) * 16;
+        // V^T: row d = l32 of each 32; slot (hi, e) of a step of 16 keys is key 8 (e / 4) + 4 hi + e % 4 (heads of 16: the upper 16 rows repeat the lower)
+        const int r = (lane & 15) >> 2;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+            voff[d] = (4 * hi + r) * ROW + ((d * 4 + (HD < 32 ? 0 : (lane & 16) >> 3) + ((lane & 3) >> 1)) ^ v_place(r)) * 16 + (lane & 1) * 8;
     }
-    f32x16_t acc[NB], l;
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        l[i] = 0.f;
+        for (int q = 0; q < QT; ++q) {
+            l[q] = 0.f;
+            m[q] = -INFINITY;
 #pragma unroll
-        for (int d = 0; d < NB; ++d) acc[d][i] = 0.f;
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[q][d][i] = 0.f;
+        }
     }
-    float m = -INFINITY;
-    const float c0 = a.scale * PACKED_LOG2E, c = CAP || BIAS ? 1.0f : c0, ahead = fminf(PACKED_AHEAD / c, 0x1p+127f);
-    const float cap2 = a.cap * PACKED_LOG2E, into = CAP ? 2.0f * c0 / a.cap : 0.f;
-    const __bf16 one = (__bf16)1.0f;
-    const bf16x8_t ones = {one, one, one, one, one, one, one, one};
+    // requests the keys of tile tk and the values of tile tv (those that lie before `end`) into their slots; keys behind the sample's last one repeat it
+    __device__ __forceinline__ void request(int tk, int kslot, int tv, int vslot, int end) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int n = wave * LOADS + i;
+            const bool of_k = n < 2 * LOADS;
+            const int at = (of_k ? n : n - 2 * LOADS) * 1024 + lane * 16, r = at / ROW, tile = of_k ? tk : tv;
+            if (tile >= end || tile < 0) continue;
+            const int chunk = at % ROW / 16 ^ (of_k ? k_place(r) : v_place(r)), key = min(tile * U + r, it.keys - 1);
+            const bf16_t* p = (of_k ? kb + key * a.k_tok : vb + key * a.v_tok) + chunk * 8;
+            unsigned char* to = (of_k ? kl + kslot * TILE : vl + vslot * TILE) + (of_k ? n : n - 2 * LOADS) * 1024;
+            lds_dma16(p, (unsigned)uniform((int)(unsigned)(size_t)PS_LDS_PTR(to)));
+        }
+    }
+    __device__ __forceinline__ void frames(int tile, int slot) {     // (visible behind the next barrier)
+        if (BIAS && threadIdx.x < U) fl[slot * U + threadIdx.x] = packed_frame(a, it, tile * U + (int)threadIdx.x);
+    }
 
-    if (j0 < j1) fetch(j0 * KT);
-    for (int j = j0; j < j1; ++j) {
-        const int kv0 = j * KT;
-        __syncthreads();                                 // nobody reads the last tile any more
+    __device__ __forceinline__ void scores(f32x16_t (&s)[QT], int slot, int half) const {
+        const unsigned char* kt = kl + slot * TILE + half * 32 * ROW;
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int e = threadIdx.x + 256 * u, r = e / CH, d = e % CH * 8;
-            if (KT * CH % 256 && r >= KT) continue;
-            *reinterpret_cast<i32x4_t*>(Ks + r * LDK + d) = kn[u];
-            *reinterpret_cast<i32x4_t*>(Vs + r * LDV + d) = vn[u];
+        for (int q = 0; q < QT; ++q)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[q][i] = 0.f;
+#pragma unroll
+        for (int x = 0; x < QS; ++x) {
+            const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(kt + koff[x]);
+#pragma unroll
+            for (int q = 0; q < QT; ++q) s[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[q][x], s[q], 0, 0, 0);
         }
-        if (BIAS && threadIdx.x < KT) Fs[threadIdx.x] = fn;
-        __syncthreads();
-        if (j + 1 < j1) fetch(kv0 + KT);
-        if (kv0 >= most) continue;                       // (the wave: nothing that its rows see)
-        const bool cut = kv0 + KT > least;
-        f32x16_t sc[2];
+    }
+    __device__ __forceinline__ float capped(float s) const {         // in powers of two
+        return __builtin_fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * into)), cap2);
+    }
+    // keys that the row does not see
+    __device__ __forceinline__ void cut(f32x16_t& s, int q, int kv0) const {
+        const int left = me[q].reach - kv0 - 4 * hi;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < left ? s[i] : -INFINITY;
+    }
+    // whether the half's keys are all in the prefix, or all in one frame: a row's bias is one number
+    __device__ __forceinline__ bool one_frame(int kv0, float& frame) const {
+        frame = __uint_as_float(0x7fc00000u);
+        if (kv0 + 32 <= it.prefix) return true;
+        if (kv0 < it.prefix) return false;
+        const unsigned f = (unsigned)(kv0 - it.prefix) / (unsigned)a.frame;
+        frame = (float)f;
+        return f == (unsigned)(kv0 + 31 - it.prefix) / (unsigned)a.frame;
+    }
+    __device__ __forceinline__ static float largest(const f32x16_t& s) {
+        float top = s[0];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[g][i] = 0.f;
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        return max_xor32(top);
+    }
+    // Weights 2^(x - ref) of a half, rounded to bf16 for the second product.  The same arithmetic whether some keys are not seen (CUT) or not.
+    template <bool CUT>
+    __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], const float (&ref)[QT], int kv0, int slot, int half) const {
+        float frame = 0.f;
+        const bool one = !BIAS || one_frame(kv0, frame);             // (uniform)
 #pragma unroll
-            for (int s = 0; s < QS; ++s)
-                sc[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(Ks + (g * 32 + l32) * LDK + s * 16 + hi * 8), qf[s], sc[g], 0, 0, 0);
-        }
-        if constexpr (CAP || BIAS) {
+        for (int q = 0; q < QT; ++q) {
+            f32x16_t& x = s[q];
+            float r = ref[q], c = c0;
+            if constexpr (CAP) {
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float x = sc[g][i];
-                    if constexpr (CAP) x = __builtin_fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * into)), cap2);
-                    else x *= c0;
-                    if constexpr (BIAS) x -= packed_bias(me, Fs[g * 32 + 8 * (i / 4) + 4 * hi + i % 4]);
-                    sc[g][i] = x;
-                }
-        }
-        if (cut) {
-            const int left = me.reach - kv0 - 4 * hi;
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[g][i] = g * 32 + 8 * (i / 4) + i % 4 < left ? sc[g][i] : -INFINITY;
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[g][i]);
-        if (__any(top > m + ahead)) {
-            const float mn = fmaxf(m, max_xor32(top));
-            const float alpha = mn == m ? 1.f : exp2_between(m, mn, c);          // 0 on the first tile
-            m = mn;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                l[i] *= alpha;
-#pragma unroll
-                for (int d = 0; d < NB; ++d) acc[d][i] *= alpha;
+                for (int i = 0; i < 16; ++i) x[i] = capped(x[i]);
+                c = 1.0f;
             }
+            if (BIAS && one) r += packed_bias(me[q], frame);
+            if (BIAS && !one) {
+                const float* f = fl + slot * U + half * 32 + 4 * hi;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = x[i] * c - packed_bias(me[q], f[8 * (i / 4) + i % 4]);
+                c = 1.0f;
+            }
+            if constexpr (CUT) cut(x, q, kv0);
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[q][y][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[y * 8 + e], c, -r));
         }
-        float mc = m == -INFINITY ? 0.f : m * c;
-        if (__any(fabsf(mc) > PACKED_FAR)) {
-            const bool far = fabsf(mc) > PACKED_FAR;
-            const float ref = far ? m : 0.f;
-            mc = far ? 0.f : mc;
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[g][i] -= ref;
-        }
-        bf16x8_t pf[4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                pf[s][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[s / 2][s % 2 * 8 + e], c, -mc));
-        // V^T: row d = l32 of each 32; slot (hi, e) of step s is key 16 s + 8 (e / 4) + 4 hi + e % 4
-        const bf16_t* vt = Vs + (4 * hi + ((lane & 15) >> 2)) * LDV + (HD < 32 ? 0 : (lane & 16)) + (lane & 3) * 4;
+    }
+    // acc += V^T P^T, l += the weights as they were rounded (one key alone has weight 1 exactly).
+    // CUT: some of the half's keys are not seen by some rows; they have the weight zero there, which a value that is not finite must not meet.
+    template <bool CUT>
+    __device__ __forceinline__ void values(const bf16x8_t (&pf)[QT][2], int kv0, int slot, int half) {
+        const unsigned char* vt = vl + slot * TILE + half * 32 * ROW;
+        const __bf16 one = (__bf16)1.0f;
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
         bool odd = false;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int x = 0; x < 2; ++x) {
 #pragma unroll
             for (int d = 0; d < NB; ++d) {
-                const bf16_t* p = vt + s * 16 * LDV + d * 32;
-                s16x4_t lo = packed_read_tr16(p), up = packed_read_tr16(p + 8 * LDV);
-                if (cut) {
-                    // Keys that some row does not see have the weight zero there, which a value that is not finite must not meet.
+                s16x4_t lo = packed_read_tr16(vt + voff[d] + x * 16 * ROW), up = packed_read_tr16(vt + voff[d] + x * 16 * ROW + 8 * ROW);
+                if constexpr (CUT) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const bool ol = (lo[i] & 0x7f80) == 0x7f80, ou = (up[i] & 0x7f80) == 0x7f80;
@@ -272,45 +335,221 @@ packed_bf16_kernel(PackedArgs a) {
                     }
                 }
                 const bf16x8_t vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4_t, lo), __builtin_bit_cast(bf16x4_t, up), 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[s], acc[d], 0, 0, 0);
+#pragma unroll
+                for (int q = 0; q < QT; ++q) acc[q][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[q][x], acc[q][d], 0, 0, 0);
             }
-            l = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pf[s], l, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    l[q] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{pf[q][x][e], pf[q][x][e + 1]}, bf16x2_t{one, one}, l[q], false);
         }
-        if (cut && __any(odd)) {                         // what was left out, for the rows that see it
-            for (int key = 0; key < min(KT, it.keys - kv0); ++key) {
-                if (kv0 + key >= me.reach) continue;
+        if (CUT && __any(odd)) {                         // what was left out, for the rows that see it
+#pragma unroll 1
+            for (int key = 0; key < 32; ++key) {
 #pragma unroll
                 for (int d = 0; d < NB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int i = 0; i < (HD < 32 ? 8 : 16); ++i) {
                         const int at = d * 32 + 8 * (i / 4) + 4 * hi + i % 4;
-                        const float x = at < HD ? to_f32(Vs[key * LDV + at]) : 0.f;
-                        if (!(fabsf(x) < INFINITY)) acc[d][i] += x;
+                        const bf16_t* row = reinterpret_cast<const bf16_t*>(vt + key * ROW);
+                        const float x = to_f32(row[(at / 8 ^ v_place(key)) * 8 + at % 8]);
+#pragma unroll
+                        for (int q = 0; q < QT; ++q)
+                            if (kv0 + key < me[q].reach && !(fabsf(x) < INFINITY)) acc[q][d][i] += x;
                     }
             }
         }
     }
-    const float sum = l[0];                              // (every lane has its row's whole sum)
-    if (w0 + l32 >= it.rows) return;
-    if (it.pieces > 1) {
-        float* p = packed_part<PACKED_BQ, HD>(a, it, it.piece) + (long)(wave * 32 + l32) * (HD + 4);
+    // a half with references that move
+    __device__ __forceinline__ void tracked(int kv0, int slot, int half) {
+        f32x16_t s[QT];
+        scores(s, slot, half);
+        const float c = CAP || BIAS ? 1.0f : c0, ahead = fminf(PACKED_AHEAD / c, 0x1p+127f);
+        bf16x8_t pf[QT][2];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            f32x16_t& x = s[q];
+            if constexpr (CAP || BIAS) {
+                const float* f = fl + slot * U + half * 32 + 4 * hi;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = (CAP ? capped(x[i]) : x[i] * c0) - (BIAS ? packed_bias(me[q], f[8 * (i / 4) + i % 4]) : 0.f);
+            }
+            cut(x, q, kv0);
+            const float top = largest(x), mn = top > m[q] + ahead ? top : m[q], alpha = mn == m[q] ? 1.f : exp2_between(m[q], mn, c);   // 0 on the first tile
+            m[q] = mn;
+            l[q] *= alpha;
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[q][d][i] *= alpha;
+            const float mm = mn == -INFINITY ? 0.f : mn * c;
+            const bool far = fabsf(mm) > PACKED_FAR;
+            const float first = far ? mn : 0.f, then = far ? 0.f : mm;
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[q][y][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[y * 8 + e] - first, c, -then));
+        }
+        values<true>(pf, kv0, slot, half);
+    }
+};
+
+template <int HD, int QT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2)
+packed_bf16_kernel(PackedArgs a) {
+    typedef PackedBf16<HD, QT, CAP, BIAS> P;
+    constexpr int U = P::U, NB = P::NB, HALVES = P::HALVES, BQ = 128 * QT;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[6 * P::TILE];
+    __shared__ float fl[BIAS ? 3 * U : 1];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l32 = lane & 31;
+    const PackedItem it = packed_item<BQ>(a, lane);
+    if (!it.any) return;                                 // (the whole workgroup)
+    const int w0 = it.r0 + wave * 32 * QT, wl = min(w0 + 32 * QT - 1, it.rows - 1), bl = min(it.r0 + BQ, it.rows) - 1;
+    const int most = w0 < it.rows ? it.reach(a, it.ahead + wl / a.share) : 0;        // (0: the wave has no rows)
+    const int tiles_all = (it.keys + U - 1) / U, tiles = (it.reach(a, it.ahead + bl / a.share) + U - 1) / U;
+    const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
+    const int end = (most + 31) / 32;                    // halves that some row of the wave sees
+
+    P t(a, it, lds, fl);
+    t.lane = lane; t.wave = wave; t.l32 = l32; t.hi = lane >> 5;
+    t.start(w0);
+    t.clear();
+    // a row's result, or its share of one
+    auto store = [&](int q, bool in) {
+        const int row = w0 + q * 32 + l32;
+        const float sum = sum_xor32(t.l[q]);
+        if (!in || row >= it.rows) return;
+        if (it.pieces > 1) {
+            float* p = packed_part<HD>(a, it, it.piece, row);
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int r = 0; r < (HD < 32 ? 2 : 4); ++r)
+                    *reinterpret_cast<f32x4_t*>(p + d * 32 + r * 8 + t.hi * 4) = f32x4_t{t.acc[q][d][4 * r], t.acc[q][d][4 * r + 1], t.acc[q][d][4 * r + 2], t.acc[q][d][4 * r + 3]};
+            if (t.hi == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, t.m[q]};
+            return;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        bf16_t* p = (bf16_t*)a.o + packed_row(a, it, row, a.o_tok, a.o_head);
 #pragma unroll
         for (int d = 0; d < NB; ++d)
 #pragma unroll
-            for (int r = 0; r < (HD < 32 ? 2 : 4); ++r)
-                *reinterpret_cast<f32x4_t*>(p + d * 32 + r * 8 + hi * 4) = f32x4_t{acc[d][4 * r], acc[d][4 * r + 1], acc[d][4 * r + 2], acc[d][4 * r + 3]};
-        if (hi == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{sum, m};
+            for (int r = 0; r < (HD < 32 ? 2 : 4); ++r) {
+                const f32x4_t x = f32x4_t{t.acc[q][d][4 * r], t.acc[q][d][4 * r + 1], t.acc[q][d][4 * r + 2], t.acc[q][d][4 * r + 3]} * inv;
+                *reinterpret_cast<bf16x4_t*>(p + d * 32 + r * 8 + t.hi * 4) = __builtin_convertvector(x, bf16x4_t);
+            }
+    };
+    if (j0 >= j1) {
+#pragma unroll
+        for (int q = 0; q < QT; ++q) store(q, true);
         return;
     }
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    bf16_t* p = (bf16_t*)a.o + packed_row(a, it, row, a.o_tok, a.o_head);
+    f32x16_t s[2][QT];
+    bf16x8_t pf[2][QT][2];
+    t.request(j0, 0, -1, 0, j1);
+    t.request(j0 + 1, 1, j0, 0, j1);
+    t.frames(j0, 0);
+    // One tile.  Per half h (of all the sample's; parity X): the scores of the next one, this one's weights, the last one's values.
+    // STEADY: all rows of the workgroup see the whole tile, which is neither the first nor the last.
+    int slot = 0;
+    auto tile = [&](int j, auto x_c, auto steady_c) {
+        constexpr bool STEADY = decltype(steady_c)::value;
+        wait_all_loads();                                // K of the next tile, V of this one
+        __syncthreads();                                 // ... everyone's; and nobody reads the last tile's K and the one before's V any more
+        const int up = slot == 2 ? 0 : slot + 1, down = slot == 0 ? 2 : slot - 1;
+        t.request(j + 2, down, j + 1, up, j1);
+        if (STEADY || j + 1 < j1) t.frames(j + 1, up);
+        if (!STEADY && j == j0 && j0 * HALVES < end) t.scores(s[0], slot, 0);
 #pragma unroll
-    for (int d = 0; d < NB; ++d)
+        for (int half = 0; half < HALVES; ++half) {
+            const int X = HALVES == 2 ? half : decltype(x_c)::value, h = j * HALVES + half, kv0 = h * 32;
+            const int next = half + 1 < HALVES ? slot : up, last = half > 0 ? slot : down, next_half = half + 1 < HALVES ? half + 1 : 0, last_half = half > 0 ? half - 1 : HALVES - 1;
+            if constexpr (STEADY) {
+                t.scores(s[X ^ 1], next, next_half);
+                t.template weights<false>(s[X], pf[X], t.mc, kv0, slot, half);
+                t.template values<false>(pf[X ^ 1], kv0 - 32, last, last_half);
+            } else {
+                if (h + 1 < min(end, j1 * HALVES)) t.scores(s[X ^ 1], next, next_half);
+                if (h < end) {
+                    if (h == j0 * HALVES) {
 #pragma unroll
-        for (int r = 0; r < (HD < 32 ? 2 : 4); ++r) {
-            const f32x4_t x = f32x4_t{acc[d][4 * r], acc[d][4 * r + 1], acc[d][4 * r + 2], acc[d][4 * r + 3]} * inv;
-            *reinterpret_cast<bf16x4_t*>(p + d * 32 + r * 8 + hi * 4) = __builtin_convertvector(x, bf16x4_t);
+                        for (int q = 0; q < QT; ++q) {
+                            f32x16_t u = s[X][q];
+                            t.cut(u, q, kv0);
+                            const float top = P::largest(u);
+                            t.m[q] = top == -INFINITY ? top : CAP ? t.capped(top) : BIAS ? top * t.c0 : top;
+                            t.mc[q] = top == -INFINITY ? 0.f : CAP || BIAS ? t.m[q] : top * t.c0;
+                        }
+                    }
+                    t.template weights<true>(s[X], pf[X], t.mc, kv0, slot, half);
+                }
+                if (h > j0 * HALVES && h - 1 < end) t.template values<true>(pf[X ^ 1], kv0 - 32, last, last_half);
+            }
         }
+        slot = up;
+    };
+    const std::integral_constant<int, 0> c0;
+    const std::integral_constant<int, 1> c1;
+    const std::true_type steady;
+    const std::false_type general;
+    const int all_see = it.reach(a, it.ahead + it.r0 / a.share);         // what the block's first row sees
+    int j = j0;
+    if constexpr (HALVES == 2) {
+        do {
+            tile(j++, c0, general);
+            for (; j + 1 < j1 && (j + 1) * U <= all_see; ++j) tile(j, c0, steady);
+        } while (j < j1);
+    } else {
+        tile(j++, c0, general);
+        while (j < j1) {
+            for (; j + 2 < j1 && (j + 2) * U <= all_see; j += 2) { tile(j, c1, steady); tile(j + 1, c0, steady); }
+            tile(j++, c1, general);
+            if (j < j1) tile(j++, c0, general);
+        }
+    }
+    const int h = j1 * HALVES;                           // the last half's values
+    if (h - 1 < end) {
+        const int last = slot == 0 ? 2 : slot - 1;
+        if (HALVES == 2 || ((h - 1 - j0) & 1)) t.template values<true>(pf[1], (h - 1) * 32, last, HALVES - 1);
+        else t.template values<true>(pf[0], (h - 1) * 32, last, HALVES - 1);
+    }
+    // rows that have to be computed again (those that see a key of the piece)
+    bool redo[QT], again = false;
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        redo[q] = false;
+        if (t.me[q].reach > j0 * U) {
+            const float sum = sum_xor32(t.l[q]);
+            redo[q] = !(sum >= PACKED_SUM_MIN && sum <= PACKED_SUM_MAX) || !(fabsf(t.mc[q]) <= PACKED_FAR);
+            float zero = 0.f;                            // (NaN if a value is not finite)
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(t.acc[q][d][i], 0.f, zero);
+            zero += max_xor32(zero);
+            redo[q] = redo[q] || (sum > PACKED_SUM_NEAR && zero != 0.f);
+        }
+        store(q, !redo[q]);
+        again = again || redo[q];
+    }
+    again = __any(again);
+    if (__syncthreads_or(again)) {                       // (the whole workgroup loads)
+        t.clear();
+        for (int j = j0; j < j1; ++j) {
+            __syncthreads();
+            t.request(j, 0, j, 0, j1);
+            t.frames(j, 0);
+            wait_all_loads();
+            __syncthreads();
+            if (again)
+#pragma unroll 1
+                for (int half = 0; half < HALVES; ++half)
+                    if (j * HALVES + half < end) t.tracked((j * HALVES + half) * 32, 0, half);
+        }
+#pragma unroll
+        for (int q = 0; q < QT; ++q) store(q, redo[q]);
+    }
 }
 
 // ------------------------------------------------------------------------------------ fp32
@@ -448,7 +687,7 @@ packed_f32_kernel(PackedArgs a) {
     l = sum_xor32(sum_xor16(l));
     if (w0 + l16 >= it.rows) return;
     if (it.pieces > 1) {
-        float* p = packed_part<PACKED_BQ_F32, HD>(a, it, it.piece) + (long)(wave * 16 + l16) * (HD + 4);
+        float* p = packed_part<HD>(a, it, it.piece, row);
 #pragma unroll
         for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[d];
         if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{l, m};
@@ -461,17 +700,17 @@ packed_f32_kernel(PackedArgs a) {
 
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
 // takes a block, a wave a row at a time: HD / 4 lanes hold 4 adjacent values each, and the wave's 256 / HD teams of them take a piece each in turn.
-template <typename T, int HD, int BQ>
+template <typename T, int HD>
 __global__ void __launch_bounds__(256)
 packed_join_kernel(PackedArgs a) {
-    constexpr int W = HD / 4, TEAMS = 64 / W;
+    constexpr int W = HD / 4, TEAMS = 64 / W, BQ = 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = lane % W * 4, team = lane / W;
     PackedItem it = packed_item<BQ>(a, lane);
     if (!it.any || it.pieces <= 1) return;
     const float c = a.cap > 0.f || a.slopes ? 1.0f : a.scale * PACKED_LOG2E;
-    const long step = packed_part<BQ, HD>(a, it, 1) - packed_part<BQ, HD>(a, it, 0);
+    const long step = (long)it.rows * (HD + 4);
     for (int r = wave; r < min(BQ, it.rows - it.r0); r += 4) {
-        const float* p = packed_part<BQ, HD>(a, it, 0) + (long)r * (HD + 4);
+        const float* p = packed_part<HD>(a, it, 0, it.r0 + r);
         float top = -INFINITY;
         for (int i = lane; i < it.pieces; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
 #pragma unroll
@@ -501,29 +740,35 @@ packed_join_kernel(PackedArgs a) {
     }
 }
 
-static int packed_block(int dtype) { return dtype == PS_BF16 ? PACKED_BQ : PACKED_BQ_F32; }
-
-size_t packed_workspace_bytes(int dtype, const PackedArgs& a) {
+size_t packed_workspace_bytes(const PackedArgs& a) {
     if (packed_most_pieces(a.own_offsets, a.kv_tokens, a.kv_heads) <= 1) return 0;
-    const long block = packed_block(dtype), rows = (long)a.q_tokens * a.share;
-    return (size_t)packed_regions(a.samples, a.kv_tokens) * PACKED_SLOTS * (rows < block ? rows : block) * (a.head_dim + 4) * sizeof(float);
+    return (size_t)packed_regions(a.samples, a.kv_tokens) * packed_region_rows(a.q_tokens * a.share, a.kv_heads) * (a.head_dim + 4) * sizeof(float);
+}
+
+template <int HD, int QT>
+static void launch_packed_bf16(const PackedArgs& a, dim3 grid, hipStream_t st) {
+    if (a.cap > 0.f && a.slopes) packed_bf16_kernel<HD, QT, true, true><<<grid, 256, 0, st>>>(a);
+    else if (a.cap > 0.f) packed_bf16_kernel<HD, QT, true, false><<<grid, 256, 0, st>>>(a);
+    else if (a.slopes) packed_bf16_kernel<HD, QT, false, true><<<grid, 256, 0, st>>>(a);
+    else packed_bf16_kernel<HD, QT, false, false><<<grid, 256, 0, st>>>(a);
 }
 
 template <int HD>
 static hipError_t launch_packed_hd(int dtype, PackedArgs a, hipStream_t st) {
-    const int block = packed_block(dtype);
+    const int block = packed_block(dtype == PS_BF16, a.q_tokens * a.share, a.samples, a.kv_heads, HD, compute_units());
     a.slots = packed_slots(a.q_tokens, a.share, a.samples, block);
     a.most_pieces = packed_most_pieces(a.own_offsets, a.kv_tokens, a.kv_heads);
     a.by_sample = packed_regions(a.samples, a.kv_tokens) == a.samples;
-    const dim3 grid((unsigned)a.slots * (unsigned)a.kv_heads, (unsigned)a.most_pieces);
+    a.region_rows = packed_region_rows(a.q_tokens * a.share, a.kv_heads);
+    const dim3 grid((unsigned)packed_workgroups(a.slots, a.kv_heads), (unsigned)a.most_pieces);
     if (dtype != PS_BF16) packed_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
-    else if (a.cap > 0.f && a.slopes) packed_bf16_kernel<HD, true, true><<<grid, 256, 0, st>>>(a);
-    else if (a.cap > 0.f) packed_bf16_kernel<HD, true, false><<<grid, 256, 0, st>>>(a);
-    else if (a.slopes) packed_bf16_kernel<HD, false, true><<<grid, 256, 0, st>>>(a);
-    else packed_bf16_kernel<HD, false, false><<<grid, 256, 0, st>>>(a);
+    else if (HD > 64 || block == 128) launch_packed_bf16<HD, 1>(a, grid, st);
+    else if constexpr (HD <= 64) launch_packed_bf16<HD, 2>(a, grid, st);
     if (a.most_pieces > 1) {
-        if (dtype == PS_BF16) packed_join_kernel<bf16_t, HD, PACKED_BQ><<<grid.x, 256, 0, st>>>(a);
-        else packed_join_kernel<float, HD, PACKED_BQ_F32><<<grid.x, 256, 0, st>>>(a);
+        a.slots = packed_slots(a.q_tokens, a.share, a.samples, 64);
+        const unsigned wgs = (unsigned)packed_workgroups(a.slots, a.kv_heads);
+        if (dtype == PS_BF16) packed_join_kernel<bf16_t, HD><<<wgs, 256, 0, st>>>(a);
+        else packed_join_kernel<float, HD><<<wgs, 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }

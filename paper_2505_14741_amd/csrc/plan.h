@@ -355,10 +355,43 @@ constexpr Fp8Plan fp8_plan(int m, int n_out, int blocks, bool split, int cus) {
 // ---- 4-bit blocks (gemm_fp4.hip): a workgroup of the quantizer, or of reading back, takes 16 rows x 512 columns
 constexpr long fp4_workgroups(int rows, int cols) { return (((long)rows + 15) / 16) * (((long)cols + 511) / 512); }
 
+// ---- 4-bit products (gemm_fp4.hip): which tile, and how many pieces of k
+// Us of a round of workgroups: fixed + stages of 256 k * stage; `lone`: up to one workgroup per compute unit.
+// Measured, us on 64 x 64 / 128 x 128 of 8 waves / 128 x 128 of 4, two to a unit / 192 x 192 / 192 x 256 tiles (operands that change from call to call):
+// 112 rows x 7680, k = 1920 5.7 / 8.4 / 10.0 / 12.2 / 14.1; 448 x 7680 13.5 / 10.0 / 11.3 / 14.9 / 16.3; 1100 x 5760 20.2 / 16.4 / 14.8 / 15.4 / 16.9;
+// 4516 x 5760 62 / 53 / 43 / 54 / 49; 4516 x 1920, k = 7680 64 / 60 / 57 / 39 / 42; 17776 x 5760, k = 1920 258 / 188 / 150 / 202 / 147; 17776 x 1920,
+// k = 7680 239 / 187 / 167 / 170 / 147, k = 256 36 / 31 / 25 / 47 / 26.  (256 x 256: 181, 183 and 46 on the last three.)
+enum Fp4TileId { FP4_64x64, FP4_128x128, FP4_128x128_PAIR, FP4_192x192, FP4_192x256, FP4_TILES };
+struct Fp4Tile { int bm, bn, per_cu; float fixed, stage, lone_fixed, lone_stage; };
+constexpr Fp4Tile kFp4Tiles[FP4_TILES] = {
+    {64, 64, 2, 2.3f, 0.42f, 3.7f, 0.27f},               // 4 waves of 32 x 32
+    {128, 128, 1, 2.6f, 0.68f, 4.8f, 0.60f},             // 8 waves of 32 x 64
+    {128, 128, 2, 2.6f, 1.28f, 5.0f, 0.67f},             // 4 waves of 64 x 64
+    {192, 192, 1, 10.6f, 1.06f, 6.0f, 1.09f},            // 8 waves of 96 x 48, three stages
+    {192, 256, 1, 5.4f, 1.45f, 4.9f, 1.22f},             // 8 waves of 96 x 64, two stages
+};
 struct Fp4Plan { int tile, pieces; };
+constexpr long fp4_tile_count(int id, int m, int n_out) {
+    return ((long)m + kFp4Tiles[id].bm - 1) / kFp4Tiles[id].bm * (((long)n_out + kFp4Tiles[id].bn - 1) / kFp4Tiles[id].bn);
+}
 constexpr Fp4Plan fp4_plan(int m, int n_out, int blocks, bool split, int cus) {
     Fp4Plan p{};
+    float best = 0.f;
+    const float stages = 0.5f * blocks;
+    for (int id = 0; id < FP4_TILES; ++id) {
+        const Fp4Tile& t = kFp4Tiles[id];
+        const long n = fp4_tile_count(id, m, n_out), slots = (long)t.per_cu * cus;
+        const float rounds = n > 4 * slots ? (float)n / slots : (float)((n + slots - 1) / slots);    // (many rounds drift apart)
+        const float us = n <= cus ? t.lone_fixed + stages * t.lone_stage : rounds * (t.fixed + stages * t.stage);
+        if (id == 0 || us < best) { best = us; p.tile = id; }
+    }
     p.pieces = 1;
+    if (split && p.tile == FP4_64x64) {
+        // tiles that leave compute units idle: pieces of 4 stages at least, and three of them, to be worth the second launch
+        long n = 2L * cus / fp4_tile_count(FP4_64x64, m, n_out);
+        if (n > blocks / 8) n = blocks / 8;
+        if (n >= 3) p.pieces = (int)n;
+    }
     return p;
 }
 
@@ -395,22 +428,31 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
 }
 
 // ---- attention of packed samples (packed_attention.hip): blocks of rows are found on the GPU; what follows is a function of one sample's shape.
-constexpr int PACKED_SLOTS = 512;                        // most (key head, piece, block) of a sample that is divided along its keys
+constexpr int PACKED_PIECES = 512;                       // most (key head, piece, block of 128 rows) of a sample that is divided along its keys
 constexpr int PACKED_KEYS = 1280;                        // least keys of such a sample
 constexpr int PACKED_ROWS = 1024;                        // most rows of one; fewer than the keys, so samples that attend to themselves never are
 // Pieces of 256 keys at least, as many as bring the workgroups to two per compute unit of 256.
-constexpr int packed_pieces(int block, int rows, int keys, int kv_heads) {
+constexpr int packed_pieces(int rows, int keys, int kv_heads) {
     if (rows > PACKED_ROWS || keys < PACKED_KEYS) return 1;
-    const int items = (rows + block - 1) / block * kv_heads, n = PACKED_SLOTS / items, most = keys / 256;
+    const int items = (rows + 127) / 128 * kv_heads, n = PACKED_PIECES / items, most = keys / 256;
     return n < 2 ? 1 : n < most ? n : most;
 }
 // bounds over all samples, of which the host knows the sums only
 constexpr int packed_most_pieces(bool keys_of_their_own, int kv_tokens, int kv_heads) {
     if (!keys_of_their_own || kv_tokens < PACKED_KEYS) return 1;
-    const int n = PACKED_SLOTS / kv_heads, most = kv_tokens / 256;
+    const int n = PACKED_PIECES / kv_heads, most = kv_tokens / 256;
     return n < 2 ? 1 : n < most ? n : most;
 }
+// scratch rows of a sample that is divided: rows * key heads * pieces
+constexpr long packed_region_rows(int rows, int kv_heads) { return (long)PACKED_PIECES * (rows < 128 ? rows : 128); }
+// rows of a workgroup (bf16, heads up to 64: 256 where that leaves two workgroups for each compute unit; a row's result does not depend on it)
+constexpr int packed_block(bool bf16, int rows, int samples, int kv_heads, int head_dim, int cus) {
+    if (!bf16) return 64;
+    return head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 2L * cus ? 256 : 128;
+}
 constexpr int packed_slots(int q_tokens, int share, int samples, int block) { return (int)((long)q_tokens * share / block) + samples; }
+// a workgroup for each slot, up to a multiple of 8, and key head
+constexpr long packed_workgroups(int slots, int kv_heads) { return (slots + 7L) / 8 * 8 * kv_heads; }
 // regions of scratch: one per sample, or per PACKED_KEYS keys, in which at most one divided sample begins
 constexpr int packed_regions(int samples, int kv_tokens) {
     const int n = kv_tokens / PACKED_KEYS + 1;
