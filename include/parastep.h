@@ -313,12 +313,12 @@ PS_API int qk_norm_rope(const void* q, const void* k, const float* table, const 
  * q and o [q_tokens, heads, head_dim], k and v [kv_tokens, kv_heads, head_dim] DEVICE in `dtype`; kv_heads divides heads: query heads h * (heads / kv_heads) .. share key head h.
  * head_dim in {16, 32, 64, 128}, its elements contiguous; token and head strides are free (elements; a multiple of 16 bytes, >= 0; those of q, k, v may be 0; of an
  * extent of 1 they are ignored).  Pointers 16-byte aligned; o must not overlap the inputs, nor its heads each other.  samples, q_tokens and
- * kv_tokens may be 0; samples and heads <= 65535, tokens <= 2^24, q_tokens * heads / kv_heads <= 2^30 and, divided by 64, plus samples, fewer than 2^24 / kv_heads.  frame >= 1; cap >= 0, and scale / cap must be finite.
+ * kv_tokens may be 0; samples and heads <= 65535, tokens <= 2^24, q_tokens * heads / kv_heads <= 2^30 and, divided by 64, plus samples, at most 2^23 / kv_heads, with own_offsets 2^19 / kv_heads.  frame >= 1; cap >= 0, and scale / cap must be finite.
  * Finite in fp32 must be, with what a query sees: scale * log2(e) (refused else), q . k and that times scale * log2(e); cap and slope * distance, times log2(e);
  * the largest |v| times the keys (in bf16 times 2^8 more).  bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32; fp32:
  * everything in fp32.  A sample's result does not depend on the others.
- * workspace: DEVICE, 256-byte aligned, >= packed_attn_workspace_bytes(...) (may be NULL when that is 0): few queries' keys are divided among workgroups, and
- * their partial sums pass through it. */
+ * workspace: DEVICE, 256-byte aligned, >= packed_attn_workspace_bytes(...) (may be NULL when that is 0): where a sample's queries do not fill the chip its keys, with
+ * own_offsets, are divided among workgroups, and their partial sums pass through it; of more than 64 samples it holds a table. */
 typedef struct {
     int samples, q_tokens, kv_tokens, heads, kv_heads, head_dim, dtype;
     int own_offsets;                             /* 1: the keys have offsets of their own */

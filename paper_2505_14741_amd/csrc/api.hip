@@ -767,7 +767,8 @@ int packed_args(const packed_attn_shape* s, PackedArgs& a) {
     if (pieces_meet(s->o_token, s->q_tokens, s->o_head, s->heads, s->head_dim)) return PS_ERR_SHAPE;
     const int share = s->heads / s->kv_heads;
     if ((long)s->q_tokens * share > (1L << 30)) return PS_ERR_SHAPE;
-    if (!grid_fits(packed_workgroups(packed_slots(s->q_tokens, share, s->samples, 64), s->kv_heads), 256)) return PS_ERR_SHAPE;
+    // with the most that pieces add, workgroups stay below 2^24
+    if (((long)s->q_tokens * share / 64 + s->samples) * s->kv_heads > (s->own_offsets ? 1L << 19 : 1L << 23)) return PS_ERR_SHAPE;
     a = PackedArgs{};
     a.samples = s->samples; a.q_tokens = s->q_tokens; a.kv_tokens = s->kv_tokens; a.kv_heads = s->kv_heads; a.share = share; a.head_dim = s->head_dim;
     a.frame = s->frame; a.causal = s->causal; a.scale = s->scale; a.cap = s->cap;
@@ -782,7 +783,7 @@ int packed_args(const packed_attn_shape* s, PackedArgs& a) {
 size_t packed_attn_workspace_bytes(const packed_attn_shape* shape) {
     PackedArgs a;
     if (packed_args(shape, a) != PS_OK || a.samples == 0 || a.q_tokens == 0) return 0;
-    return align256(packed_workspace_bytes(a));
+    return align256(packed_workspace_bytes(shape->dtype, a));
 }
 
 int packed_attn(const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* prefix_lens,
@@ -800,7 +801,7 @@ int packed_attn(const void* q, const void* k, const void* v, const int32_t* q_of
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PS_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.o = o;
     a.q_offsets = q_offsets; a.kv_offsets = kv_offsets; a.prefix = prefix_lens; a.slopes = slopes;
-    a.part = (float*)workspace;
+    a.scratch = need ? workspace : nullptr;
     return launch_packed_attention(shape->dtype, a, (hipStream_t)hip_stream) == hipSuccess ? PS_OK : PS_ERR_HIP;
 }
 

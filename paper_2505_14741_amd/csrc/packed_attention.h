@@ -15,13 +15,13 @@ struct PackedArgs {
     int samples, q_tokens, kv_tokens, kv_heads, share, head_dim, frame, causal;
     float scale, cap;                                    // cap 0: none
     long q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
-    float* part;                  // scratch of packed_workspace_bytes()
-    int slots, most_pieces;       // (set by the launcher)
-    long region_rows;             // (the same)
-    bool by_sample;               // (the same)
     bool own_offsets;             // whether kv_offsets are given, for the sizes
+    void* scratch;                // packed_workspace_bytes()
+    int slots, part_rows;         // (set by the launcher)
+    int2* table;                  // (the same: which slot is whose, or NULL)
+    float* part;                  // (the same: partial sums, or NULL)
 };
-size_t packed_workspace_bytes(const PackedArgs& a);
+size_t packed_workspace_bytes(int dtype, const PackedArgs& a);
 hipError_t launch_packed_attention(int dtype, PackedArgs a, hipStream_t st);
 
 }  // namespace ps

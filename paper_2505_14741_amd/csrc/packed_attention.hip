@@ -22,15 +22,23 @@ typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int within(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
+// n / frame for 0 <= n < 2^24 and inv = 1 / frame: the product is off by less than one
+__device__ __forceinline__ unsigned frame_of(unsigned n, unsigned frame, float inv) {
+    unsigned f = (unsigned)((float)n * inv);
+    f -= f * frame > n ? 1u : 0u;
+    return f + (n - f * frame >= frame ? 1u : 0u);
+}
+
 // (wave-uniform)
 struct PackedItem {
-    int g, r0, rows, q0, k0, keys, ahead, prefix, piece, pieces, sample;
+    int g, r0, rows, q0, k0, keys, ahead, prefix, piece, pieces, sample, slot;
+    float inv_frame;
     bool any;
     // keys that a query sees, at `pos` of the sample's keys
     __device__ __forceinline__ int reach(const PackedArgs& a, int pos) const {
         if (!a.causal) return keys;
         if (pos < prefix) return prefix;
-        return min((long)keys, prefix + ((long)((unsigned)(pos - prefix) / (unsigned)a.frame) + 1) * a.frame);
+        return (int)min((long)keys, prefix + ((long)frame_of((unsigned)(pos - prefix), (unsigned)a.frame, inv_frame) + 1) * a.frame);
     }
 };
 // Which key head and slot a workgroup takes.  Workgroup ids go to the 8 XCDs in turn, each with an L2 of its own: an XCD has kv_heads / 8 key heads to itself and
@@ -47,68 +55,113 @@ __device__ __forceinline__ void packed_place(int kv_heads, int& g, int& slot) {
         g = (int)(8 * own + u % rest);
     }
 }
-// The block's sample and rows.  Up to 64 samples: those with more keys first, each with its own blocks.  More: sample s has the slots from rows_before(s) / BQ + s
-// on, which leaves room for its last, partial block (and at most one slot of a sample is empty), so that a slot's sample is a search in a rising sequence.
-// A sample's last blocks, whose rows see most, come first.
+// A sample's slots for a key head: its blocks, each in its pieces.
+struct PackedCount { int q0, nq, k0, keys, blocks, pieces; };
+template <int BQ>
+__device__ __forceinline__ PackedCount packed_count(const PackedArgs& a, int s) {
+    PackedCount c;
+    c.q0 = within(a.q_offsets[s], 0, a.q_tokens);
+    c.nq = within(a.q_offsets[s + 1], c.q0, a.q_tokens) - c.q0;
+    c.k0 = c.q0;
+    c.keys = c.nq;
+    if (a.own_offsets) {
+        c.k0 = within(a.kv_offsets[s], 0, a.kv_tokens);
+        c.keys = within(a.kv_offsets[s + 1], c.k0, a.kv_tokens) - c.k0;
+    }
+    c.blocks = (c.nq * a.share + BQ - 1) / BQ;
+    c.pieces = a.own_offsets ? packed_pieces(c.nq * a.share, c.keys, a.kv_heads) : 1;
+    return c;
+}
+// More than PACKED_SEARCH samples: a table of (sample, slot of the sample) for every slot, table[0].x of them behind it; made by one workgroup.
+template <int BQ>
+__global__ void __launch_bounds__(1024)
+packed_table_kernel(PackedArgs a) {
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int2* const table = a.table;
+    int base = 0;
+    for (int s0 = 0; s0 < a.samples; s0 += 1024) {
+        const int s = s0 + (int)threadIdx.x;
+        int n = 0;
+        if (s < a.samples) {
+            const PackedCount c = packed_count<BQ>(a, s);
+            n = c.blocks * c.pieces;
+        }
+        int upto = n;                                    // inclusive sums
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            const int v = __shfl_up(upto, x);
+            upto += lane >= x ? v : 0;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        int at = base + upto - n;
+        for (int w = 0; w < 16; ++w) {
+            at += w < wave ? sums[w] : 0;
+            base += sums[w];
+        }
+        for (int i = 0; i < n; ++i)
+            if (at + i < a.slots) table[1 + at + i] = make_int2(s, i);   // (offsets that fall could count more)
+    }
+    if (threadIdx.x == 0) table[0] = make_int2(min(base, a.slots), 0);
+}
+
+// The block's sample, rows and piece.  Up to 64 samples are looked through here, those with more keys first.  A sample's last blocks, whose rows see most, come
+// first.
 template <int BQ>
 __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane) {
     PackedItem t;
-    int slot, first;                                     // first: the sample's first slot
+    int slot, of_sample;                                 // of_sample: which of the sample's slots
     packed_place(a.kv_heads, t.g, slot);
-    t.piece = blockIdx.y;
     t.any = false;
-    int s = 0;
-    if (a.samples <= 64) {
-        const int at = min(lane, a.samples - 1);
-        const int32_t* of = a.kv_offsets ? a.kv_offsets : a.q_offsets;
-        const int q0 = within(a.q_offsets[at], 0, a.q_tokens), nq = within(a.q_offsets[at + 1], q0, a.q_tokens) - q0;
-        const int keys = max(of[at + 1], 0) - max(of[at], 0), blocks = lane < a.samples ? (nq * a.share + BQ - 1) / BQ : 0;
-        int before = 0;                                  // blocks of the samples in front
+    t.slot = slot;
+    if (slot >= a.slots) return t;
+    PackedCount c;
+    if (a.samples <= PACKED_SEARCH) {
+        c = packed_count<BQ>(a, min(lane, a.samples - 1));
+        const int n = lane < a.samples ? c.blocks * c.pieces : 0;
+        int before = 0;                                  // slots of the samples in front
         for (int i = 0; i < a.samples; ++i) {
-            const int k = __builtin_amdgcn_readlane(keys, i), n = __builtin_amdgcn_readlane(blocks, i);
-            before += k > keys || (k == keys && i < lane) ? n : 0;
+            const int k = __builtin_amdgcn_readlane(c.keys, i), m = __builtin_amdgcn_readlane(n, i);
+            before += k > c.keys || (k == c.keys && i < lane) ? m : 0;
         }
-        const unsigned long long here = __ballot(slot >= before && slot < before + blocks);
+        const unsigned long long here = __ballot(slot >= before && slot < before + n);
         if (here == 0) return t;
-        s = __builtin_ctzll(here);
-        first = uniform(__shfl(before, s));
+        t.sample = __builtin_ctzll(here);
+        of_sample = slot - __builtin_amdgcn_readlane(before, t.sample);
+        c.q0 = __builtin_amdgcn_readlane(c.q0, t.sample);
+        c.nq = __builtin_amdgcn_readlane(c.nq, t.sample);
+        c.k0 = __builtin_amdgcn_readlane(c.k0, t.sample);
+        c.keys = __builtin_amdgcn_readlane(c.keys, t.sample);
+        c.blocks = __builtin_amdgcn_readlane(c.blocks, t.sample);
+        c.pieces = __builtin_amdgcn_readlane(c.pieces, t.sample);
     } else {
-        const auto first_slot = [&](int s) { return (int)((unsigned)within(a.q_offsets[s], 0, a.q_tokens) * (unsigned)a.share / BQ) + s; };
-        int n = a.samples, step;
-        do {
-            step = (n + 63) / 64;
-            const int i = lane * step;
-            const unsigned long long below = __ballot(i < n && first_slot(s + min(i, n - 1)) <= slot);
-            if (below == 0) return t;
-            const int c = (__popcll(below) - 1) * step;
-            s += c;
-            n = min(step, n - c);
-        } while (step > 1);
-        first = uniform(first_slot(s));
+        if (slot >= uniform(a.table[0].x)) return t;
+        const int2 e = a.table[1 + slot];
+        t.sample = uniform(e.x);
+        of_sample = uniform(e.y);
+        c = packed_count<BQ>(a, t.sample);
+        c.q0 = uniform(c.q0); c.nq = uniform(c.nq); c.k0 = uniform(c.k0); c.keys = uniform(c.keys); c.blocks = uniform(c.blocks); c.pieces = uniform(c.pieces);
     }
-    t.sample = uniform(s);
-    t.q0 = uniform(within(a.q_offsets[t.sample], 0, a.q_tokens));
-    const int nq = uniform(within(a.q_offsets[t.sample + 1], t.q0, a.q_tokens)) - t.q0;
-    t.rows = nq * a.share;
-    t.r0 = ((t.rows + BQ - 1) / BQ - 1 - (slot - first)) * BQ;
-    if (t.r0 < 0) return t;
-    t.k0 = t.q0;
-    t.keys = nq;
-    if (a.kv_offsets) {
-        t.k0 = uniform(within(a.kv_offsets[t.sample], 0, a.kv_tokens));
-        t.keys = uniform(within(a.kv_offsets[t.sample + 1], t.k0, a.kv_tokens)) - t.k0;
-    }
-    t.ahead = t.keys - nq;
+    const int block = (int)((unsigned)of_sample / (unsigned)c.pieces);
+    t.piece = of_sample - block * c.pieces;
+    t.pieces = c.pieces;
+    t.q0 = c.q0;
+    t.rows = c.nq * a.share;
+    t.r0 = (c.blocks - 1 - block) * BQ;
+    t.k0 = c.k0;
+    t.keys = c.keys;
+    t.ahead = c.keys - c.nq;
     t.prefix = a.prefix ? uniform(within(a.prefix[t.sample], 0, t.keys)) : 0;
-    t.pieces = a.most_pieces > 1 ? packed_pieces(t.rows, t.keys, a.kv_heads) : 1;
-    t.any = t.piece < t.pieces;
+    t.inv_frame = 1.0f / (float)a.frame;
+    t.any = true;
     return t;
 }
-// where the partial sums of a piece's row lie: a region of PACKED_PART_ROWS rows for each sample that is divided
-template <int HD>
+// where the partial sums of a block's row lie: a block of rows for each slot and key head (slots of the block's pieces are neighbours)
+template <int BQ, int HD>
 __device__ __forceinline__ float* packed_part(const PackedArgs& a, const PackedItem& t, int piece, int row) {
-    const int region = a.by_sample ? t.sample : t.k0 / PACKED_KEYS;
-    return a.part + (region * a.region_rows + (long)(t.g * t.pieces + piece) * t.rows + row) * (HD + 4);
+    return a.part + (((long)(t.slot - t.piece + piece) * a.kv_heads + t.g) * a.part_rows + (row - t.r0)) * (HD + 4);
 }
 
 // offset of a row of the sample in q or o
@@ -126,13 +179,13 @@ __device__ __forceinline__ PackedRow packed_query(const PackedArgs& a, const Pac
     r.slope = r.frame = 0.f;
     if (a.slopes && pos >= t.prefix) {
         r.slope = a.slopes[t.g * a.share + (row - i * a.share)];
-        r.frame = (float)((unsigned)(pos - t.prefix) / (unsigned)a.frame);
+        r.frame = (float)frame_of((unsigned)(pos - t.prefix), (unsigned)a.frame, t.inv_frame);
     }
     return r;
 }
 // A key's frame, NaN in the prefix.
 __device__ __forceinline__ float packed_frame(const PackedArgs& a, const PackedItem& t, int key) {
-    return key < t.prefix ? __uint_as_float(0x7fc00000u) : (float)((unsigned)(key - t.prefix) / (unsigned)a.frame);
+    return key < t.prefix ? __uint_as_float(0x7fc00000u) : (float)frame_of((unsigned)min(key - t.prefix, (1 << 24) - 1), (unsigned)a.frame, t.inv_frame);
 }
 // slope * distance, 0 where the key is in the prefix
 __device__ __forceinline__ float packed_bias(const PackedRow& r, float frame) {
@@ -140,7 +193,9 @@ __device__ __forceinline__ float packed_bias(const PackedRow& r, float frame) {
     return far == far ? r.slope * far : 0.f;
 }
 
-__device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_between(float a, float b, float c) {
     const float half = (0.5f * a - 0.5f * b) * c;
@@ -247,17 +302,21 @@ struct PackedBf16 {
         if (BIAS && threadIdx.x < U) fl[slot * U + threadIdx.x] = packed_frame(a, it, tile * U + (int)threadIdx.x);
     }
 
-    __device__ __forceinline__ void scores(f32x16_t (&s)[QT], int slot, int half) const {
-        const unsigned char* kt = kl + slot * TILE + half * 32 * ROW;
+    __device__ __forceinline__ const unsigned char* keys_at(int slot, int half) const { return kl + slot * TILE + half * 32 * ROW; }
+    __device__ __forceinline__ const unsigned char* values_at(int slot, int half) const { return vl + slot * TILE + half * 32 * ROW; }
+    __device__ __forceinline__ const float* frames_at(int slot, int half) const { return fl + slot * U + half * 32; }
+    // QN: query tiles that count
+    template <int QN>
+    __device__ __forceinline__ void scores(f32x16_t (&s)[QN], const unsigned char* kt) const {
 #pragma unroll
-        for (int q = 0; q < QT; ++q)
+        for (int q = 0; q < QN; ++q)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[q][i] = 0.f;
 #pragma unroll
         for (int x = 0; x < QS; ++x) {
             const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(kt + koff[x]);
 #pragma unroll
-            for (int q = 0; q < QT; ++q) s[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[q][x], s[q], 0, 0, 0);
+            for (int q = 0; q < QN; ++q) s[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[q][x], s[q], 0, 0, 0);
         }
     }
     __device__ __forceinline__ float capped(float s) const {         // in powers of two
@@ -273,10 +332,10 @@ struct PackedBf16 {
     __device__ __forceinline__ bool one_frame(int kv0, float& frame) const {
         frame = __uint_as_float(0x7fc00000u);
         if (kv0 + 32 <= it.prefix) return true;
-        if (kv0 < it.prefix) return false;
-        const unsigned f = (unsigned)(kv0 - it.prefix) / (unsigned)a.frame;
+        if (kv0 < it.prefix || a.frame < 32) return false;
+        const unsigned n = (unsigned)(kv0 - it.prefix), f = frame_of(n, (unsigned)a.frame, it.inv_frame);
         frame = (float)f;
-        return f == (unsigned)(kv0 + 31 - it.prefix) / (unsigned)a.frame;
+        return uniform((int)(n + 31 - f * (unsigned)a.frame < (unsigned)a.frame)) != 0;
     }
     __device__ __forceinline__ static float largest(const f32x16_t& s) {
         float top = s[0];
@@ -286,7 +345,7 @@ struct PackedBf16 {
     }
     // Weights 2^(x - ref) of a half, rounded to bf16 for the second product.  The same arithmetic whether some keys are not seen (CUT) or not.
     template <bool CUT>
-    __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], const float (&ref)[QT], int kv0, int slot, int half) const {
+    __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], const float (&ref)[QT], int kv0, const float* of) const {
         float frame = 0.f;
         const bool one = !BIAS || one_frame(kv0, frame);             // (uniform)
 #pragma unroll
@@ -300,9 +359,16 @@ struct PackedBf16 {
             }
             if (BIAS && one) r += packed_bias(me[q], frame);
             if (BIAS && !one) {
-                const float* f = fl + slot * U + half * 32 + 4 * hi;
+                const float* f = of + 4 * hi;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = x[i] * c - packed_bias(me[q], f[8 * (i / 4) + i % 4]);
+                for (int i = 0; i < 16; ++i) x[i] *= c;
+                if (kv0 >= it.prefix) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-me[q].slope, fabsf(me[q].frame - f[8 * (i / 4) + i % 4]), x[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] -= packed_bias(me[q], f[8 * (i / 4) + i % 4]);
+                }
                 c = 1.0f;
             }
             if constexpr (CUT) cut(x, q, kv0);
@@ -314,9 +380,8 @@ struct PackedBf16 {
     }
     // acc += V^T P^T, l += the weights as they were rounded (one key alone has weight 1 exactly).
     // CUT: some of the half's keys are not seen by some rows; they have the weight zero there, which a value that is not finite must not meet.
-    template <bool CUT>
-    __device__ __forceinline__ void values(const bf16x8_t (&pf)[QT][2], int kv0, int slot, int half) {
-        const unsigned char* vt = vl + slot * TILE + half * 32 * ROW;
+    template <bool CUT, int QN>
+    __device__ __forceinline__ void values(const bf16x8_t (&pf)[QN][2], int kv0, const unsigned char* vt) {
         const __bf16 one = (__bf16)1.0f;
         typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
         bool odd = false;
@@ -336,10 +401,10 @@ struct PackedBf16 {
                 }
                 const bf16x8_t vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4_t, lo), __builtin_bit_cast(bf16x4_t, up), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int q = 0; q < QT; ++q) acc[q][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[q][x], acc[q][d], 0, 0, 0);
+                for (int q = 0; q < QN; ++q) acc[q][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[q][x], acc[q][d], 0, 0, 0);
             }
 #pragma unroll
-            for (int q = 0; q < QT; ++q)
+            for (int q = 0; q < QN; ++q)
 #pragma unroll
                 for (int e = 0; e < 8; e += 2)
                     l[q] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{pf[q][x][e], pf[q][x][e + 1]}, bf16x2_t{one, one}, l[q], false);
@@ -355,23 +420,21 @@ struct PackedBf16 {
                         const bf16_t* row = reinterpret_cast<const bf16_t*>(vt + key * ROW);
                         const float x = to_f32(row[(at / 8 ^ v_place(key)) * 8 + at % 8]);
 #pragma unroll
-                        for (int q = 0; q < QT; ++q)
+                        for (int q = 0; q < QN; ++q)
                             if (kv0 + key < me[q].reach && !(fabsf(x) < INFINITY)) acc[q][d][i] += x;
                     }
             }
         }
     }
-    // a half with references that move
-    __device__ __forceinline__ void tracked(int kv0, int slot, int half) {
-        f32x16_t s[QT];
-        scores(s, slot, half);
+    // weights of a half with references that move
+    template <int QN>
+    __device__ __forceinline__ void tracked(f32x16_t (&s)[QN], bf16x8_t (&pf)[QN][2], int kv0, const float* of) {
         const float c = CAP || BIAS ? 1.0f : c0, ahead = fminf(PACKED_AHEAD / c, 0x1p+127f);
-        bf16x8_t pf[QT][2];
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
+        for (int q = 0; q < QN; ++q) {
             f32x16_t& x = s[q];
             if constexpr (CAP || BIAS) {
-                const float* f = fl + slot * U + half * 32 + 4 * hi;
+                const float* f = of + 4 * hi;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = (CAP ? capped(x[i]) : x[i] * c0) - (BIAS ? packed_bias(me[q], f[8 * (i / 4) + i % 4]) : 0.f);
             }
@@ -391,7 +454,88 @@ struct PackedBf16 {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) pf[q][y][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[y * 8 + e] - first, c, -then));
         }
-        values<true>(pf, kv0, slot, half);
+    }
+
+    // Few rows (PACKED_FEW_ROWS): memory binds, and the waves take every fourth half of the keys each, through slots of their own and without a barrier; their
+    // sums are united behind the last key, in the first wave's registers.
+    static constexpr int FEW_SLOTS = HD > 64 ? 1 : 2, FEW_LOADS = 32 * ROW / 1024, FEW_HALF = 32 * ROW, FEW_BYTES = 4 * FEW_SLOTS * 2 * FEW_HALF;
+    __device__ __forceinline__ void request_half(int h, unsigned char* to, bool of_k) {
+#pragma unroll
+        for (int i = 0; i < FEW_LOADS; ++i) {
+            const int at = i * 1024 + lane * 16, r = at / ROW, chunk = at % ROW / 16 ^ (of_k ? k_place(r) : v_place(r)), key = min(h * 32 + r, it.keys - 1);
+            const bf16_t* p = (of_k ? kb + key * a.k_tok : vb + key * a.v_tok) + chunk * 8;
+            lds_dma16(p, (unsigned)uniform((int)(unsigned)(size_t)PS_LDS_PTR(to + i * 1024)));
+        }
+    }
+    __device__ __forceinline__ void few(int first, int end) {        // halves first .. end - 1
+        constexpr int L = FEW_LOADS, NS = FEW_SLOTS;
+        unsigned char* const own = kl + wave * NS * 2 * FEW_HALF;    // [slot][keys | values]
+        float* const of = fl + wave * 32;
+        const int h0 = first + wave;
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+            if (h0 + 4 * n < end) {
+                request_half(h0 + 4 * n, own + n * 2 * FEW_HALF, true);
+                request_half(h0 + 4 * n, own + n * 2 * FEW_HALF + FEW_HALF, false);
+            }
+        int slot = 0;
+        for (int h = h0; h < end; h += 4) {
+            unsigned char *const ks = own + slot * 2 * FEW_HALF, *const vs = ks + FEW_HALF;
+            const bool more = h + 4 < end;               // (with two slots: its loads are out)
+            if (NS == 2 && more) wait_loads<3 * L>(); else wait_loads<L>();
+            f32x16_t s[1];
+            bf16x8_t pf[1][2];
+            scores<1>(s, ks);
+            if (BIAS && lane < 32) of[lane] = packed_frame(a, it, h * 32 + lane);
+            wait_lds();
+            if (NS == 1 && more) request_half(h + 4, ks, true);
+            tracked<1>(s, pf, h * 32, of);
+            if (more) wait_loads<(NS == 2 ? 2 : 1) * L>(); else wait_loads<0>();
+            values<true, 1>(pf, h * 32, vs);
+            wait_lds();
+            if (NS == 1 && more) request_half(h + 4, vs, false);
+            if (NS == 2 && h + 8 < end) {
+                request_half(h + 8, ks, true);
+                request_half(h + 8, vs, false);
+            }
+            slot = NS == 2 ? slot ^ 1 : 0;
+        }
+        __syncthreads();                                 // (nobody reads its slots any more)
+        float* const sums = reinterpret_cast<float*>(kl);            // [wave - 1][value][lane]
+        constexpr int N = NB * 16 + 2;
+        static_assert(3 * N * 64 * 4 <= FEW_BYTES, "scratch");
+        if (wave > 0) {
+            float* to = sums + (wave - 1) * N * 64 + lane;
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) to[(d * 16 + i) * 64] = acc[0][d][i];
+            to[(N - 2) * 64] = l[0];
+            to[(N - 1) * 64] = m[0];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        const float c = CAP || BIAS ? 1.0f : c0;
+        float top = m[0];
+#pragma unroll
+        for (int w = 0; w < 3; ++w) top = fmaxf(top, sums[(w * N + N - 1) * 64 + lane]);
+        const float ref = top == -INFINITY ? 0.f : top, mine = exp2_between(m[0], ref, c);
+        m[0] = top;
+        l[0] *= mine;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[0][d][i] *= mine;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) {
+            const float* from = sums + w * N * 64 + lane;
+            const float f = exp2_between(from[(N - 1) * 64], ref, c);
+            l[0] = __builtin_fmaf(from[(N - 2) * 64], f, l[0]);
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[0][d][i] = __builtin_fmaf(from[(d * 16 + i) * 64], f, acc[0][d][i]);
+        }
     }
 };
 
@@ -400,12 +544,13 @@ __global__ void __launch_bounds__(256, 2)
 packed_bf16_kernel(PackedArgs a) {
     typedef PackedBf16<HD, QT, CAP, BIAS> P;
     constexpr int U = P::U, NB = P::NB, HALVES = P::HALVES, BQ = 128 * QT;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[6 * P::TILE];
-    __shared__ float fl[BIAS ? 3 * U : 1];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[6 * P::TILE > P::FEW_BYTES ? 6 * P::TILE : P::FEW_BYTES];
+    __shared__ float fl[BIAS ? (3 * U > 128 ? 3 * U : 128) : 1];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l32 = lane & 31;
     const PackedItem it = packed_item<BQ>(a, lane);
     if (!it.any) return;                                 // (the whole workgroup)
-    const int w0 = it.r0 + wave * 32 * QT, wl = min(w0 + 32 * QT - 1, it.rows - 1), bl = min(it.r0 + BQ, it.rows) - 1;
+    const bool few = it.rows <= PACKED_FEW_ROWS && it.keys > PACKED_FEW_MIN;         // (then all waves have the same rows)
+    const int w0 = it.r0 + (few ? 0 : wave * 32 * QT), wl = min(w0 + 32 * QT - 1, it.rows - 1), bl = min(it.r0 + BQ, it.rows) - 1;
     const int most = w0 < it.rows ? it.reach(a, it.ahead + wl / a.share) : 0;        // (0: the wave has no rows)
     const int tiles_all = (it.keys + U - 1) / U, tiles = (it.reach(a, it.ahead + bl / a.share) + U - 1) / U;
     const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
@@ -421,7 +566,7 @@ packed_bf16_kernel(PackedArgs a) {
         const float sum = sum_xor32(t.l[q]);
         if (!in || row >= it.rows) return;
         if (it.pieces > 1) {
-            float* p = packed_part<HD>(a, it, it.piece, row);
+            float* p = packed_part<BQ, HD>(a, it, it.piece, row);
 #pragma unroll
             for (int d = 0; d < NB; ++d)
 #pragma unroll
@@ -440,9 +585,14 @@ packed_bf16_kernel(PackedArgs a) {
                 *reinterpret_cast<bf16x4_t*>(p + d * 32 + r * 8 + t.hi * 4) = __builtin_convertvector(x, bf16x4_t);
             }
     };
-    if (j0 >= j1) {
+    if (j0 >= j1) {                                      // (of few rows, every wave the same)
 #pragma unroll
         for (int q = 0; q < QT; ++q) store(q, true);
+        return;
+    }
+    if (few) {
+        t.few(j0 * HALVES, min(j1 * HALVES, end));
+        if (wave == 0) store(0, true);
         return;
     }
     f32x16_t s[2][QT];
@@ -455,22 +605,22 @@ packed_bf16_kernel(PackedArgs a) {
     int slot = 0;
     auto tile = [&](int j, auto x_c, auto steady_c) {
         constexpr bool STEADY = decltype(steady_c)::value;
-        wait_all_loads();                                // K of the next tile, V of this one
+        wait_loads<0>();                                // K of the next tile, V of this one
         __syncthreads();                                 // ... everyone's; and nobody reads the last tile's K and the one before's V any more
         const int up = slot == 2 ? 0 : slot + 1, down = slot == 0 ? 2 : slot - 1;
         t.request(j + 2, down, j + 1, up, j1);
         if (STEADY || j + 1 < j1) t.frames(j + 1, up);
-        if (!STEADY && j == j0 && j0 * HALVES < end) t.scores(s[0], slot, 0);
+        if (!STEADY && j == j0 && j0 * HALVES < end) t.template scores<QT>(s[0], t.keys_at(slot, 0));
 #pragma unroll
         for (int half = 0; half < HALVES; ++half) {
             const int X = HALVES == 2 ? half : decltype(x_c)::value, h = j * HALVES + half, kv0 = h * 32;
             const int next = half + 1 < HALVES ? slot : up, last = half > 0 ? slot : down, next_half = half + 1 < HALVES ? half + 1 : 0, last_half = half > 0 ? half - 1 : HALVES - 1;
             if constexpr (STEADY) {
-                t.scores(s[X ^ 1], next, next_half);
-                t.template weights<false>(s[X], pf[X], t.mc, kv0, slot, half);
-                t.template values<false>(pf[X ^ 1], kv0 - 32, last, last_half);
+                t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
+                t.template weights<false>(s[X], pf[X], t.mc, kv0, t.frames_at(slot, half));
+                t.template values<false, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
             } else {
-                if (h + 1 < min(end, j1 * HALVES)) t.scores(s[X ^ 1], next, next_half);
+                if (h + 1 < min(end, j1 * HALVES)) t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
                 if (h < end) {
                     if (h == j0 * HALVES) {
 #pragma unroll
@@ -482,9 +632,9 @@ packed_bf16_kernel(PackedArgs a) {
                             t.mc[q] = top == -INFINITY ? 0.f : CAP || BIAS ? t.m[q] : top * t.c0;
                         }
                     }
-                    t.template weights<true>(s[X], pf[X], t.mc, kv0, slot, half);
+                    t.template weights<true>(s[X], pf[X], t.mc, kv0, t.frames_at(slot, half));
                 }
-                if (h > j0 * HALVES && h - 1 < end) t.template values<true>(pf[X ^ 1], kv0 - 32, last, last_half);
+                if (h > j0 * HALVES && h - 1 < end) t.template values<true, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
             }
         }
         slot = up;
@@ -511,8 +661,8 @@ packed_bf16_kernel(PackedArgs a) {
     const int h = j1 * HALVES;                           // the last half's values
     if (h - 1 < end) {
         const int last = slot == 0 ? 2 : slot - 1;
-        if (HALVES == 2 || ((h - 1 - j0) & 1)) t.template values<true>(pf[1], (h - 1) * 32, last, HALVES - 1);
-        else t.template values<true>(pf[0], (h - 1) * 32, last, HALVES - 1);
+        if (HALVES == 2 || ((h - 1 - j0) & 1)) t.template values<true, QT>(pf[1], (h - 1) * 32, t.values_at(last, HALVES - 1));
+        else t.template values<true, QT>(pf[0], (h - 1) * 32, t.values_at(last, HALVES - 1));
     }
     // rows that have to be computed again (those that see a key of the piece)
     bool redo[QT], again = false;
@@ -540,12 +690,16 @@ packed_bf16_kernel(PackedArgs a) {
             __syncthreads();
             t.request(j, 0, j, 0, j1);
             t.frames(j, 0);
-            wait_all_loads();
+            wait_loads<0>();
             __syncthreads();
             if (again)
 #pragma unroll 1
                 for (int half = 0; half < HALVES; ++half)
-                    if (j * HALVES + half < end) t.tracked((j * HALVES + half) * 32, 0, half);
+                    if (j * HALVES + half < end) {
+                        t.template scores<QT>(s[0], t.keys_at(0, half));
+                        t.template tracked<QT>(s[0], pf[0], (j * HALVES + half) * 32, t.frames_at(0, half));
+                        t.template values<true, QT>(pf[0], (j * HALVES + half) * 32, t.values_at(0, half));
+                    }
         }
 #pragma unroll
         for (int q = 0; q < QT; ++q) store(q, redo[q]);
@@ -555,6 +709,19 @@ packed_bf16_kernel(PackedArgs a) {
 // ------------------------------------------------------------------------------------ fp32
 // 16 rows per wave with full fp32 products (v_mfma_f32_16x16x4_f32): S^T = K Q^T leaves a row in lane % 16 with keys 4 (lane / 16) + i of every 16.
 // Probabilities in fp32, exponentials as exact as expf.
+// tanh in 20 instructions, good for 3 roundings: (1 - t) / (1 + t) with t = exp(-2 |x|), and below 0.35, where 1 - t cancels, the series to x^11 (what is left
+// out is below 2^-26 of it).
+__device__ __forceinline__ float tanh_of(float x) {
+    const float y = fabsf(x), t = exp_near(fmaxf(-2.0f * y, EXP_NEAR)), d = 1.0f + t, r = __builtin_amdgcn_rcpf(d), n = 1.0f - t, q = n * r;
+    const float big = __builtin_fmaf(__builtin_fmaf(-d, q, n), r, q), z = x * x;
+    float p = -1382.0f / 155925.0f;
+    p = __builtin_fmaf(p, z, 62.0f / 2835.0f);
+    p = __builtin_fmaf(p, z, -17.0f / 315.0f);
+    p = __builtin_fmaf(p, z, 2.0f / 15.0f);
+    p = __builtin_fmaf(p, z, -1.0f / 3.0f);
+    return y < 0.35f ? __builtin_fmaf(p * z, x, x) : x != x ? x : __builtin_copysignf(big, x);
+}
+
 template <int HD>
 __global__ void __launch_bounds__(256, HD >= 128 ? 2 : HD == 64 ? 3 : 4)
 packed_f32_kernel(PackedArgs a) {
@@ -564,12 +731,14 @@ packed_f32_kernel(PackedArgs a) {
     const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane);
     if (!it.any) return;
     const float *kb = (const float*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const float*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
+    constexpr int BQ = PACKED_BQ_F32;
     const int w0 = it.r0 + wave * 16, wl = min(w0 + 15, it.rows - 1), bl = min(it.r0 + PACKED_BQ_F32, it.rows) - 1, row = min(w0 + l16, it.rows - 1);
     const bool mine = w0 < it.rows;
     const int least = mine ? it.reach(a, it.ahead + w0 / a.share) : 0, most = mine ? it.reach(a, it.ahead + wl / a.share) : 0;
     const int tiles_all = (it.keys + KT - 1) / KT, tiles = (it.reach(a, it.ahead + bl / a.share) + KT - 1) / KT;
     const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
     const PackedRow me = packed_query(a, it, row);
+    const float inv_cap = a.cap > 0.f ? 1.0f / a.cap : 0.f;
     f32x4_t qf[NB];
     {
         const float* p = (const float*)a.q + packed_row(a, it, row, a.q_tok, a.q_head);
@@ -626,7 +795,7 @@ packed_f32_kernel(PackedArgs a) {
             }
             if (a.cap > 0.f) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[g][i] = a.cap * tanhf(sc[g][i] / a.cap);
+                for (int i = 0; i < 4; ++i) sc[g][i] = a.cap * tanh_of(sc[g][i] * inv_cap);
             }
             if (a.slopes) {
                 const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + g * 16 + kgrp * 4);
@@ -687,7 +856,7 @@ packed_f32_kernel(PackedArgs a) {
     l = sum_xor32(sum_xor16(l));
     if (w0 + l16 >= it.rows) return;
     if (it.pieces > 1) {
-        float* p = packed_part<HD>(a, it, it.piece, row);
+        float* p = packed_part<BQ, HD>(a, it, it.piece, row);
 #pragma unroll
         for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[d];
         if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{l, m};
@@ -700,17 +869,18 @@ packed_f32_kernel(PackedArgs a) {
 
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
 // takes a block, a wave a row at a time: HD / 4 lanes hold 4 adjacent values each, and the wave's 256 / HD teams of them take a piece each in turn.
-template <typename T, int HD>
+template <typename T, int HD, int BQ>
 __global__ void __launch_bounds__(256)
 packed_join_kernel(PackedArgs a) {
-    constexpr int W = HD / 4, TEAMS = 64 / W, BQ = 64;
+    constexpr int W = HD / 4, TEAMS = 64 / W;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = lane % W * 4, team = lane / W;
-    PackedItem it = packed_item<BQ>(a, lane);
+    const PackedItem it = packed_item<BQ>(a, lane);
     if (!it.any || it.pieces <= 1) return;
+    // (the block's rows are shared among its pieces' workgroups)
     const float c = a.cap > 0.f || a.slopes ? 1.0f : a.scale * PACKED_LOG2E;
-    const long step = (long)it.rows * (HD + 4);
-    for (int r = wave; r < min(BQ, it.rows - it.r0); r += 4) {
-        const float* p = packed_part<HD>(a, it, 0, it.r0 + r);
+    const long step = (long)a.kv_heads * a.part_rows * (HD + 4);
+    for (int r = wave + 4 * it.piece; r < min(BQ, it.rows - it.r0); r += 4 * it.pieces) {
+        const float* p = packed_part<BQ, HD>(a, it, 0, it.r0 + r);
         float top = -INFINITY;
         for (int i = lane; i < it.pieces; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
 #pragma unroll
@@ -740,35 +910,40 @@ packed_join_kernel(PackedArgs a) {
     }
 }
 
-size_t packed_workspace_bytes(const PackedArgs& a) {
-    if (packed_most_pieces(a.own_offsets, a.kv_tokens, a.kv_heads) <= 1) return 0;
-    return (size_t)packed_regions(a.samples, a.kv_tokens) * packed_region_rows(a.q_tokens * a.share, a.kv_heads) * (a.head_dim + 4) * sizeof(float);
+static PackedPlan packed_plan_of(int dtype, const PackedArgs& a) {
+    return packed_plan(dtype == PS_BF16, a.own_offsets, a.samples, a.q_tokens * a.share, a.kv_tokens, a.kv_heads, a.head_dim, compute_units());
+}
+size_t packed_workspace_bytes(int dtype, const PackedArgs& a) {
+    const PackedPlan p = packed_plan_of(dtype, a);
+    return p.table_bytes + p.part_bytes;
 }
 
 template <int HD, int QT>
-static void launch_packed_bf16(const PackedArgs& a, dim3 grid, hipStream_t st) {
+static void launch_packed_bf16(const PackedArgs& a, unsigned grid, hipStream_t st) {
+    if (a.samples > PACKED_SEARCH) packed_table_kernel<128 * QT><<<1, 1024, 0, st>>>(a);
     if (a.cap > 0.f && a.slopes) packed_bf16_kernel<HD, QT, true, true><<<grid, 256, 0, st>>>(a);
     else if (a.cap > 0.f) packed_bf16_kernel<HD, QT, true, false><<<grid, 256, 0, st>>>(a);
     else if (a.slopes) packed_bf16_kernel<HD, QT, false, true><<<grid, 256, 0, st>>>(a);
     else packed_bf16_kernel<HD, QT, false, false><<<grid, 256, 0, st>>>(a);
+    if (a.part) packed_join_kernel<bf16_t, HD, 128 * QT><<<grid, 256, 0, st>>>(a);
 }
 
 template <int HD>
 static hipError_t launch_packed_hd(int dtype, PackedArgs a, hipStream_t st) {
-    const int block = packed_block(dtype == PS_BF16, a.q_tokens * a.share, a.samples, a.kv_heads, HD, compute_units());
-    a.slots = packed_slots(a.q_tokens, a.share, a.samples, block);
-    a.most_pieces = packed_most_pieces(a.own_offsets, a.kv_tokens, a.kv_heads);
-    a.by_sample = packed_regions(a.samples, a.kv_tokens) == a.samples;
-    a.region_rows = packed_region_rows(a.q_tokens * a.share, a.kv_heads);
-    const dim3 grid((unsigned)packed_workgroups(a.slots, a.kv_heads), (unsigned)a.most_pieces);
-    if (dtype != PS_BF16) packed_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
-    else if (HD > 64 || block == 128) launch_packed_bf16<HD, 1>(a, grid, st);
-    else if constexpr (HD <= 64) launch_packed_bf16<HD, 2>(a, grid, st);
-    if (a.most_pieces > 1) {
-        a.slots = packed_slots(a.q_tokens, a.share, a.samples, 64);
-        const unsigned wgs = (unsigned)packed_workgroups(a.slots, a.kv_heads);
-        if (dtype == PS_BF16) packed_join_kernel<bf16_t, HD><<<wgs, 256, 0, st>>>(a);
-        else packed_join_kernel<float, HD><<<wgs, 256, 0, st>>>(a);
+    const PackedPlan p = packed_plan_of(dtype, a);
+    a.slots = p.slots;
+    a.part_rows = p.part_rows;
+    a.table = p.table_bytes ? (int2*)a.scratch : nullptr;
+    a.part = p.part_bytes ? (float*)((char*)a.scratch + p.table_bytes) : nullptr;
+    const unsigned grid = (unsigned)packed_workgroups(p.slots, a.kv_heads);
+    if (dtype != PS_BF16) {
+        if (a.samples > PACKED_SEARCH) packed_table_kernel<PACKED_BQ_F32><<<1, 1024, 0, st>>>(a);
+        packed_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
+        if (a.part) packed_join_kernel<float, HD, PACKED_BQ_F32><<<grid, 256, 0, st>>>(a);
+    } else if (HD > 64 || p.block == 128) {
+        launch_packed_bf16<HD, 1>(a, grid, st);
+    } else if constexpr (HD <= 64) {
+        launch_packed_bf16<HD, 2>(a, grid, st);
     }
     return hipGetLastError();
 }

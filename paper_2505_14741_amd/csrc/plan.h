@@ -427,36 +427,52 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
     return p;
 }
 
-// ---- attention of packed samples (packed_attention.hip): blocks of rows are found on the GPU; what follows is a function of one sample's shape.
-constexpr int PACKED_PIECES = 512;                       // most (key head, piece, block of 128 rows) of a sample that is divided along its keys
-constexpr int PACKED_KEYS = 1280;                        // least keys of such a sample
-constexpr int PACKED_ROWS = 1024;                        // most rows of one; fewer than the keys, so samples that attend to themselves never are
-// Pieces of 256 keys at least, as many as bring the workgroups to two per compute unit of 256.
+// ---- attention of packed samples (packed_attention.hip): a sample's blocks of rows and pieces of its keys are found on the GPU; the host knows the sums
+// over all samples only.
+constexpr int PACKED_SEARCH = 64;                        // most samples that a workgroup looks through itself; more: a table
+constexpr int PACKED_KEYS = 1280;                        // least keys of a sample that is divided
+constexpr int PACKED_FEW_ROWS = 32;                      // rows up to which a workgroup's waves take keys apart instead of rows
+constexpr int PACKED_FEW_KEYS = 1024;                    // least keys of a piece there
+constexpr int PACKED_FEW_MIN = 128;                      // keys from which they do
+constexpr int PACKED_PIECES = 512;                       // workgroups of a round, two per compute unit of 256
+// Pieces of a sample's keys (calls whose keys have offsets of their own), a function of the sample alone.  items: workgroups without.  Few rows: pieces of
+// PACKED_FEW_KEYS keys, one round at most.  Else pieces of 256 keys at least: one round of them where items are a quarter of one; up to two rounds of items, in up to 4
+// pieces, as many as need the least rounds * tiles, a piece's partial sums counted as 8 tiles of 64 keys (1350 rows of 30 heads, 17776 keys).
 constexpr int packed_pieces(int rows, int keys, int kv_heads) {
-    if (rows > PACKED_ROWS || keys < PACKED_KEYS) return 1;
-    const int items = (rows + 127) / 128 * kv_heads, n = PACKED_PIECES / items, most = keys / 256;
-    return n < 2 ? 1 : n < most ? n : most;
+    if (keys < PACKED_KEYS || rows < 1) return 1;
+    const int items = (rows + 127) / 128 * kv_heads;
+    if (rows <= PACKED_FEW_ROWS || items <= PACKED_PIECES / 4) {
+        const int n = PACKED_PIECES / items, most = keys / (rows <= PACKED_FEW_ROWS ? PACKED_FEW_KEYS : 256);
+        return n < most ? (n < 1 ? 1 : n) : most < 1 ? 1 : most;
+    }
+    if (items >= 2 * PACKED_PIECES) return 1;
+    const int tiles = (keys + 63) / 64;
+    int best = 1, least = (items + PACKED_PIECES - 1) / PACKED_PIECES * tiles;
+    for (int n = 2; n <= 4; ++n) {
+        const int cost = (items * n + PACKED_PIECES - 1) / PACKED_PIECES * ((tiles + n - 1) / n + 8);
+        if (cost < least) { least = cost; best = n; }
+    }
+    return best;
 }
-// bounds over all samples, of which the host knows the sums only
-constexpr int packed_most_pieces(bool keys_of_their_own, int kv_tokens, int kv_heads) {
-    if (!keys_of_their_own || kv_tokens < PACKED_KEYS) return 1;
-    const int n = PACKED_PIECES / kv_heads, most = kv_tokens / 256;
-    return n < 2 ? 1 : n < most ? n : most;
+// block: rows of a workgroup (bf16, heads up to 64: 256 where that leaves two workgroups for each compute unit; a row's result does not depend on it); slots:
+// the most workgroups of a key head; scratch: a table of the slots, and a block of partial sums for each slot and key head
+struct PackedPlan { int block, slots, part_rows; size_t table_bytes, part_bytes; };
+constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int kv_heads, int block) {
+    const long blocks = rows / block + samples;
+    if (!own || kv_tokens < PACKED_KEYS) return blocks;
+    const int divided = kv_tokens / PACKED_KEYS;         // samples that can be
+    return 4 * blocks + (samples < divided ? samples : divided) * (long)(PACKED_PIECES / kv_heads) * (block < 128 ? 2 : 1);
 }
-// scratch rows of a sample that is divided: rows * key heads * pieces
-constexpr long packed_region_rows(int rows, int kv_heads) { return (long)PACKED_PIECES * (rows < 128 ? rows : 128); }
-// rows of a workgroup (bf16, heads up to 64: 256 where that leaves two workgroups for each compute unit; a row's result does not depend on it)
-constexpr int packed_block(bool bf16, int rows, int samples, int kv_heads, int head_dim, int cus) {
-    if (!bf16) return 64;
-    return head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 2L * cus ? 256 : 128;
-}
-constexpr int packed_slots(int q_tokens, int share, int samples, int block) { return (int)((long)q_tokens * share / block) + samples; }
 // a workgroup for each slot, up to a multiple of 8, and key head
-constexpr long packed_workgroups(int slots, int kv_heads) { return (slots + 7L) / 8 * 8 * kv_heads; }
-// regions of scratch: one per sample, or per PACKED_KEYS keys, in which at most one divided sample begins
-constexpr int packed_regions(int samples, int kv_tokens) {
-    const int n = kv_tokens / PACKED_KEYS + 1;
-    return samples < n ? samples : n;
+constexpr long packed_workgroups(long slots, int kv_heads) { return (slots + 7) / 8 * 8 * kv_heads; }
+constexpr PackedPlan packed_plan(bool bf16, bool own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, int cus) {
+    PackedPlan p{};
+    p.block = !bf16 ? 64 : head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 2L * cus ? 256 : 128;
+    p.slots = (int)packed_slots(own, samples, rows, kv_tokens, kv_heads, p.block);
+    p.part_rows = rows < p.block ? rows : p.block;
+    if (samples > PACKED_SEARCH) p.table_bytes = ((size_t)p.slots + 1) * 8 / 256 * 256 + 256;
+    if (own && kv_tokens >= PACKED_KEYS) p.part_bytes = (size_t)p.slots * kv_heads * p.part_rows * (head_dim + 4) * sizeof(float);
+    return p;
 }
 
 // ---- group norm: `slices` slices of slice_groups whole groups (the last may have fewer), each over `chunks` chunks of positions.

@@ -1,10 +1,14 @@
 """Operators of self-attention on packed samples: what they refuse, on the host and before any launch, and the rules that divide their work."""
 import ctypes as C
+import os
+import random
+import subprocess
 
 import pytest
 import torch
 
 from paper_2505_14741_amd import binding as B
+from paper_2505_14741_amd import build
 
 FAKE = 0x10000                                                   # never dereferenced: every call below is refused or has nothing to do
 
@@ -120,17 +124,114 @@ def test_packed_attention_refuses_pointers():
 
 
 def test_packed_attention_workspace():
-    """Only keys with offsets of their own may be divided; a missing, small or misaligned workspace is refused; its size follows the samples and keys."""
+    """Keys with offsets of their own may be divided, and more than 64 samples need a table; a missing, small or misaligned workspace is refused."""
     bytes_of = lambda **kw: B.lib().packed_attn_workspace_bytes(C.byref(packed_shape(**kw)))  # noqa: E731
-    assert bytes_of() == 0 and bytes_of(q_tokens=17776, kv_tokens=17776) == 0
+    assert bytes_of() == 0 and bytes_of(q_tokens=17776, kv_tokens=17776) == 0 and bytes_of(samples=64) == 0
+    table = bytes_of(samples=65)
+    assert table >= 66 * 8 and table % 256 == 0
     one = dict(samples=1, q_tokens=1, kv_tokens=17776, own_offsets=1)
     n = bytes_of(**one)
-    assert n >= 512 * 2 * 68 * 4 and n % 256 == 0
+    assert n >= 17 * 2 * 2 * 68 * 4 and n % 256 == 0                     # 17 pieces of two query heads for each of two key heads
     assert bytes_of(**dict(one, kv_tokens=1279)) == 0
-    assert bytes_of(**dict(one, samples=8, q_tokens=8)) == 8 * 8 * n     # 8 regions of up to 8 tokens' rows
-    assert bytes_of(**dict(one, samples=1000)) == 14 * n                 # of 1280 keys each at least
     s = packed_shape(**one)
     assert call_packed(s, ko=6 * FAKE) == -4 and call_packed(s, ko=6 * FAKE, ws=7 * FAKE, nb=n - 1) == -4 and call_packed(s, ko=6 * FAKE, ws=7 * FAKE + 128, nb=n) == -4
+    assert call_packed(packed_shape(samples=65)) == -4 and call_packed(packed_shape(samples=65), ws=7 * FAKE, nb=table - 256) == -4
+
+
+RULES = """
+#include "plan.h"
+extern "C" int pieces(int rows, int keys, int kv_heads) { return ps::packed_pieces(rows, keys, kv_heads); }
+extern "C" void plan(int bf16, int own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, long* out) {
+    const ps::PackedPlan p = ps::packed_plan(bf16 != 0, own != 0, samples, rows, kv_tokens, kv_heads, head_dim, 256);
+    out[0] = p.block; out[1] = p.slots; out[2] = p.part_rows; out[3] = (long)p.table_bytes; out[4] = (long)p.part_bytes; out[5] = ps::packed_workgroups(p.slots, kv_heads);
+}
+extern "C" void fp4(int m, int n, int blocks, int split, int* out) {
+    const ps::Fp4Plan p = ps::fp4_plan(m, n, blocks, split != 0, 256);
+    out[0] = p.tile; out[1] = p.pieces; out[2] = ps::kFp4Tiles[p.tile].bm; out[3] = ps::kFp4Tiles[p.tile].bn;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("packed_rules")
+    src, lib = os.path.join(d, "rules.cpp"), os.path.join(d, "rules.so")
+    with open(src, "w") as f:
+        f.write(RULES)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", build.CSRC, src, "-o", lib], check=True)
+    return C.CDLL(lib)
+
+
+def test_packed_attention_slots_hold_every_block_and_piece(rules):
+    """Samples of any lengths have slots enough, scratch for each, and launches below 2^32 threads; pieces are not empty."""
+    r = random.Random(1)
+    log = lambda lo, hi: int(round(lo * (hi / lo) ** r.random()))  # noqa: E731
+    out = (C.c_long * 6)()
+    for _ in range(4000):
+        kv_heads, share = r.choice([1, 2, 6, 30, 64, 200, 600]), r.choice([1, 1, 5, 8])
+        n = r.choice([1, 1, 2, 8, 70, 300])
+        own = r.random() < 0.7
+        q = [log(1, 30000) if r.random() < 0.3 else r.randint(0, 40) for _ in range(n)]
+        k = [log(1, 60000) if r.random() < 0.6 else r.randint(0, 2000) for _ in range(n)] if own else q
+        rows, kv = sum(q) * share, sum(k)
+        if (rows // 64 + n) * kv_heads > (1 << 19 if own else 1 << 23):
+            continue
+        for bf16, d in ((1, 64), (1, 128), (0, 32)):
+            rules.plan(bf16, own, n, rows, kv, kv_heads, d, out)
+            block, slots, part_rows, table, part, wgs = list(out)
+            used = 0
+            for a, b in zip(q, k):
+                p = rules.pieces(a * share, b, kv_heads) if own else 1
+                assert 1 <= p and (p == 1 or (b >= 1280 and p <= b // 256 and part > 0))
+                used += -(-a * share // block) * p
+            assert used <= slots and part_rows == min(rows, block)
+            assert wgs >= slots * kv_heads and wgs < 1 << 24
+            assert table >= (8 * (slots + 1) if n > 64 else 0) and table % 256 == 0
+            assert part == (slots * kv_heads * part_rows * (d + 4) * 4 if own and kv >= 1280 else 0)
+
+
+def test_packed_attention_launches_are_below_the_limit(rules):
+    """The largest calls that are not refused: samples of 1280 keys each, or rows without end."""
+    out = (C.c_long * 6)()
+    for kv_heads in (1, 2, 8, 64, 512):
+        for n in (1, 100, 13107, 65535):
+            for own in (0, 1):
+                rows = min(64 * (((1 << 19) if own else (1 << 23)) // kv_heads - n), 1 << 30)
+                if rows < 1:
+                    continue
+                for bf16 in (0, 1):
+                    rules.plan(bf16, own, n, rows, 1 << 24, kv_heads, 16, out)
+                    assert out[5] < 1 << 24, (kv_heads, n, own, bf16)
+
+
+def test_packed_attention_places_cover_every_head_and_slot():
+    """Workgroup id -> (key head, slot), as the kernel computes it: every pair once, whatever the number of heads."""
+    for kv_heads in (1, 2, 6, 7, 8, 9, 30, 64, 100):
+        for slots in (8, 16, 72):
+            seen = set()
+            for wg in range(slots * kv_heads):
+                x, n, own, rest = wg & 7, wg >> 3, kv_heads // 8, kv_heads % 8
+                period, i = divmod(n, kv_heads)
+                if i < 8 * own:
+                    seen.add((x * own + i % own, period * 8 + i // own))
+                else:
+                    u = (period * rest + i - 8 * own) * 8 + x
+                    seen.add((8 * own + u % rest, u // rest))
+            assert seen == {(g, s) for g in range(kv_heads) for s in range(slots)}
+
+
+def test_4_bit_product_plans(rules):
+    r = random.Random(2)
+    out = (C.c_int * 4)()
+    sizes = [(1, 1, 1), (112, 7680, 15), (17776, 5760, 15), (1 << 24, 64, 1), (1, 1 << 24, 4), (60, 100, 32768)]
+    sizes += [(int(2 ** r.uniform(0, 16)), int(2 ** r.uniform(0, 14)), int(2 ** r.uniform(0, 10))) for _ in range(4000)]
+    for m, n, blocks in sizes:
+        for split in (0, 1):
+            rules.fp4(m, n, blocks, split, out)
+            tile, pieces, bm, bn = list(out)
+            assert 0 <= tile < 5 and 1 <= pieces and bm <= 256 and bn <= 256
+            if pieces > 1:                                               # 4 stages of 256 at least, a round of workgroups at most
+                assert split and 8 * pieces <= blocks and -(-m // bm) * -(-n // bn) * pieces <= 512
 
 
 def test_binding_refuses_tensors():
