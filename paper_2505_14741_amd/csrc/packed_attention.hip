@@ -223,22 +223,25 @@ __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
 }
 
+enum PackedFrames { PACKED_ONE, PACKED_EACH, PACKED_ANY };
+
 template <int HD, int QT, bool CAP, bool BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
+    static constexpr int SLOTS = 3;                                  // tiles of K, and of V, in LDS (four, requested a tile earlier: as fast)
     static constexpr int NB = HD < 32 ? 1 : HD / 32, QS = HD / 16, ROW = HD * 2, TILE = U * ROW;
     static constexpr int LOADS = 2 * TILE / 1024 / 4;                // 1 KB loads per wave: K's by the first waves, V's by the others
     static_assert(LOADS * 4 * 1024 == 2 * TILE, "every wave requests as many");
 
     const PackedArgs& a;
     const PackedItem& it;
-    unsigned char *const kl, *const vl;                              // three tiles each
-    float* const fl;                                                 // frames of three tiles' keys
+    unsigned char *const kl, *const vl;                              // SLOTS tiles each
+    float* const fl;                                                 // frames of their keys
     const bf16_t *kb, *vb;
     int lane, wave, l32, hi;
     PackedRow me[QT];
-    float c0, cap2, into, m[QT], mc[QT];                             // m: the reference, a score (capped or biased: in powers of two); mc: in powers of two
-    int koff[QS], voff[NB];
+    float c0, cap2, into, m[QT], mc[QT], ref[QT];                    // m: the reference, a score (capped or biased: in powers of two); mc: in powers of two; ref: see refer()
+    int koff[QS], voff[NB], now, now_end;
     bf16x8_t qf[QT][QS];
     f32x16_t acc[QT][NB];
     float l[QT];                                                     // of the lane's keys
@@ -248,7 +251,7 @@ struct PackedBf16 {
     __device__ __forceinline__ static int v_place(int r) { return HD <= 32 ? 0 : HD == 64 ? (r & 3) | (r & 2) << 1 : (r & 3) << 2; }
 
     __device__ __forceinline__ PackedBf16(const PackedArgs& a_, const PackedItem& it_, unsigned char* lds, float* frames)
-        : a(a_), it(it_), kl(lds), vl(lds + 3 * TILE), fl(frames) {}
+        : a(a_), it(it_), kl(lds), vl(lds + SLOTS * TILE), fl(frames) {}
 
     __device__ __forceinline__ void start(int w0) {
         kb = (const bf16_t*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head;
@@ -328,14 +331,28 @@ struct PackedBf16 {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < left ? s[i] : -INFINITY;
     }
-    // whether the half's keys are all in the prefix, or all in one frame: a row's bias is one number
-    __device__ __forceinline__ bool one_frame(int kv0, float& frame) const {
-        frame = __uint_as_float(0x7fc00000u);
-        if (kv0 + 32 <= it.prefix) return true;
-        if (kv0 < it.prefix || a.frame < 32) return false;
-        const unsigned n = (unsigned)(kv0 - it.prefix), f = frame_of(n, (unsigned)a.frame, it.inv_frame);
-        frame = (float)f;
-        return uniform((int)(n + 31 - f * (unsigned)a.frame < (unsigned)a.frame)) != 0;
+    // The frame of the keys at hand (-1: the prefix) and where it ends; keys come in order.  Those that lie there have one bias for each row: ref is
+    // the reference and it.
+    __device__ __forceinline__ void first_frame(int kv0) {
+        now = kv0 < it.prefix ? -1 : uniform((int)frame_of((unsigned)(kv0 - it.prefix), (unsigned)a.frame, it.inv_frame));
+        now_end = (int)min((long)it.prefix + (long)(now + 1) * a.frame, 1L << 30);
+    }
+    __device__ __forceinline__ void refer() {
+#pragma unroll
+        for (int q = 0; q < QT; ++q) ref[q] = BIAS && now >= 0 ? __builtin_fmaf(me[q].slope, fabsf(me[q].frame - (float)now), mc[q]) : mc[q];
+    }
+    // whether keys kv0 .. kv0 + n - 1 lie in one frame, or in the prefix (frames of fewer than 64: no)
+    __device__ __forceinline__ bool one_frame(int kv0, int n) {
+        if (!BIAS) return true;
+        if (a.frame < 64) return kv0 + n <= it.prefix;
+        if (kv0 >= now_end) {
+            while (kv0 >= now_end) {
+                ++now;
+                now_end = (int)min((long)now_end + a.frame, 1L << 30);
+            }
+            refer();
+        }
+        return kv0 + n <= now_end;
     }
     __device__ __forceinline__ static float largest(const f32x16_t& s) {
         float top = s[0];
@@ -343,39 +360,29 @@ struct PackedBf16 {
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         return max_xor32(top);
     }
-    // Weights 2^(x - ref) of a half, rounded to bf16 for the second product.  The same arithmetic whether some keys are not seen (CUT) or not.
-    template <bool CUT>
-    __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], const float (&ref)[QT], int kv0, const float* of) const {
-        float frame = 0.f;
-        const bool one = !BIAS || one_frame(kv0, frame);             // (uniform)
+    // Weights 2^(x - reference - bias) of a half, rounded to bf16 for the second product; the same numbers whichever way their keys' frames are looked at
+    // (PACKED_ONE: one_frame(); PACKED_EACH: each key's, none in the prefix; PACKED_ANY) and whether some keys are not seen by some rows (CUT) or not.
+    template <bool CUT, int FRAMES>
+    __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], int kv0, const float* of) const {
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             f32x16_t& x = s[q];
-            float r = ref[q], c = c0;
+            const float c = CAP ? 1.0f : c0;
             if constexpr (CAP) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = capped(x[i]);
-                c = 1.0f;
-            }
-            if (BIAS && one) r += packed_bias(me[q], frame);
-            if (BIAS && !one) {
-                const float* f = of + 4 * hi;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] *= c;
-                if (kv0 >= it.prefix) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-me[q].slope, fabsf(me[q].frame - f[8 * (i / 4) + i % 4]), x[i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] -= packed_bias(me[q], f[8 * (i / 4) + i % 4]);
-                }
-                c = 1.0f;
             }
             if constexpr (CUT) cut(x, q, kv0);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pf[q][y][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[y * 8 + e], c, -r));
+            for (int i = 0; i < 16; ++i) {
+                float r = ref[q];
+                if constexpr (FRAMES != PACKED_ONE) {
+                    const float far = fabsf(me[q].frame - of[4 * hi + 8 * (i / 4) + i % 4]);
+                    r = __builtin_fmaf(me[q].slope, far, mc[q]);
+                    if constexpr (FRAMES == PACKED_ANY) r = far == far ? r : mc[q];
+                }
+                pf[q][i / 8][i % 8] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -r));
+            }
         }
     }
     // acc += V^T P^T, l += the weights as they were rounded (one key alone has weight 1 exactly).
@@ -458,7 +465,8 @@ struct PackedBf16 {
 
     // Few rows (PACKED_FEW_ROWS): memory binds, and the waves take every fourth half of the keys each, through slots of their own and without a barrier; their
     // sums are united behind the last key, in the first wave's registers.
-    static constexpr int FEW_SLOTS = HD > 64 ? 1 : 2, FEW_LOADS = 32 * ROW / 1024, FEW_HALF = 32 * ROW, FEW_BYTES = 4 * FEW_SLOTS * 2 * FEW_HALF;
+    static constexpr int FEW_UNITS = HD > 64 ? 2 : 3, FEW_LOADS = 32 * ROW / 1024, FEW_HALF = 32 * ROW, FEW_BYTES = 4 * FEW_UNITS * FEW_HALF;
+    static constexpr int MOST = 2 * SLOTS * TILE > FEW_BYTES ? 2 * SLOTS * TILE : FEW_BYTES, SUMS = 3 * (NB * 16 + 2) * 256, LDS_BYTES = MOST > SUMS ? MOST : SUMS;
     __device__ __forceinline__ void request_half(int h, unsigned char* to, bool of_k) {
 #pragma unroll
         for (int i = 0; i < FEW_LOADS; ++i) {
@@ -468,42 +476,38 @@ struct PackedBf16 {
         }
     }
     __device__ __forceinline__ void few(int first, int end) {        // halves first .. end - 1
-        constexpr int L = FEW_LOADS, NS = FEW_SLOTS;
-        unsigned char* const own = kl + wave * NS * 2 * FEW_HALF;    // [slot][keys | values]
+        // Units of a wave in turn: keys, values, keys of the next half, ...; each is requested again as soon as it has been read.
+        constexpr int L = FEW_LOADS, N3 = FEW_UNITS == 3;
+        unsigned char* const own = kl + wave * FEW_UNITS * FEW_HALF;
         float* const of = fl + wave * 32;
         const int h0 = first + wave;
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-            if (h0 + 4 * n < end) {
-                request_half(h0 + 4 * n, own + n * 2 * FEW_HALF, true);
-                request_half(h0 + 4 * n, own + n * 2 * FEW_HALF + FEW_HALF, false);
-            }
-        int slot = 0;
+        if (h0 < end) {
+            request_half(h0, own, true);
+            request_half(h0, own + FEW_HALF, false);
+            if (N3 && h0 + 4 < end) request_half(h0 + 4, own + 2 * FEW_HALF, true);
+        }
+        int u = 0;                                       // the keys' unit
         for (int h = h0; h < end; h += 4) {
-            unsigned char *const ks = own + slot * 2 * FEW_HALF, *const vs = ks + FEW_HALF;
-            const bool more = h + 4 < end;               // (with two slots: its loads are out)
-            if (NS == 2 && more) wait_loads<3 * L>(); else wait_loads<L>();
+            const int uv = u + 1 == FEW_UNITS ? 0 : u + 1;
+            unsigned char *const ks = own + u * FEW_HALF, *const vs = own + uv * FEW_HALF;
+            const bool more = h + 4 < end;
+            if (N3 && more) wait_loads<2 * L>(); else wait_loads<L>();
             f32x16_t s[1];
             bf16x8_t pf[1][2];
             scores<1>(s, ks);
             if (BIAS && lane < 32) of[lane] = packed_frame(a, it, h * 32 + lane);
             wait_lds();
-            if (NS == 1 && more) request_half(h + 4, ks, true);
+            if (more) request_half(h + 4, ks, !N3);      // the next values, or (of two units) the next keys
             tracked<1>(s, pf, h * 32, of);
-            if (more) wait_loads<(NS == 2 ? 2 : 1) * L>(); else wait_loads<0>();
+            if (more) wait_loads<(N3 ? 2 : 1) * L>(); else wait_loads<0>();
             values<true, 1>(pf, h * 32, vs);
             wait_lds();
-            if (NS == 1 && more) request_half(h + 4, vs, false);
-            if (NS == 2 && h + 8 < end) {
-                request_half(h + 8, ks, true);
-                request_half(h + 8, vs, false);
-            }
-            slot = NS == 2 ? slot ^ 1 : 0;
+            if (N3 ? h + 8 < end : more) request_half(N3 ? h + 8 : h + 4, vs, N3);
+            u = N3 ? (uv + 1 == FEW_UNITS ? 0 : uv + 1) : 0;
         }
         __syncthreads();                                 // (nobody reads its slots any more)
         float* const sums = reinterpret_cast<float*>(kl);            // [wave - 1][value][lane]
         constexpr int N = NB * 16 + 2;
-        static_assert(3 * N * 64 * 4 <= FEW_BYTES, "scratch");
         if (wave > 0) {
             float* to = sums + (wave - 1) * N * 64 + lane;
 #pragma unroll
@@ -540,12 +544,12 @@ struct PackedBf16 {
 };
 
 template <int HD, int QT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, QT == 1 && HD <= 64 && !BIAS ? 3 : 2)
 packed_bf16_kernel(PackedArgs a) {
     typedef PackedBf16<HD, QT, CAP, BIAS> P;
     constexpr int U = P::U, NB = P::NB, HALVES = P::HALVES, BQ = 128 * QT;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[6 * P::TILE > P::FEW_BYTES ? 6 * P::TILE : P::FEW_BYTES];
-    __shared__ float fl[BIAS ? (3 * U > 128 ? 3 * U : 128) : 1];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[P::LDS_BYTES];
+    __shared__ float fl[BIAS ? (P::SLOTS * U > 128 ? P::SLOTS * U : 128) : 1];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l32 = lane & 31;
     const PackedItem it = packed_item<BQ>(a, lane);
     if (!it.any) return;                                 // (the whole workgroup)
@@ -597,14 +601,20 @@ packed_bf16_kernel(PackedArgs a) {
     }
     f32x16_t s[2][QT];
     bf16x8_t pf[2][QT][2];
+    if constexpr (BIAS) {
+        t.frames(j0, 0);
+        t.first_frame(j0 * U);
+    }
+    constexpr int SLOTS = P::SLOTS;
     t.request(j0, 0, -1, 0, j1);
     t.request(j0 + 1, 1, j0, 0, j1);
-    t.frames(j0, 0);
     // One tile.  Per half h (of all the sample's; parity X): the scores of the next one, this one's weights, the last one's values.
-    // STEADY: all rows of the workgroup see the whole tile, which is neither the first nor the last.
+    // Kinds: PACKED_ONE, all rows of the workgroup see the whole tile, which lies in one frame and is neither the first nor the last; PACKED_EACH, the same
+    // behind the prefix with any frames; PACKED_ANY.
     int slot = 0;
-    auto tile = [&](int j, auto x_c, auto steady_c) {
-        constexpr bool STEADY = decltype(steady_c)::value;
+    auto tile = [&](int j, auto x_c, auto kind_c) {
+        constexpr int FRAMES = BIAS ? decltype(kind_c)::value : PACKED_ONE;
+        constexpr bool STEADY = decltype(kind_c)::value != PACKED_ANY;
         wait_loads<0>();                                // K of the next tile, V of this one
         __syncthreads();                                 // ... everyone's; and nobody reads the last tile's K and the one before's V any more
         const int up = slot == 2 ? 0 : slot + 1, down = slot == 0 ? 2 : slot - 1;
@@ -617,7 +627,7 @@ packed_bf16_kernel(PackedArgs a) {
             const int next = half + 1 < HALVES ? slot : up, last = half > 0 ? slot : down, next_half = half + 1 < HALVES ? half + 1 : 0, last_half = half > 0 ? half - 1 : HALVES - 1;
             if constexpr (STEADY) {
                 t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
-                t.template weights<false>(s[X], pf[X], t.mc, kv0, t.frames_at(slot, half));
+                t.template weights<false, FRAMES>(s[X], pf[X], kv0, t.frames_at(slot, half));
                 t.template values<false, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
             } else {
                 if (h + 1 < min(end, j1 * HALVES)) t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
@@ -631,8 +641,9 @@ packed_bf16_kernel(PackedArgs a) {
                             t.m[q] = top == -INFINITY ? top : CAP ? t.capped(top) : BIAS ? top * t.c0 : top;
                             t.mc[q] = top == -INFINITY ? 0.f : CAP || BIAS ? t.m[q] : top * t.c0;
                         }
+                        t.refer();
                     }
-                    t.template weights<true>(s[X], pf[X], t.mc, kv0, t.frames_at(slot, half));
+                    t.template weights<true, FRAMES>(s[X], pf[X], kv0, t.frames_at(slot, half));
                 }
                 if (h > j0 * HALVES && h - 1 < end) t.template values<true, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
             }
@@ -641,26 +652,33 @@ packed_bf16_kernel(PackedArgs a) {
     };
     const std::integral_constant<int, 0> c0;
     const std::integral_constant<int, 1> c1;
-    const std::true_type steady;
-    const std::false_type general;
+    const std::integral_constant<int, PACKED_ONE> steady;
+    const std::integral_constant<int, PACKED_EACH> each;
+    const std::integral_constant<int, PACKED_ANY> general;
     const int all_see = it.reach(a, it.ahead + it.r0 / a.share);         // what the block's first row sees
     int j = j0;
     if constexpr (HALVES == 2) {
         do {
             tile(j++, c0, general);
-            for (; j + 1 < j1 && (j + 1) * U <= all_see; ++j) tile(j, c0, steady);
+            for (; j + 1 < j1 && (j + 1) * U <= all_see && t.one_frame(j * U, U); ++j) tile(j, c0, steady);
+            if constexpr (BIAS)
+                if (a.frame < 64)
+                    for (; j + 1 < j1 && (j + 1) * U <= all_see && j * U >= it.prefix; ++j) tile(j, c0, each);
         } while (j < j1);
     } else {
         tile(j++, c0, general);
         while (j < j1) {
-            for (; j + 2 < j1 && (j + 2) * U <= all_see; j += 2) { tile(j, c1, steady); tile(j + 1, c0, steady); }
+            for (; j + 2 < j1 && (j + 2) * U <= all_see && t.one_frame(j * U, 2 * U); j += 2) { tile(j, c1, steady); tile(j + 1, c0, steady); }
+            if constexpr (BIAS)
+                if (a.frame < 64)
+                    for (; j + 2 < j1 && (j + 2) * U <= all_see && j * U >= it.prefix; j += 2) { tile(j, c1, each); tile(j + 1, c0, each); }
             tile(j++, c1, general);
             if (j < j1) tile(j++, c0, general);
         }
     }
     const int h = j1 * HALVES;                           // the last half's values
     if (h - 1 < end) {
-        const int last = slot == 0 ? 2 : slot - 1;
+        const int last = slot == 0 ? SLOTS - 1 : slot - 1;
         if (HALVES == 2 || ((h - 1 - j0) & 1)) t.template values<true, QT>(pf[1], (h - 1) * 32, t.values_at(last, HALVES - 1));
         else t.template values<true, QT>(pf[0], (h - 1) * 32, t.values_at(last, HALVES - 1));
     }
@@ -722,17 +740,15 @@ __device__ __forceinline__ float tanh_of(float x) {
     return y < 0.35f ? __builtin_fmaf(p * z, x, x) : x != x ? x : __builtin_copysignf(big, x);
 }
 
-template <int HD>
-__global__ void __launch_bounds__(256, HD >= 128 ? 2 : HD == 64 ? 3 : 4)
-packed_f32_kernel(PackedArgs a) {
-    constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256;
-    __shared__ __attribute__((aligned(16))) float Ks[KT * LD], Vs[KT * LD], Fs[KT];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, kgrp = lane >> 4;
-    const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane);
-    if (!it.any) return;
+// APART: the workgroup takes 16 rows (of the block's 64, those of blockIdx.y), each wave a quarter of every tile's keys, and the waves' sums are united
+// behind the last key: where a sample has too few rows to fill the chip, a quarter of the steps behind each other.
+template <int HD, bool APART>
+__device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave) {
+    constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256, BQ = PACKED_BQ_F32, NG = APART ? 1 : 4;
+    const int l16 = lane & 15, kgrp = lane >> 4, g0 = APART ? wave : 0;              // g0: the wave's first 16 keys of a tile
     const float *kb = (const float*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const float*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
-    constexpr int BQ = PACKED_BQ_F32;
-    const int w0 = it.r0 + wave * 16, wl = min(w0 + 15, it.rows - 1), bl = min(it.r0 + PACKED_BQ_F32, it.rows) - 1, row = min(w0 + l16, it.rows - 1);
+    const int w0 = it.r0 + 16 * (APART ? (int)blockIdx.y : wave), wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
+    const int bl = APART ? wl : min(it.r0 + BQ, it.rows) - 1;        // the workgroup's last row
     const bool mine = w0 < it.rows;
     const int least = mine ? it.reach(a, it.ahead + w0 / a.share) : 0, most = mine ? it.reach(a, it.ahead + wl / a.share) : 0;
     const int tiles_all = (it.keys + KT - 1) / KT, tiles = (it.reach(a, it.ahead + bl / a.share) + KT - 1) / KT;
@@ -776,19 +792,20 @@ packed_f32_kernel(PackedArgs a) {
         if (a.slopes && threadIdx.x < KT) Fs[threadIdx.x] = fn;
         __syncthreads();
         if (j + 1 < j1) fetch(kv0 + KT);
-        if (kv0 >= most) continue;
-        const int blocks = min(4, (most - kv0 + 15) / 16);           // 16-key blocks that some row of the wave sees
-        const bool cut = kv0 + KT > least;
-        const int left = me.reach - kv0 - 4 * kgrp;
-        f32x4_t sc[4];
+        const int k0 = kv0 + g0 * 16;                    // the wave's keys
+        if (k0 >= most) continue;
+        const int blocks = min(NG, (most - k0 + 15) / 16);           // 16-key blocks that some row of the wave sees
+        const bool cut = k0 + 16 * NG > least;
+        const int left = me.reach - k0 - 4 * kgrp;
+        f32x4_t sc[NG];
         float top = -INFINITY, low = INFINITY;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < NG; ++g) {
             sc[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             if (g < blocks) {
 #pragma unroll
                 for (int d = 0; d < NB; ++d) {
-                    const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + (g * 16 + l16) * LD + d * 16 + kgrp * 4);
+                    const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + ((g0 + g) * 16 + l16) * LD + d * 16 + kgrp * 4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[d][e], sc[g], 0, 0, 0);
                 }
@@ -798,7 +815,7 @@ packed_f32_kernel(PackedArgs a) {
                 for (int i = 0; i < 4; ++i) sc[g][i] = a.cap * tanh_of(sc[g][i] * inv_cap);
             }
             if (a.slopes) {
-                const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + g * 16 + kgrp * 4);
+                const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + (g0 + g) * 16 + kgrp * 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sc[g][i] -= packed_bias(me, f[i]);
             }
@@ -821,7 +838,7 @@ packed_f32_kernel(PackedArgs a) {
         const bool near = __ballot(low - ref < EXP_NEAR) == 0;       // (of the whole wave; not with keys that a row does not see)
         bool odd = false;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < NG; ++g) {
             if (g >= blocks) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) sc[g][i] = near ? exp_near(sc[g][i] - ref) : expf(sc[g][i] - ref);
@@ -831,7 +848,7 @@ packed_f32_kernel(PackedArgs a) {
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int d = 0; d < NB; ++d) {
-                    float x = Vs[(g * 16 + kgrp * 4 + e) * LD + d * 16 + l16];
+                    float x = Vs[((g0 + g) * 16 + kgrp * 4 + e) * LD + d * 16 + l16];
                     if (cut) {                           // (as in the bf16 kernel)
                         const bool o = !(fabsf(x) < INFINITY);
                         odd = odd || o;
@@ -841,19 +858,54 @@ packed_f32_kernel(PackedArgs a) {
                 }
         }
         if (cut && __any(odd)) {
-            for (int key = 0; key < min(KT, it.keys - kv0); ++key) {
-                if (kv0 + key >= me.reach) continue;
+#pragma unroll 1
+            for (int key = 0; key < min(16 * NG, it.keys - k0); ++key) {
+                if (k0 + key >= me.reach) continue;
 #pragma unroll
                 for (int d = 0; d < NB; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = Vs[key * LD + d * 16 + 4 * kgrp + i];
+                        const float x = Vs[(g0 * 16 + key) * LD + d * 16 + 4 * kgrp + i];
                         if (!(fabsf(x) < INFINITY)) acc[d][i] += x;
                     }
             }
         }
     }
     l = sum_xor32(sum_xor16(l));
+    if constexpr (APART) {
+        constexpr int N = NB * 4 + 2;                    // [wave - 1][value][lane]
+        static_assert(3 * N * 64 <= 2 * KT * LD, "scratch");
+        __syncthreads();
+        if (wave > 0) {
+            float* to = Ks + (wave - 1) * N * 64 + lane;
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[(d * 4 + i) * 64] = acc[d][i];
+            to[(N - 2) * 64] = l;
+            to[(N - 1) * 64] = m;
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        float top = m;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) top = fmaxf(top, Ks[(w * N + N - 1) * 64 + lane]);
+        const float ref = top == -INFINITY ? 0.f : top, f0 = expf(m - ref);
+        m = top;
+        l *= f0;
+#pragma unroll
+        for (int d = 0; d < NB; ++d) acc[d] *= f0;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) {
+            const float* from = Ks + w * N * 64 + lane;
+            const float f = expf(from[(N - 1) * 64] - ref);
+            l = __builtin_fmaf(from[(N - 2) * 64], f, l);
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[d][i] = __builtin_fmaf(from[(d * 4 + i) * 64], f, acc[d][i]);
+        }
+    }
     if (w0 + l16 >= it.rows) return;
     if (it.pieces > 1) {
         float* p = packed_part<BQ, HD>(a, it, it.piece, row);
@@ -865,6 +917,21 @@ packed_f32_kernel(PackedArgs a) {
     float* p = (float*)a.o + packed_row(a, it, row, a.o_tok, a.o_head) + kgrp * 4;
 #pragma unroll
     for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16) = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc[d] / l;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(256, HD >= 128 ? 2 : HD == 64 ? 3 : 4)
+packed_f32_kernel(PackedArgs a) {
+    constexpr int KT = 64, LD = HD + 4;
+    __shared__ __attribute__((aligned(16))) float lds[2 * KT * LD], Fs[KT];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane);
+    if (!it.any) return;                                 // (the whole workgroup)
+    if (packed_apart(it.rows, it.pieces, a.kv_heads)) {
+        if (it.r0 + 16 * (int)blockIdx.y < it.rows) packed_f32_rows<HD, true>(a, it, lds, lds + KT * LD, Fs, lane, wave);
+    } else if (blockIdx.y == 0) {
+        packed_f32_rows<HD, false>(a, it, lds, lds + KT * LD, Fs, lane, wave);
+    }
 }
 
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
@@ -938,7 +1005,7 @@ static hipError_t launch_packed_hd(int dtype, PackedArgs a, hipStream_t st) {
     const unsigned grid = (unsigned)packed_workgroups(p.slots, a.kv_heads);
     if (dtype != PS_BF16) {
         if (a.samples > PACKED_SEARCH) packed_table_kernel<PACKED_BQ_F32><<<1, 1024, 0, st>>>(a);
-        packed_f32_kernel<HD><<<grid, 256, 0, st>>>(a);
+        packed_f32_kernel<HD><<<dim3(grid, 4), 256, 0, st>>>(a);
         if (a.part) packed_join_kernel<float, HD, PACKED_BQ_F32><<<grid, 256, 0, st>>>(a);
     } else if (HD > 64 || p.block == 128) {
         launch_packed_bf16<HD, 1>(a, grid, st);

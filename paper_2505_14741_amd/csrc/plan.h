@@ -454,6 +454,8 @@ constexpr int packed_pieces(int rows, int keys, int kv_heads) {
     }
     return best;
 }
+// fp32: whether a sample's workgroups, up to four rounds of them, take 16 rows each and their waves keys apart
+constexpr bool packed_apart(int rows, int pieces, int kv_heads) { return (rows + 63L) / 64 * pieces * kv_heads <= 2 * PACKED_PIECES; }
 // block: rows of a workgroup (bf16, heads up to 64: 256 where that leaves two workgroups for each compute unit; a row's result does not depend on it); slots:
 // the most workgroups of a key head; scratch: a table of the slots, and a block of partial sums for each slot and key head
 struct PackedPlan { int block, slots, part_rows; size_t table_bytes, part_bytes; };
