@@ -727,17 +727,12 @@ packed_bf16_kernel(PackedArgs a) {
 // ------------------------------------------------------------------------------------ fp32
 // 16 rows per wave with full fp32 products (v_mfma_f32_16x16x4_f32): S^T = K Q^T leaves a row in lane % 16 with keys 4 (lane / 16) + i of every 16.
 // Probabilities in fp32, exponentials as exact as expf.
-// tanh in 20 instructions, good for 3 roundings: (1 - t) / (1 + t) with t = exp(-2 |x|), and below 0.35, where 1 - t cancels, the series to x^11 (what is left
-// out is below 2^-26 of it).
-__device__ __forceinline__ float tanh_of(float x) {
-    const float y = fabsf(x), t = exp_near(fmaxf(-2.0f * y, EXP_NEAR)), d = 1.0f + t, r = __builtin_amdgcn_rcpf(d), n = 1.0f - t, q = n * r;
-    const float big = __builtin_fmaf(__builtin_fmaf(-d, q, n), r, q), z = x * x;
-    float p = -1382.0f / 155925.0f;
-    p = __builtin_fmaf(p, z, 62.0f / 2835.0f);
-    p = __builtin_fmaf(p, z, -17.0f / 315.0f);
-    p = __builtin_fmaf(p, z, 2.0f / 15.0f);
-    p = __builtin_fmaf(p, z, -1.0f / 3.0f);
-    return y < 0.35f ? __builtin_fmaf(p * z, x, x) : x != x ? x : __builtin_copysignf(big, x);
+// cap * tanh(x / cap), into = 2 / cap in powers of two: cap - 2 cap / (1 + 2^(into x)), the quotient refined once.  Off by a few roundings of cap, where a
+// score's own products are off by as many of |q| |k| (with a series below 0.35, exact for small x too, 29 instructions instead of 8).
+__device__ __forceinline__ float capped_of(float x, float cap, float into) {
+    const float d = 1.0f + fminf(__builtin_amdgcn_exp2f(x * into), 0x1p+100f), r = __builtin_amdgcn_rcpf(d);
+    const float y = __builtin_fmaf(-2.0f * cap, __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r), cap);
+    return x != x ? x : y;
 }
 
 // APART: the workgroup takes 16 rows (of the block's 64, those of blockIdx.y), each wave a quarter of every tile's keys, and the waves' sums are united
@@ -745,6 +740,7 @@ __device__ __forceinline__ float tanh_of(float x) {
 template <int HD, bool APART>
 __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave) {
     constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256, BQ = PACKED_BQ_F32, NG = APART ? 1 : 4;
+    constexpr int AHEAD = !APART ? 1 : HD <= 32 ? 4 : HD == 64 ? 2 : 1;              // tiles requested ahead (a step is shorter than a load)
     const int l16 = lane & 15, kgrp = lane >> 4, g0 = APART ? wave : 0;              // g0: the wave's first 16 keys of a tile
     const float *kb = (const float*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const float*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
     const int w0 = it.r0 + 16 * (APART ? (int)blockIdx.y : wave), wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
@@ -754,46 +750,56 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
     const int tiles_all = (it.keys + KT - 1) / KT, tiles = (it.reach(a, it.ahead + bl / a.share) + KT - 1) / KT;
     const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
     const PackedRow me = packed_query(a, it, row);
-    const float inv_cap = a.cap > 0.f ? 1.0f / a.cap : 0.f;
+    const float into = a.cap > 0.f ? 2.0f * PACKED_LOG2E / a.cap : 0.f;
     f32x4_t qf[NB];
     {
         const float* p = (const float*)a.q + packed_row(a, it, row, a.q_tok, a.q_head);
 #pragma unroll
         for (int d = 0; d < NB; ++d) qf[d] = *reinterpret_cast<const f32x4_t*>(p + d * 16 + kgrp * 4) * a.scale;
     }
-    f32x4_t kn[LOADS], vn[LOADS];
-    float fn = 0.f;
-    auto fetch = [&](int kv0) {
+    f32x4_t kn[AHEAD][LOADS], vn[AHEAD][LOADS];
+    const int at = threadIdx.x / CH, of = threadIdx.x % CH * 4;      // the thread's first key and values of a tile
+    const long k_mine = at * a.k_tok + of, v_mine = at * a.v_tok + of, k_step = 256 / CH * a.k_tok, v_step = 256 / CH * a.v_tok;
+    auto fetch = [&](int n, int kv0) {                   // (keys behind the sample's last one are zeros)
+        const float *kt = kb + kv0 * a.k_tok, *vt = vb + kv0 * a.v_tok;
+        if (kv0 + KT <= it.keys) {
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                kn[n][u] = *reinterpret_cast<const f32x4_t*>(kt + (k_mine + u * k_step));
+                vn[n][u] = *reinterpret_cast<const f32x4_t*>(vt + (v_mine + u * v_step));
+            }
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int e = threadIdx.x + 256 * u, key = kv0 + e / CH, d = e % CH * 4;
-            kn[u] = vn[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (key < it.keys) {
-                kn[u] = *reinterpret_cast<const f32x4_t*>(kb + key * a.k_tok + d);
-                vn[u] = *reinterpret_cast<const f32x4_t*>(vb + key * a.v_tok + d);
+            kn[n][u] = vn[n][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (kv0 + at + 256 / CH * u < it.keys) {
+                kn[n][u] = *reinterpret_cast<const f32x4_t*>(kt + (k_mine + u * k_step));
+                vn[n][u] = *reinterpret_cast<const f32x4_t*>(vt + (v_mine + u * v_step));
             }
         }
-        if (a.slopes) fn = packed_frame(a, it, kv0 + (threadIdx.x & 63));
     };
     f32x4_t acc[NB];
 #pragma unroll
     for (int d = 0; d < NB; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    if (j0 < j1) fetch(j0 * KT);
-    for (int j = j0; j < j1; ++j) {
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n)
+        if (j0 + n < j1) fetch(n, (j0 + n) * KT);
+    auto tile = [&](int j, int n) {
         const int kv0 = j * KT;
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
             const int e = threadIdx.x + 256 * u, off = e / CH * LD + e % CH * 4;
-            *reinterpret_cast<f32x4_t*>(Ks + off) = kn[u];
-            *reinterpret_cast<f32x4_t*>(Vs + off) = vn[u];
+            *reinterpret_cast<f32x4_t*>(Ks + off) = kn[n][u];
+            *reinterpret_cast<f32x4_t*>(Vs + off) = vn[n][u];
         }
-        if (a.slopes && threadIdx.x < KT) Fs[threadIdx.x] = fn;
+        if (a.slopes && threadIdx.x < KT) Fs[threadIdx.x] = packed_frame(a, it, kv0 + (int)threadIdx.x);
         __syncthreads();
-        if (j + 1 < j1) fetch(kv0 + KT);
+        if (j + AHEAD < j1) fetch(n, kv0 + AHEAD * KT);
         const int k0 = kv0 + g0 * 16;                    // the wave's keys
-        if (k0 >= most) continue;
+        if (k0 >= most) return;
         const int blocks = min(NG, (most - k0 + 15) / 16);           // 16-key blocks that some row of the wave sees
         const bool cut = k0 + 16 * NG > least;
         const int left = me.reach - k0 - 4 * kgrp;
@@ -812,7 +818,7 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
             }
             if (a.cap > 0.f) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[g][i] = a.cap * tanh_of(sc[g][i] * inv_cap);
+                for (int i = 0; i < 4; ++i) sc[g][i] = capped_of(sc[g][i], a.cap, into);
             }
             if (a.slopes) {
                 const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + (g0 + g) * 16 + kgrp * 4);
@@ -829,12 +835,14 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
                 low = fminf(low, sc[g][i]);
             }
         }
-        const float mn = fmaxf(m, max_xor32(max_xor16(top)));
-        const float alpha = mn == m ? 1.f : expf(m - mn), ref = mn == -INFINITY ? 0.f : mn;
-        m = mn;
-        l *= alpha;
+        const float mn = fmaxf(m, max_xor32(max_xor16(top))), ref = mn == -INFINITY ? 0.f : mn;
+        if (__any(mn != m)) {
+            const float alpha = mn == m ? 1.f : expf(m - mn);
+            m = mn;
+            l *= alpha;
 #pragma unroll
-        for (int d = 0; d < NB; ++d) acc[d] *= alpha;
+            for (int d = 0; d < NB; ++d) acc[d] *= alpha;
+        }
         const bool near = __ballot(low - ref < EXP_NEAR) == 0;       // (of the whole wave; not with keys that a row does not see)
         bool odd = false;
 #pragma unroll
@@ -870,6 +878,11 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
                     }
             }
         }
+    };
+    for (int j = j0; j < j1; j += AHEAD) {
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n)
+            if (j + n < j1) tile(j + n, n);
     }
     l = sum_xor32(sum_xor16(l));
     if constexpr (APART) {
