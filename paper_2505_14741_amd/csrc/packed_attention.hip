@@ -224,8 +224,11 @@ __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
 }
 
 enum PackedFrames { PACKED_ONE, PACKED_EACH, PACKED_ANY };
+enum PackedState { ROW_REACH, ROW_SLOPE, ROW_FRAME, ROW_M, ROW_MC, ROW_STATES };     // (ROW_MC: the reference in powers of two)
 
-template <int HD, int QT, bool CAP, bool BIAS>
+// BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  (One kernel with the loops of both has
+// no registers left: 32 bytes of scratch per lane and tile, eight times as slow.)
+template <int HD, int QT, bool CAP, int BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
     static constexpr int SLOTS = 3;                                  // tiles of K, and of V, in LDS (four, requested a tile earlier: as fast)
@@ -239,8 +242,8 @@ struct PackedBf16 {
     float* const fl;                                                 // frames of their keys
     const bf16_t *kb, *vb;
     int lane, wave, l32, hi;
-    PackedRow me[QT];
-    float c0, cap2, into, m[QT], mc[QT], ref[QT];                    // m: the reference, a score (capped or biased: in powers of two); mc: in powers of two; ref: see refer()
+    float* const rs;                                                 // the lane's rows' state, which the steady loop has no registers for: [ROW_*][row]
+    float c0, cap2, into, m[QT], ref[QT];                            // m: the reference, a score (capped or biased: in powers of two); ref: see refer()
     int koff[QS], voff[NB], now, now_end;
     bf16x8_t qf[QT][QS];
     f32x16_t acc[QT][NB];
@@ -250,8 +253,10 @@ struct PackedBf16 {
     __device__ __forceinline__ static int k_place(int r) { return HD == 16 ? 0 : HD == 32 ? (r >> 2) & 3 : r & 7; }
     __device__ __forceinline__ static int v_place(int r) { return HD <= 32 ? 0 : HD == 64 ? (r & 3) | (r & 2) << 1 : (r & 3) << 2; }
 
-    __device__ __forceinline__ PackedBf16(const PackedArgs& a_, const PackedItem& it_, unsigned char* lds, float* frames)
-        : a(a_), it(it_), kl(lds), vl(lds + SLOTS * TILE), fl(frames) {}
+    __device__ __forceinline__ PackedBf16(const PackedArgs& a_, const PackedItem& it_, unsigned char* lds, float* frames, float* rows)
+        : a(a_), it(it_), kl(lds), vl(lds + SLOTS * TILE), fl(frames), rs(rows) {}
+    __device__ __forceinline__ float& state(int what, int q) const { return rs[what * 128 * QT + q * 32]; }
+    __device__ __forceinline__ PackedRow me(int q) const { return PackedRow{__float_as_int(state(ROW_REACH, q)), state(ROW_SLOPE, q), state(ROW_FRAME, q)}; }
 
     __device__ __forceinline__ void start(int w0) {
         kb = (const bf16_t*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head;
@@ -262,8 +267,10 @@ struct PackedBf16 {
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             const int row = min(w0 + q * 32 + l32, it.rows - 1);
-            me[q] = packed_query(a, it, row);
-            me[q].slope *= PACKED_LOG2E;
+            const PackedRow r = packed_query(a, it, row);
+            state(ROW_REACH, q) = __int_as_float(r.reach);
+            state(ROW_SLOPE, q) = r.slope * PACKED_LOG2E;
+            state(ROW_FRAME, q) = r.frame;
             const bf16_t* p = (const bf16_t*)a.q + packed_row(a, it, row, a.q_tok, a.q_head) + hi * 8;      // second operand of S^T: 8 consecutive d of row l32
 #pragma unroll
             for (int s = 0; s < QS; ++s) qf[q][s] = *reinterpret_cast<const bf16x8_t*>(p + s * 16);
@@ -289,16 +296,16 @@ struct PackedBf16 {
     }
     // requests the keys of tile tk and the values of tile tv (those that lie before `end`) into their slots; keys behind the sample's last one repeat it
     __device__ __forceinline__ void request(int tk, int kslot, int tv, int vslot, int end) {
+        const bool of_k = wave < 2;                      // (uniform)
+        const int tile = of_k ? tk : tv;
+        if (tile < 0 || tile >= end) return;
+        const bf16_t* const from = of_k ? kb : vb;
+        const long tok = of_k ? a.k_tok : a.v_tok;
+        unsigned char* const to = (of_k ? kl + kslot * TILE : vl + vslot * TILE) + (wave & 1) * LOADS * 1024;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int n = wave * LOADS + i;
-            const bool of_k = n < 2 * LOADS;
-            const int at = (of_k ? n : n - 2 * LOADS) * 1024 + lane * 16, r = at / ROW, tile = of_k ? tk : tv;
-            if (tile >= end || tile < 0) continue;
-            const int chunk = at % ROW / 16 ^ (of_k ? k_place(r) : v_place(r)), key = min(tile * U + r, it.keys - 1);
-            const bf16_t* p = (of_k ? kb + key * a.k_tok : vb + key * a.v_tok) + chunk * 8;
-            unsigned char* to = (of_k ? kl + kslot * TILE : vl + vslot * TILE) + (of_k ? n : n - 2 * LOADS) * 1024;
-            lds_dma16(p, (unsigned)uniform((int)(unsigned)(size_t)PS_LDS_PTR(to)));
+            const int at = ((wave & 1) * LOADS + i) * 1024 + lane * 16, r = at / ROW, chunk = at % ROW / 16 ^ (of_k ? k_place(r) : v_place(r));
+            lds_dma16(from + min(tile * U + r, it.keys - 1) * tok + chunk * 8, (unsigned)uniform((int)(unsigned)(size_t)PS_LDS_PTR(to + i * 1024)));
         }
     }
     __device__ __forceinline__ void frames(int tile, int slot) {     // (visible behind the next barrier)
@@ -327,7 +334,7 @@ struct PackedBf16 {
     }
     // keys that the row does not see
     __device__ __forceinline__ void cut(f32x16_t& s, int q, int kv0) const {
-        const int left = me[q].reach - kv0 - 4 * hi;
+        const int left = me(q).reach - kv0 - 4 * hi;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < left ? s[i] : -INFINITY;
     }
@@ -339,20 +346,17 @@ struct PackedBf16 {
     }
     __device__ __forceinline__ void refer() {
 #pragma unroll
-        for (int q = 0; q < QT; ++q) ref[q] = BIAS && now >= 0 ? __builtin_fmaf(me[q].slope, fabsf(me[q].frame - (float)now), mc[q]) : mc[q];
-    }
-    // whether keys kv0 .. kv0 + n - 1 lie in one frame, or in the prefix (frames of fewer than 64: no)
-    __device__ __forceinline__ bool one_frame(int kv0, int n) {
-        if (!BIAS) return true;
-        if (a.frame < 64) return kv0 + n <= it.prefix;
-        if (kv0 >= now_end) {
-            while (kv0 >= now_end) {
-                ++now;
-                now_end = (int)min((long)now_end + a.frame, 1L << 30);
-            }
-            refer();
+        for (int q = 0; q < QT; ++q) {
+            const float mc = state(ROW_MC, q);
+            ref[q] = BIAS == 1 && now >= 0 ? __builtin_fmaf(me(q).slope, fabsf(me(q).frame - (float)now), mc) : mc;
         }
-        return kv0 + n <= now_end;
+    }
+    __device__ __forceinline__ void advance(int kv0) {
+        while (kv0 >= now_end) {
+            ++now;
+            now_end = (int)min((long)now_end + a.frame, 1L << 30);
+        }
+        refer();
     }
     __device__ __forceinline__ static float largest(const f32x16_t& s) {
         float top = s[0];
@@ -361,13 +365,14 @@ struct PackedBf16 {
         return max_xor32(top);
     }
     // Weights 2^(x - reference - bias) of a half, rounded to bf16 for the second product; the same numbers whichever way their keys' frames are looked at
-    // (PACKED_ONE: one_frame(); PACKED_EACH: each key's, none in the prefix; PACKED_ANY) and whether some keys are not seen by some rows (CUT) or not.
+    // (PACKED_ONE: all in the frame at hand; PACKED_EACH: each key's, none in the prefix; PACKED_ANY) and whether some keys are not seen by some rows (CUT) or not.
     template <bool CUT, int FRAMES>
     __device__ __forceinline__ void weights(f32x16_t (&s)[QT], bf16x8_t (&pf)[QT][2], int kv0, const float* of) const {
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             f32x16_t& x = s[q];
-            const float c = CAP ? 1.0f : c0;
+            const float c = CAP ? 1.0f : c0, mc = FRAMES == PACKED_ONE ? 0.f : state(ROW_MC, q);
+            const PackedRow row = me(q);
             if constexpr (CAP) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = capped(x[i]);
@@ -377,9 +382,9 @@ struct PackedBf16 {
             for (int i = 0; i < 16; ++i) {
                 float r = ref[q];
                 if constexpr (FRAMES != PACKED_ONE) {
-                    const float far = fabsf(me[q].frame - of[4 * hi + 8 * (i / 4) + i % 4]);
-                    r = __builtin_fmaf(me[q].slope, far, mc[q]);
-                    if constexpr (FRAMES == PACKED_ANY) r = far == far ? r : mc[q];
+                    const float far = fabsf(row.frame - of[4 * hi + 8 * (i / 4) + i % 4]);
+                    r = __builtin_fmaf(row.slope, far, mc);
+                    if constexpr (FRAMES == PACKED_ANY) r = far == far ? r : mc;
                 }
                 pf[q][i / 8][i % 8] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -r));
             }
@@ -428,7 +433,7 @@ struct PackedBf16 {
                         const float x = to_f32(row[(at / 8 ^ v_place(key)) * 8 + at % 8]);
 #pragma unroll
                         for (int q = 0; q < QN; ++q)
-                            if (kv0 + key < me[q].reach && !(fabsf(x) < INFINITY)) acc[q][d][i] += x;
+                            if (kv0 + key < me(q).reach && !(fabsf(x) < INFINITY)) acc[q][d][i] += x;
                     }
             }
         }
@@ -442,8 +447,9 @@ struct PackedBf16 {
             f32x16_t& x = s[q];
             if constexpr (CAP || BIAS) {
                 const float* f = of + 4 * hi;
+                const PackedRow row = me(q);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = (CAP ? capped(x[i]) : x[i] * c0) - (BIAS ? packed_bias(me[q], f[8 * (i / 4) + i % 4]) : 0.f);
+                for (int i = 0; i < 16; ++i) x[i] = (CAP ? capped(x[i]) : x[i] * c0) - (BIAS ? packed_bias(row, f[8 * (i / 4) + i % 4]) : 0.f);
             }
             cut(x, q, kv0);
             const float top = largest(x), mn = top > m[q] + ahead ? top : m[q], alpha = mn == m[q] ? 1.f : exp2_between(m[q], mn, c);   // 0 on the first tile
@@ -543,8 +549,8 @@ struct PackedBf16 {
     }
 };
 
-template <int HD, int QT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, QT == 1 && HD <= 64 && !BIAS ? 3 : 2)
+template <int HD, int QT, bool CAP, int BIAS>
+__global__ void __launch_bounds__(256, QT == 1 && HD <= 64 ? 3 : 2)
 packed_bf16_kernel(PackedArgs a) {
     typedef PackedBf16<HD, QT, CAP, BIAS> P;
     constexpr int U = P::U, NB = P::NB, HALVES = P::HALVES, BQ = 128 * QT;
@@ -560,7 +566,8 @@ packed_bf16_kernel(PackedArgs a) {
     const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
     const int end = (most + 31) / 32;                    // halves that some row of the wave sees
 
-    P t(a, it, lds, fl);
+    __shared__ float rows[ROW_STATES * BQ];
+    P t(a, it, lds, fl, rows + wave * 32 * QT + l32);
     t.lane = lane; t.wave = wave; t.l32 = l32; t.hi = lane >> 5;
     t.start(w0);
     t.clear();
@@ -638,8 +645,9 @@ packed_bf16_kernel(PackedArgs a) {
                             f32x16_t u = s[X][q];
                             t.cut(u, q, kv0);
                             const float top = P::largest(u);
-                            t.m[q] = top == -INFINITY ? top : CAP ? t.capped(top) : BIAS ? top * t.c0 : top;
-                            t.mc[q] = top == -INFINITY ? 0.f : CAP || BIAS ? t.m[q] : top * t.c0;
+                            const float m = top == -INFINITY ? top : CAP ? t.capped(top) : BIAS ? top * t.c0 : top;
+                            t.state(ROW_M, q) = m;
+                            t.state(ROW_MC, q) = top == -INFINITY ? 0.f : CAP || BIAS ? m : top * t.c0;
                         }
                         t.refer();
                     }
@@ -652,26 +660,29 @@ packed_bf16_kernel(PackedArgs a) {
     };
     const std::integral_constant<int, 0> c0;
     const std::integral_constant<int, 1> c1;
-    const std::integral_constant<int, PACKED_ONE> steady;
-    const std::integral_constant<int, PACKED_EACH> each;
+    const std::integral_constant<int, BIAS == 2 ? PACKED_EACH : PACKED_ONE> steady;
     const std::integral_constant<int, PACKED_ANY> general;
     const int all_see = it.reach(a, it.ahead + it.r0 / a.share);         // what the block's first row sees
+    // the first tile from j on that is not as those before it: for the workgroup, or for a row's bias (counted in front of the loops: a condition that
+    // changes the frame costs them their registers)
+    const auto alike = [&](int j) {
+        int stop = min(j1 - 1, all_see / U);
+        if constexpr (BIAS == 1) {
+            t.advance(j * U);
+            stop = min(stop, t.now_end / U);
+        }
+        return BIAS == 2 && j * U < it.prefix ? j : stop;
+    };
     int j = j0;
     if constexpr (HALVES == 2) {
         do {
             tile(j++, c0, general);
-            for (; j + 1 < j1 && (j + 1) * U <= all_see && t.one_frame(j * U, U); ++j) tile(j, c0, steady);
-            if constexpr (BIAS)
-                if (a.frame < 64)
-                    for (; j + 1 < j1 && (j + 1) * U <= all_see && j * U >= it.prefix; ++j) tile(j, c0, each);
+            for (const int stop = alike(j); j < stop; ++j) tile(j, c0, steady);
         } while (j < j1);
     } else {
         tile(j++, c0, general);
         while (j < j1) {
-            for (; j + 2 < j1 && (j + 2) * U <= all_see && t.one_frame(j * U, 2 * U); j += 2) { tile(j, c1, steady); tile(j + 1, c0, steady); }
-            if constexpr (BIAS)
-                if (a.frame < 64)
-                    for (; j + 2 < j1 && (j + 2) * U <= all_see && j * U >= it.prefix; j += 2) { tile(j, c1, each); tile(j + 1, c0, each); }
+            for (const int stop = alike(j); j + 1 < stop; j += 2) { tile(j, c1, steady); tile(j + 1, c0, steady); }
             tile(j++, c1, general);
             if (j < j1) tile(j++, c0, general);
         }
@@ -687,9 +698,10 @@ packed_bf16_kernel(PackedArgs a) {
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
         redo[q] = false;
-        if (t.me[q].reach > j0 * U) {
+        if (end > j0 * HALVES) t.m[q] = t.state(ROW_M, q);           // (set with the wave's first half)
+        if (t.me(q).reach > j0 * U) {
             const float sum = sum_xor32(t.l[q]);
-            redo[q] = !(sum >= PACKED_SUM_MIN && sum <= PACKED_SUM_MAX) || !(fabsf(t.mc[q]) <= PACKED_FAR);
+            redo[q] = !(sum >= PACKED_SUM_MIN && sum <= PACKED_SUM_MAX) || !(fabsf(t.state(ROW_MC, q)) <= PACKED_FAR);
             float zero = 0.f;                            // (NaN if a value is not finite)
 #pragma unroll
             for (int d = 0; d < NB; ++d)
@@ -1001,10 +1013,16 @@ size_t packed_workspace_bytes(int dtype, const PackedArgs& a) {
 template <int HD, int QT>
 static void launch_packed_bf16(const PackedArgs& a, unsigned grid, hipStream_t st) {
     if (a.samples > PACKED_SEARCH) packed_table_kernel<128 * QT><<<1, 1024, 0, st>>>(a);
-    if (a.cap > 0.f && a.slopes) packed_bf16_kernel<HD, QT, true, true><<<grid, 256, 0, st>>>(a);
-    else if (a.cap > 0.f) packed_bf16_kernel<HD, QT, true, false><<<grid, 256, 0, st>>>(a);
-    else if (a.slopes) packed_bf16_kernel<HD, QT, false, true><<<grid, 256, 0, st>>>(a);
-    else packed_bf16_kernel<HD, QT, false, false><<<grid, 256, 0, st>>>(a);
+    const int bias = !a.slopes ? 0 : a.frame >= 64 ? 1 : 2;
+    if (a.cap > 0.f) {
+        if (bias == 0) packed_bf16_kernel<HD, QT, true, 0><<<grid, 256, 0, st>>>(a);
+        else if (bias == 1) packed_bf16_kernel<HD, QT, true, 1><<<grid, 256, 0, st>>>(a);
+        else packed_bf16_kernel<HD, QT, true, 2><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (bias == 0) packed_bf16_kernel<HD, QT, false, 0><<<grid, 256, 0, st>>>(a);
+        else if (bias == 1) packed_bf16_kernel<HD, QT, false, 1><<<grid, 256, 0, st>>>(a);
+        else packed_bf16_kernel<HD, QT, false, 2><<<grid, 256, 0, st>>>(a);
+    }
     if (a.part) packed_join_kernel<bf16_t, HD, 128 * QT><<<grid, 256, 0, st>>>(a);
 }
 

@@ -435,12 +435,14 @@ constexpr int PACKED_FEW_ROWS = 32;                      // rows up to which a w
 constexpr int PACKED_FEW_KEYS = 1024;                    // least keys of a piece there
 constexpr int PACKED_FEW_MIN = 128;                      // keys from which they do
 constexpr int PACKED_PIECES = 512;                       // workgroups of a round, two per compute unit of 256
+constexpr int PACKED_UNIT = 128;                         // rows by which pieces are counted
 // Pieces of a sample's keys (calls whose keys have offsets of their own), a function of the sample alone.  items: workgroups without.  Few rows: pieces of
 // PACKED_FEW_KEYS keys, one round at most.  Else pieces of 256 keys at least: one round of them where items are a quarter of one; up to two rounds of items, in up to 4
-// pieces, as many as need the least rounds * tiles, a piece's partial sums counted as 8 tiles of 64 keys (1350 rows of 30 heads, 17776 keys).
+// pieces, as many as need the least rounds * tiles, a piece's partial sums counted as 8 tiles of 64 keys (1350 rows of 30 heads, 17776
+// keys: whole 516 us, in 3 pieces 297; in 2 pieces of blocks of 256 rows 355).
 constexpr int packed_pieces(int rows, int keys, int kv_heads) {
     if (keys < PACKED_KEYS || rows < 1) return 1;
-    const int items = (rows + 127) / 128 * kv_heads;
+    const int items = (rows + PACKED_UNIT - 1) / PACKED_UNIT * kv_heads;
     if (rows <= PACKED_FEW_ROWS || items <= PACKED_PIECES / 4) {
         const int n = PACKED_PIECES / items, most = keys / (rows <= PACKED_FEW_ROWS ? PACKED_FEW_KEYS : 256);
         return n < most ? (n < 1 ? 1 : n) : most < 1 ? 1 : most;
@@ -463,7 +465,9 @@ constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int 
     const long blocks = rows / block + samples;
     if (!own || kv_tokens < PACKED_KEYS) return blocks;
     const int divided = kv_tokens / PACKED_KEYS;         // samples that can be
-    return 4 * blocks + (samples < divided ? samples : divided) * (long)(PACKED_PIECES / kv_heads) * (block < 128 ? 2 : 1);
+    const long more = (samples < divided ? samples : divided) * (long)(PACKED_PIECES / kv_heads) * (PACKED_UNIT > block ? PACKED_UNIT / block : 1);
+    const long each = ((rows < block ? rows : (long)PACKED_PIECES * block) + block - 1) / block * (kv_tokens / 256);     // blocks of a sample that has more than 4 pieces
+    return 4 * blocks + (more < each ? more : each);
 }
 // a workgroup for each slot, up to a multiple of 8, and key head
 constexpr long packed_workgroups(long slots, int kv_heads) { return (slots + 7) / 8 * 8 * kv_heads; }
