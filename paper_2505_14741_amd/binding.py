@@ -444,21 +444,29 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
 
 
 # ------------------------------------- operators of self-attention on packed samples
+@functools.lru_cache(maxsize=1024)
+def _fp4_quantize_plan(dtype, shape, stride):
+    w = "fp4_quantize"
+    _need(len(shape) == 2 and shape[1] >= 1, w, "x must be [rows, cols]")
+    dt = _CODE.get(dtype)
+    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
+    rows, cols = shape
+    _need_extents(w, rows, cols)
+    _need(stride[1] == 1 or cols == 1, w, "the elements of a row must be contiguous")
+    kp = (cols + 127) // 128 * 128
+    return dt, (rows, kp // 2), (kp // 32, (rows + 15) // 16 * 16)
+
+
 def fp4_quantize(x: torch.Tensor):
     """x [rows, cols], float32 or bfloat16, rows any distance apart -> (q uint8 [rows, kp / 2], two e2m1 codes to a byte, scale float8_e8m0fnu
     [kp / 32, pitch]): kp is cols rounded up to 128, pitch is rows rounded up to 16, both filled up as include/parastep.h says."""
-    w = "fp4_quantize"
-    _need(x.dim() == 2 and x.shape[1] >= 1, w, "x must be [rows, cols]")
-    dt = _CODE.get(x.dtype)
-    _need(dt is not None, w, "float32 or bfloat16", PS_ERR_DTYPE)
-    rows, cols = x.shape
-    _need_extents(w, rows, cols)
-    _need(x.stride(1) == 1 or cols == 1, w, "the elements of a row must be contiguous")
-    _need_here(w, x)
-    kp = (cols + 127) // 128 * 128
-    q = torch.empty((rows, kp // 2), dtype=torch.uint8, device=x.device)
-    scale = torch.empty((kp // 32, (rows + 15) // 16 * 16), dtype=torch.float8_e8m0fnu, device=x.device)
-    _check(lib().fp4_quantize(x.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, x.stride(0), dt, _stream()), w)
+    shape, stride = x.shape, x.stride()
+    dt, of_q, of_scale = _fp4_quantize_plan(x.dtype, shape, stride)
+    _need_here("fp4_quantize", x)
+    dev = x.device
+    q = torch.empty(of_q, dtype=torch.uint8, device=dev)
+    scale = torch.empty(of_scale, dtype=torch.float8_e8m0fnu, device=dev)
+    _check(lib().fp4_quantize(x.data_ptr(), q.data_ptr(), scale.data_ptr(), shape[0], shape[1], stride[0], dt, _stream()), "fp4_quantize")
     return q, scale
 
 
@@ -520,25 +528,31 @@ def dit_linear_fp4(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_sc
     return out
 
 
+@functools.lru_cache(maxsize=1024)
+def _rope_plan(dtype, shape, stride, dims, thetas):
+    w, n = "rope_table", len(dims)
+    _need(len(shape) == 2 and 1 <= n <= 4 and shape[1] == n, w, "positions must be [tokens, axes], 1 to 4 axes of axis_dims")
+    _need(dtype == torch.float32, w, "positions must be float32", PS_ERR_DTYPE)
+    thetas = thetas if isinstance(thetas, tuple) else (thetas,) * n
+    _need(len(thetas) == n, w, "theta must be one number, or one for each axis")
+    _need(all(0 < d <= 256 and d % 2 == 0 for d in dims), w, "axis_dims must be even, 256 in all at most")
+    _need_extents(w, shape[0])
+    _need(n == 1 or stride[1] == 1 or shape[0] == 0, w, "a token's positions must be contiguous")
+    return n, (C.c_int * n)(*dims), (C.c_double * n)(*thetas), (shape[0], sum(dims) // 2, 2)
+
+
 def rope_table(positions: torch.Tensor, axis_dims: Sequence[int], theta=10000.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """positions float32 [tokens, axes] -> float32 [tokens, sum(axis_dims) / 2, 2] of (cos, sin); theta one number, or one for each axis."""
-    w = "rope_table"
-    n = len(axis_dims)
-    _need(positions.dim() == 2 and 1 <= n <= 4 and positions.shape[1] == n, w, "positions must be [tokens, axes], 1 to 4 axes of axis_dims")
-    _need(positions.dtype == torch.float32, w, "positions must be float32", PS_ERR_DTYPE)
-    thetas = [float(t) for t in theta] if isinstance(theta, (list, tuple)) else [float(theta)] * n
-    _need(len(thetas) == n, w, "theta must be one number, or one for each axis")
-    dims = [int(d) for d in axis_dims]
-    _need(all(0 < d <= 256 and d % 2 == 0 for d in dims), w, "axis_dims must be even, 256 in all at most")
-    _need_extents(w, positions.shape[0])
-    _need(n == 1 or positions.stride(1) == 1 or positions.shape[0] == 0, w, "a token's positions must be contiguous")
-    shape = (positions.shape[0], sum(dims) // 2, 2)
+    w, stride = "rope_table", positions.stride()
+    n, dims, thetas, shape = _rope_plan(positions.dtype, positions.shape, stride, tuple(int(d) for d in axis_dims),
+                                        tuple(float(t) for t in theta) if isinstance(theta, (list, tuple)) else float(theta))
     if out is None:
         out = torch.empty(shape, dtype=torch.float32, device=positions.device)
-    _need(out.dtype == torch.float32, w, "out must be float32", PS_ERR_DTYPE)
-    _need(out.shape == shape and out.is_contiguous(), w, "out must be [tokens, sum(axis_dims) / 2, 2], contiguous")
+    else:
+        _need(out.dtype == torch.float32, w, "out must be float32", PS_ERR_DTYPE)
+        _need(out.shape == shape and out.is_contiguous(), w, "out must be [tokens, sum(axis_dims) / 2, 2], contiguous")
     _need_here(w, positions, out)
-    _check(lib().rope_table(positions.data_ptr(), positions.stride(0), n, (C.c_int * n)(*dims), (C.c_double * n)(*thetas), out.data_ptr(), shape[0], _stream()), w)
+    _check(lib().rope_table(positions.data_ptr(), stride[0], n, dims, thetas, out.data_ptr(), shape[0], _stream()), w)
     return out
 
 
@@ -547,7 +561,7 @@ def _like(t: Optional[torch.Tensor]):
 
 
 @functools.lru_cache(maxsize=1024)
-def _qk_plan(q, k, qo, ko, table, affine, norm, eps, halves, device):
+def _qk_plan(q, k, qo, ko, table, norm, eps, halves):
     w = "qk_norm_rope"
     _need(len(q[1]) == 4, w, "q must be [B, N, H, d]")
     B, N, H, d = q[1]
@@ -562,9 +576,6 @@ def _qk_plan(q, k, qo, ko, table, affine, norm, eps, halves, device):
         _need(t is None or t[2][3] == 1, w, "the elements of a head must be contiguous")
     _need(0 <= norm <= 2, w, "norm 0, 1 or 2")
     _need_extents(w, B, N, H, d, k[1][2] if k else 0)
-    for t in affine:
-        _need(t is None or t[0] == torch.float32, w, "gamma and beta must be float32", PS_ERR_DTYPE)
-        _need(t is None or (t[1] == (d,) and t[2] == (1,)), w, "gamma and beta must be [d], contiguous")
     rotated = table_batch = 0
     if table is not None:
         _need(table[0] == torch.float32, w, "table must be float32", PS_ERR_DTYPE)
@@ -588,8 +599,11 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: Optional[tor
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k_out is None and k is not None:
         k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    shape = _qk_plan(_like(q), _like(k), _like(q_out), _like(k_out), _like(table), (_like(gamma_q), _like(beta_q), _like(gamma_k), _like(beta_k)),
-                     int(norm), float(eps), bool(halves), q.get_device())
+    shape = _qk_plan(_like(q), _like(k), _like(q_out), _like(k_out), _like(table), int(norm), float(eps), bool(halves))
+    for t in (gamma_q, gamma_k, beta_q, beta_k):
+        if t is not None:
+            _need(t.dtype is torch.float32, "qk_norm_rope", "gamma and beta must be float32", PS_ERR_DTYPE)
+            _need(t.shape == q.shape[3:] and t.is_contiguous(), "qk_norm_rope", "gamma and beta must be [d], contiguous")
     _need_here("qk_norm_rope", q, k, q_out, k_out, table, gamma_q, gamma_k, beta_q, beta_k)
     _check(lib().qk_norm_rope(q.data_ptr(), _ptr(k), _ptr(table), _ptr(gamma_q), _ptr(beta_q), _ptr(gamma_k), _ptr(beta_k), q_out.data_ptr(), _ptr(k_out),
                               shape, _stream()), "qk_norm_rope")
