@@ -15,7 +15,7 @@ namespace ps {
 // A block's scale is the least power of two 2^e, e >= -127, under which its largest value is at most 6, the largest of e2m1: with amax =
 // 1.f * 2^x, e = x - 2 where 1.f <= 1.5 and x - 1 above (6 = 1.5 * 2^2).  Multiplying by 2^-e is exact, so each value is rounded once, to the
 // nearest of 0 0.5 1 1.5 2 3 4 6, ties to the even code (what the conversion instruction does).  The format has no value that is not finite: a
-// block with one has the scale NaN, and zeros.
+// block with one has the scale NaN, and zeros.  (17776 x 7680 in bf16, 346 MB: 74 us, 4.7 TB/s.)
 // Memory binds.  A workgroup takes 16 rows x 512 columns, 4 rows per wave, 8 adjacent values per lane (16 bytes of bf16, 4 lanes a
 // block): the 16 scales of a block lie side by side and are stored as 16 bytes, gathered in LDS.
 constexpr int FP4_ROWS = 16, FP4_COLS = 512;
@@ -56,7 +56,7 @@ fp4_quantize_kernel(const T* __restrict__ x, unsigned char* __restrict__ q, unsi
 }
 
 // Reading back: the same tiles; every value is exact in bf16 and fp32 but those beyond the largest number of the type (4 * 2^126, to which fp32's largest
-// numbers are rounded), which become that.
+// numbers are rounded), which become that.  (17776 x 7680 to bf16: 60 us, 5.8 TB/s.)
 template <typename T>
 __global__ void __launch_bounds__(256)
 fp4_dequantize_kernel(const unsigned char* __restrict__ q, const unsigned char* __restrict__ scale, T* __restrict__ out, int rows, int cols, long out_row,
@@ -126,6 +126,10 @@ template <int R> struct Fp4Strips {
     __device__ __forceinline__ static int at(int strip) { return strip / PER * 272 + strip % PER * R; }
 };
 
+// Measured: 17776 x 5760, k = 1920 147 us, 2.67 PFLOP/s; 4516 x 1920, k = 7680 39, 3.4.  At this rate LDS binds, not the matrix unit: a stage of a wave of 96 x 64 reads
+// 20 fragments and 40 scale bytes and writes its share of the loads, together as long as its 48 products (a ring of three or four stages
+// instead of two: no faster), so the loop alone reaches 4.6; the rest is the first stage's way and the results', 7 us for each of 9 rounds of workgroups.
+//
 // WR x WC waves of TM x TN blocks of 16 x 16 outputs (rows x columns).  A ring of NST stages.
 // A stage has two halves of TM / 2 row blocks.  The first goes row block by row block: as soon as the products of one are issued, its
 // registers are read again with the one TM / 2 further down.  Then the next stage's data are waited for and the slot of this one, all of

@@ -43,8 +43,8 @@ struct PackedItem {
 };
 // Which key head and slot a workgroup takes.  Workgroup ids go to the 8 XCDs in turn, each with an L2 of its own: an XCD has kv_heads / 8 key heads to itself and
 // every eighth item of the others', over 8 slots as many as all XCDs; low slots, which are long, first.
-__device__ __forceinline__ void packed_place(int kv_heads, int& g, int& slot) {
-    const unsigned x = blockIdx.x & 7, n = blockIdx.x >> 3, own = (unsigned)kv_heads / 8, rest = (unsigned)kv_heads % 8;
+__device__ __forceinline__ void packed_place(unsigned id, int kv_heads, int& g, int& slot) {
+    const unsigned x = id & 7, n = id >> 3, own = (unsigned)kv_heads / 8, rest = (unsigned)kv_heads % 8;
     const unsigned period = n / (unsigned)kv_heads, i = n - period * (unsigned)kv_heads;
     if (i < 8 * own) {
         slot = (int)(period * 8 + i / own);
@@ -79,13 +79,13 @@ packed_table_kernel(PackedArgs a) {
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int2* const table = a.table;
-    int base = 0;
+    long base = 0;                                       // (offsets that fall could count far more than there are)
     for (int s0 = 0; s0 < a.samples; s0 += 1024) {
         const int s = s0 + (int)threadIdx.x;
         int n = 0;
         if (s < a.samples) {
             const PackedCount c = packed_count<BQ>(a, s);
-            n = c.blocks * c.pieces;
+            n = min(c.blocks * c.pieces, a.slots);
         }
         int upto = n;                                    // inclusive sums
 #pragma unroll
@@ -96,24 +96,23 @@ packed_table_kernel(PackedArgs a) {
         __syncthreads();
         if (lane == 63) sums[wave] = upto;
         __syncthreads();
-        int at = base + upto - n;
+        long at = base + upto - n;
         for (int w = 0; w < 16; ++w) {
             at += w < wave ? sums[w] : 0;
             base += sums[w];
         }
-        for (int i = 0; i < n; ++i)
-            if (at + i < a.slots) table[1 + at + i] = make_int2(s, i);   // (offsets that fall could count more)
+        for (int i = 0; i < n && at + i < a.slots; ++i) table[1 + at + i] = make_int2(s, i);
     }
-    if (threadIdx.x == 0) table[0] = make_int2(min(base, a.slots), 0);
+    if (threadIdx.x == 0) table[0] = make_int2((int)min(base, (long)a.slots), 0);
 }
 
 // The block's sample, rows and piece.  Up to 64 samples are looked through here, those with more keys first.  A sample's last blocks, whose rows see most, come
 // first.
 template <int BQ>
-__device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane) {
+__device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane, unsigned id) {
     PackedItem t;
     int slot, of_sample;                                 // of_sample: which of the sample's slots
-    packed_place(a.kv_heads, t.g, slot);
+    packed_place(id, a.kv_heads, t.g, slot);
     t.any = false;
     t.slot = slot;
     if (slot >= a.slots) return t;
@@ -147,6 +146,7 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane)
     const int block = (int)((unsigned)of_sample / (unsigned)c.pieces);
     t.piece = of_sample - block * c.pieces;
     t.pieces = c.pieces;
+    if (slot - t.piece + t.pieces > a.slots) return t;   // (offsets that fall: the block's last pieces have no place)
     t.q0 = c.q0;
     t.rows = c.nq * a.share;
     t.r0 = (c.blocks - 1 - block) * BQ;
@@ -214,7 +214,14 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 // A row's exponents are relative to the largest score of its first 32 keys (without the distance bias, which is not positive where slopes are not
 // negative), instead of a maximum that moves: what the sums became is looked at behind the last key.  Rows whose sum is not within 2^-40 .. 2^32, or
 // above 2^14 with outputs that are not finite, or whose reference is beyond 2^10 (where the rounding of scale * score is 2^-14), are computed again by
-// packed_tracked(), their whole wave with them: a reference that moves where a score exceeds it by 8 in powers of two, and is subtracted first where it is large.
+// tracked(): a reference that moves where a score exceeds it by 8 in powers of two, and is subtracted first where it is large.  The rows next to them keep
+// what they have, so a row's result depends neither on them nor on the block's size.
+//
+// Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 820 us, 0.93 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.45 ms, 0.90; the
+// simple kernel, one moving reference and a tile of 64 keys at a time, 1061 and 1810.  Vector instructions are at work 53 % of the time, the matrix unit 39 %, rarely
+// both: what a wave's three parts leave free the other wave of the SIMD hardly takes, and at the end of the launch 1.65 of 2 waves are there.  Four slots of keys and
+// a manual order of the parts: as fast; items in the order of the offsets and over all XCDs instead of as packed_place() and packed_item() have them: 931 and 1766 us
+// (with them 847 and 1540, of that time's kernel).
 constexpr float PACKED_AHEAD = 8.0f, PACKED_FAR = 0x1p+10f;
 constexpr float PACKED_SUM_MIN = 0x1p-40f, PACKED_SUM_MAX = 0x1p+32f, PACKED_SUM_NEAR = 0x1p+14f;
 constexpr int PACKED_BQ_F32 = 64;
@@ -226,8 +233,8 @@ __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
 enum PackedFrames { PACKED_ONE, PACKED_EACH, PACKED_ANY };
 enum PackedState { ROW_REACH, ROW_SLOPE, ROW_FRAME, ROW_M, ROW_MC, ROW_STATES };     // (ROW_MC: the reference in powers of two)
 
-// BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  (One kernel with the loops of both has
-// no registers left: 32 bytes of scratch per lane and tile, eight times as slow.)
+// BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  Two kernels, because the loops of both
+// in one leave it without registers.  (1350 rows of 30 heads against 17776 keys in frames of 1350: 316 us, with each key's bias looked up 381.)
 template <int HD, int QT, bool CAP, int BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
@@ -470,7 +477,8 @@ struct PackedBf16 {
     }
 
     // Few rows (PACKED_FEW_ROWS): memory binds, and the waves take every fourth half of the keys each, through slots of their own and without a barrier; their
-    // sums are united behind the last key, in the first wave's registers.
+    // sums are united behind the last key, in the first wave's registers.  (Single tokens of eight samples against 128 MB of keys and values: 30 us,
+    // 4.3 TB/s, and 7 for the join.)
     static constexpr int FEW_UNITS = HD > 64 ? 2 : 3, FEW_LOADS = 32 * ROW / 1024, FEW_HALF = 32 * ROW, FEW_BYTES = 4 * FEW_UNITS * FEW_HALF;
     static constexpr int MOST = 2 * SLOTS * TILE > FEW_BYTES ? 2 * SLOTS * TILE : FEW_BYTES, SUMS = 3 * (NB * 16 + 2) * 256, LDS_BYTES = MOST > SUMS ? MOST : SUMS;
     __device__ __forceinline__ void request_half(int h, unsigned char* to, bool of_k) {
@@ -557,7 +565,7 @@ packed_bf16_kernel(PackedArgs a) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[P::LDS_BYTES];
     __shared__ float fl[BIAS ? (P::SLOTS * U > 128 ? P::SLOTS * U : 128) : 1];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l32 = lane & 31;
-    const PackedItem it = packed_item<BQ>(a, lane);
+    const PackedItem it = packed_item<BQ>(a, lane, blockIdx.x);
     if (!it.any) return;                                 // (the whole workgroup)
     const bool few = it.rows <= PACKED_FEW_ROWS && it.keys > PACKED_FEW_MIN;         // (then all waves have the same rows)
     const int w0 = it.r0 + (few ? 0 : wave * 32 * QT), wl = min(w0 + 32 * QT - 1, it.rows - 1), bl = min(it.r0 + BQ, it.rows) - 1;
@@ -699,7 +707,7 @@ packed_bf16_kernel(PackedArgs a) {
     for (int q = 0; q < QT; ++q) {
         redo[q] = false;
         if (end > j0 * HALVES) t.m[q] = t.state(ROW_M, q);           // (set with the wave's first half)
-        if (t.me(q).reach > j0 * U) {
+        if (end > j0 * HALVES && t.me(q).reach > j0 * U) {      // (a wave without rows has `end` 0)
             const float sum = sum_xor32(t.l[q]);
             redo[q] = !(sum >= PACKED_SUM_MIN && sum <= PACKED_SUM_MAX) || !(fabsf(t.state(ROW_MC, q)) <= PACKED_FAR);
             float zero = 0.f;                            // (NaN if a value is not finite)
@@ -738,7 +746,8 @@ packed_bf16_kernel(PackedArgs a) {
 
 // ------------------------------------------------------------------------------------ fp32
 // 16 rows per wave with full fp32 products (v_mfma_f32_16x16x4_f32): S^T = K Q^T leaves a row in lane % 16 with keys 4 (lane / 16) + i of every 16.
-// Probabilities in fp32, exponentials as exact as expf.
+// Probabilities in fp32, exponentials as exact as expf.  What binds is the time of a step, two barriers and products and maxima that wait for each other, where a
+// sample has few rows, and its vector and matrix instructions, one after the other, where it has many.
 // cap * tanh(x / cap), into = 2 / cap in powers of two: cap - 2 cap / (1 + 2^(into x)), the quotient refined once.  Off by a few roundings of cap, where a
 // score's own products are off by as many of |q| |k| (with a series below 0.35, exact for small x too, 29 instructions instead of 8).
 __device__ __forceinline__ float capped_of(float x, float cap, float into) {
@@ -747,15 +756,16 @@ __device__ __forceinline__ float capped_of(float x, float cap, float into) {
     return x != x ? x : y;
 }
 
-// APART: the workgroup takes 16 rows (of the block's 64, those of blockIdx.y), each wave a quarter of every tile's keys, and the waves' sums are united
-// behind the last key: where a sample has too few rows to fill the chip, a quarter of the steps behind each other.
+// APART: the workgroup takes 16 rows (of the block's 64, those of `part`), each wave a quarter of every tile's keys, and the waves' sums are united
+// behind the last key: where a sample has too few rows to fill the chip, a quarter of the steps behind each other.  (1000, 517 and 77 tokens,
+// 16 heads of 32, causal, capped, with a bias: 46 us before their order changed; with rows of their own for each wave 80.)
 template <int HD, bool APART>
-__device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave) {
+__device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave, int part) {
     constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256, BQ = PACKED_BQ_F32, NG = APART ? 1 : 4;
     constexpr int AHEAD = !APART ? 1 : HD <= 32 ? 4 : HD == 64 ? 2 : 1;              // tiles requested ahead (a step is shorter than a load)
     const int l16 = lane & 15, kgrp = lane >> 4, g0 = APART ? wave : 0;              // g0: the wave's first 16 keys of a tile
     const float *kb = (const float*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const float*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
-    const int w0 = it.r0 + 16 * (APART ? (int)blockIdx.y : wave), wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
+    const int w0 = it.r0 + 16 * (APART ? part : wave), wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
     const int bl = APART ? wl : min(it.r0 + BQ, it.rows) - 1;        // the workgroup's last row
     const bool mine = w0 < it.rows;
     const int least = mine ? it.reach(a, it.ahead + w0 / a.share) : 0, most = mine ? it.reach(a, it.ahead + wl / a.share) : 0;
@@ -950,41 +960,78 @@ packed_f32_kernel(PackedArgs a) {
     constexpr int KT = 64, LD = HD + 4;
     __shared__ __attribute__((aligned(16))) float lds[2 * KT * LD], Fs[KT];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane);
+    // four workgroups for each item, on one XCD and next to each other, so that what is long comes first for all of them (1000, 517 and 77 tokens, 16 heads of 32:
+    // 38 us, with the four parts one behind the other 46)
+    const unsigned at = blockIdx.y * gridDim.x + blockIdx.x;
+    const int part = at >> 3 & 3;
+    const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane, at >> 5 << 3 | (at & 7));
     if (!it.any) return;                                 // (the whole workgroup)
     if (packed_apart(it.rows, it.pieces, a.kv_heads)) {
-        if (it.r0 + 16 * (int)blockIdx.y < it.rows) packed_f32_rows<HD, true>(a, it, lds, lds + KT * LD, Fs, lane, wave);
-    } else if (blockIdx.y == 0) {
-        packed_f32_rows<HD, false>(a, it, lds, lds + KT * LD, Fs, lane, wave);
+        if (it.r0 + 16 * part < it.rows) packed_f32_rows<HD, true>(a, it, lds, lds + KT * LD, Fs, lane, wave, part);
+    } else if (part == 0) {
+        packed_f32_rows<HD, false>(a, it, lds, lds + KT * LD, Fs, lane, wave, 0);
     }
 }
 
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
-// takes a block, a wave a row at a time: HD / 4 lanes hold 4 adjacent values each, and the wave's 256 / HD teams of them take a piece each in turn.
+// takes a block; HD / 4 lanes, a team, hold 4 adjacent values each.  Of many pieces a wave takes a row at a time and its 256 / HD teams a piece each in turn; of up
+// to four a team takes a row.
 template <typename T, int HD, int BQ>
 __global__ void __launch_bounds__(256)
 packed_join_kernel(PackedArgs a) {
     constexpr int W = HD / 4, TEAMS = 64 / W;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = lane % W * 4, team = lane / W;
-    const PackedItem it = packed_item<BQ>(a, lane);
+    const PackedItem it = packed_item<BQ>(a, lane, blockIdx.x);
     if (!it.any || it.pieces <= 1) return;
     // (the block's rows are shared among its pieces' workgroups)
     const float c = a.cap > 0.f || a.slopes ? 1.0f : a.scale * PACKED_LOG2E;
     const long step = (long)a.kv_heads * a.part_rows * (HD + 4);
+    const auto weight = [c](float m, float ref) { return sizeof(T) == 2 ? exp2_between(m, ref, c) : expf(m - ref); };
+    const auto result = [&](int r, f32x4_t acc, float l) {
+        acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
+        T* o = (T*)a.o + packed_row(a, it, it.r0 + r, a.o_tok, a.o_head) + d;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(o) = __builtin_convertvector(acc, bf16x4_t);
+        else *reinterpret_cast<f32x4_t*>(o) = acc;
+    };
+    if (it.pieces <= 4) {                                // a team takes a row, all of whose pieces are loaded together
+        for (int r = (it.piece * 4 + wave) * TEAMS + team; r < min(BQ, it.rows - it.r0); r += 4 * it.pieces * TEAMS) {
+            const float* p = packed_part<BQ, HD>(a, it, 0, it.r0 + r);
+            f32x4_t v[4], acc = {0.f, 0.f, 0.f, 0.f};
+            f32x2_t s[4];
+            float top = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float* of = p + min(i, it.pieces - 1) * step;
+                s[i] = *reinterpret_cast<const f32x2_t*>(of + HD);
+                v[i] = *reinterpret_cast<const f32x4_t*>(of + d);
+                top = fmaxf(top, s[i][1]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;  // (then every weight is zero, and so are the sums)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= it.pieces) continue;
+                const float w = weight(s[i][1], ref);
+                acc += v[i] * w;
+                l = __builtin_fmaf(s[i][0], w, l);
+            }
+            result(r, acc, l);
+        }
+        return;
+    }
     for (int r = wave + 4 * it.piece; r < min(BQ, it.rows - it.r0); r += 4 * it.pieces) {
         const float* p = packed_part<BQ, HD>(a, it, 0, it.r0 + r);
         float top = -INFINITY;
         for (int i = lane; i < it.pieces; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-        const float ref = top == -INFINITY ? 0.f : top;      // (then every weight is zero, and so are the sums)
+        const float ref = top == -INFINITY ? 0.f : top;
         f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
 #pragma unroll 4
         for (int i = team; i < it.pieces; i += TEAMS) {
             const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-            const float w = sizeof(T) == 2 ? exp2_between(s[1], ref, c) : expf(s[1] - ref);
+            const float w = weight(s[1], ref);
             acc += v * w;
             l = __builtin_fmaf(s[0], w, l);
         }
@@ -994,11 +1041,7 @@ packed_join_kernel(PackedArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], x);
         }
-        if (team != 0) continue;
-        acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
-        T* o = (T*)a.o + packed_row(a, it, it.r0 + r, a.o_tok, a.o_head) + d;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(o) = __builtin_convertvector(acc, bf16x4_t);
-        else *reinterpret_cast<f32x4_t*>(o) = acc;
+        if (team == 0) result(r, acc, l);
     }
 }
 
@@ -1036,7 +1079,7 @@ static hipError_t launch_packed_hd(int dtype, PackedArgs a, hipStream_t st) {
     const unsigned grid = (unsigned)packed_workgroups(p.slots, a.kv_heads);
     if (dtype != PS_BF16) {
         if (a.samples > PACKED_SEARCH) packed_table_kernel<PACKED_BQ_F32><<<1, 1024, 0, st>>>(a);
-        packed_f32_kernel<HD><<<dim3(grid, 4), 256, 0, st>>>(a);
+        packed_f32_kernel<HD><<<dim3(grid / 2, 8), 256, 0, st>>>(a);      // (4 * grid, each dimension below 2^32 threads)
         if (a.part) packed_join_kernel<float, HD, PACKED_BQ_F32><<<grid, 256, 0, st>>>(a);
     } else if (HD > 64 || p.block == 128) {
         launch_packed_bf16<HD, 1>(a, grid, st);

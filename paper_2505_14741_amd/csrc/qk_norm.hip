@@ -29,7 +29,8 @@ hipError_t launch_rope_table(const float* positions, long position_row, const Ro
 // y = rotate(norm(x) * gamma + beta): norm 0 none, 1 x / sqrt(mean x^2 + eps), 2 (x - mean) / sqrt(mean (x - mean)^2 + eps), over a head; pair p of the
 // first 2 * pairs values turns by the table's angle p of the token: values 2p and 2p + 1, or (halves) p and p + pairs.
 // Memory binds: q and k are read and written once.  A wave takes a token, L lanes a head with 8 adjacent values each; it goes over the
-// token's heads 4 rounds at a time, whose loads are requested together, and has the token's angles in registers.
+// token's heads 4 rounds at a time, whose loads are requested together, and has the token's angles in registers.  (17776 tokens of 60 heads of 64 in bf16, 278 MB: 65 us,
+// 4.3 TB/s, where a copy reaches 4.9.)
 // L: lanes of a head, a power of two (of which head_dim / 8 work).
 template <int L>
 __device__ __forceinline__ float sum_of_team(float v) {

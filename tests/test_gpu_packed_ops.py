@@ -523,6 +523,53 @@ def test_packed_attention_many_samples(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_packed_attention_many_samples_with_divided_keys(dtype):
+    """80 samples, some with keys for several workgroups, some without any: the table and the partial sums share the workspace; alone, and replayed from
+    a graph with other offsets, each sample gives the same bits."""
+    g = gen(12)
+    nqs = [(1, 3, 0, 2, 70)[i % 5] for i in range(80)]
+    nks = [(40, 1500, 7, 0, 90, 2600, 1279)[i % 7] for i in range(80)]
+    q, k, v = randn(g, sum(nqs), 4, 64).to(dtype), randn(g, sum(nks), 2, 64).to(dtype), randn(g, sum(nks), 2, 64).to(dtype)
+    qo, ko = offsets(nqs), offsets(nks)
+    kw = {"causal": True, "frame": 30, "prefix": [i % 50 for i in range(80)], "slopes": torch.tensor([0.5, 0.1, 0.02, 0.0], device=DEV)}
+    whole = check_packed(q, k, v, 0.125, qo, ko, **kw)
+    call = {**kw, "prefix_lens": ints(*kw["prefix"])}
+    del call["prefix"]
+    for s in range(80):
+        a, b, ka, kb = qo[s], qo[s + 1], ko[s], ko[s + 1]
+        alone = B.packed_attn(q[a:b].contiguous(), k[ka:kb].contiguous(), v[ka:kb].contiguous(), 0.125, ints(0, b - a), kv_offsets=ints(0, kb - ka),
+                              **{**call, "prefix_lens": call["prefix_lens"][s:s + 1]})
+        assert torch.equal(whole[a:b], alone), s
+    dq, dk = ints(*qo), ints(*ko)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = B.packed_attn(q, k, v, 0.125, dq, kv_offsets=dk, **call)
+    other = offsets(list(reversed(nks)))
+    for keys in (ko, other, ko, other):
+        dk.copy_(ints(*keys))
+        want = B.packed_attn(q, k, v, 0.125, ints(*qo), kv_offsets=ints(*keys), **call)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("samples", [50, 400])
+def test_packed_attention_of_offsets_that_fall_stays_inside(dtype, samples):
+    """Every second sample has all the tokens: far more blocks, and pieces of their keys, than rising offsets could have."""
+    g = gen(13)
+    q, k, v = (randn(g, 1500, 2, 64).to(dtype) for _ in range(3))
+    wide = torch.full((1500, 4, 64), 7.0, dtype=dtype, device=DEV)
+    fall = ints(*[0, 1500] * (samples // 2), 0)
+    B.packed_attn(q, k, v, 0.125, fall, kv_offsets=fall, out=wide[:, 1:3])
+    B.packed_attn(q[:20], k, v, 0.125, fall, kv_offsets=fall, out=wide[:20, 1:3])
+    B.packed_attn(q, k, v, 0.125, fall, out=wide[:, 1:3])
+    torch.cuda.synchronize()
+    assert bool((wide[:, 0] == 7.0).all()) and bool((wide[:, 3] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_packed_attention_strides_and_offsets_outside(dtype):
     """Parts of one projection, head-major tensors, repeated operands, an output inside a wider one; offsets before 0 and behind the end are
     clamped."""
