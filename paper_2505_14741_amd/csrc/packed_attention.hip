@@ -217,7 +217,7 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 // tracked(): a reference that moves where a score exceeds it by 8 in powers of two, and is subtracted first where it is large.  The rows next to them keep
 // what they have, so a row's result depends neither on them nor on the block's size.
 //
-// Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 820 us, 0.93 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.45 ms, 0.90; the
+// Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 806 us, 0.94 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.45 ms, 0.90; the
 // simple kernel, one moving reference and a tile of 64 keys at a time, 1061 and 1810.  Vector instructions are at work 53 % of the time, the matrix unit 39 %, rarely
 // both: what a wave's three parts leave free the other wave of the SIMD hardly takes, and at the end of the launch 1.65 of 2 waves are there.  Four slots of keys and
 // a manual order of the parts: as fast; items in the order of the offsets and over all XCDs instead of as packed_place() and packed_item() have them: 931 and 1766 us
@@ -234,7 +234,8 @@ enum PackedFrames { PACKED_ONE, PACKED_EACH, PACKED_ANY };
 enum PackedState { ROW_REACH, ROW_SLOPE, ROW_FRAME, ROW_M, ROW_MC, ROW_STATES };     // (ROW_MC: the reference in powers of two)
 
 // BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  Two kernels, because the loops of both
-// in one leave it without registers.  (1350 rows of 30 heads against 17776 keys in frames of 1350: 316 us, with each key's bias looked up 381.)
+// in one leave it without registers.  (1350 rows of 30 heads against 17776 keys in frames of 1350: 316 us, with each
+// key's bias looked up 381; now, with its join, 275.)
 template <int HD, int QT, bool CAP, int BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
@@ -623,7 +624,8 @@ packed_bf16_kernel(PackedArgs a) {
     constexpr int SLOTS = P::SLOTS;
     t.request(j0, 0, -1, 0, j1);
     t.request(j0 + 1, 1, j0, 0, j1);
-    // One tile.  Per half h (of all the sample's; parity X): the scores of the next one, this one's weights, the last one's values.
+    // One tile.  Per half h (of all the sample's; parity X): the last one's values, the scores of the next one, this one's weights; the compiler mixes the three, and
+    // from this order it makes the fastest code (17776 tokens 2478 us; scores, weights, values 2592, the other orders between 2533 and 2631).
     // Kinds: PACKED_ONE, all rows of the workgroup see the whole tile, which lies in one frame and is neither the first nor the last; PACKED_EACH, the same
     // behind the prefix with any frames; PACKED_ANY.
     int slot = 0;
@@ -641,9 +643,9 @@ packed_bf16_kernel(PackedArgs a) {
             const int X = HALVES == 2 ? half : decltype(x_c)::value, h = j * HALVES + half, kv0 = h * 32;
             const int next = half + 1 < HALVES ? slot : up, last = half > 0 ? slot : down, next_half = half + 1 < HALVES ? half + 1 : 0, last_half = half > 0 ? half - 1 : HALVES - 1;
             if constexpr (STEADY) {
+                t.template values<false, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
                 t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
                 t.template weights<false, FRAMES>(s[X], pf[X], kv0, t.frames_at(slot, half));
-                t.template values<false, QT>(pf[X ^ 1], kv0 - 32, t.values_at(last, last_half));
             } else {
                 if (h + 1 < min(end, j1 * HALVES)) t.template scores<QT>(s[X ^ 1], t.keys_at(next, next_half));
                 if (h < end) {
