@@ -126,9 +126,9 @@ template <int R> struct Fp4Strips {
     __device__ __forceinline__ static int at(int strip) { return strip / PER * 272 + strip % PER * R; }
 };
 
-// Measured: 17776 x 5760, k = 1920 147 us, 2.67 PFLOP/s; 4516 x 1920, k = 7680 39, 3.4.  At this rate LDS binds, not the matrix unit: a stage of a wave of 96 x 64 reads
-// 20 fragments and 40 scale bytes and writes its share of the loads, together as long as its 48 products (a ring of three or four stages
-// instead of two: no faster), so the loop alone reaches 4.6; the rest is the first stage's way and the results', 7 us for each of 9 rounds of workgroups.
+// Measured: 17776 x 5760, k = 1920 147 to 160 us, 2.5 to 2.67 PFLOP/s; 4516 x 1920, k = 7680 39 to 42, 3.2 to 3.4.  No unit is busy for long (the first: matrix instructions 28 % of the
+// cycles, vector 32, LDS reads 18).  The loop alone reaches 4.6 PFLOP/s: a stage's 57 KB are read by 8 waves through 40 fragments and 40 scale bytes for
+// every 96 products of a SIMD.  The rest is the first stage's way and the results', 7 us for each of 9 rounds of workgroups.
 //
 // WR x WC waves of TM x TN blocks of 16 x 16 outputs (rows x columns).  A ring of NST stages.
 // A stage has two halves of TM / 2 row blocks.  The first goes row block by row block: as soon as the products of one are issued, its
