@@ -748,8 +748,7 @@ packed_bf16_kernel(PackedArgs a) {
 
 // ------------------------------------------------------------------------------------ fp32
 // 16 rows per wave with full fp32 products (v_mfma_f32_16x16x4_f32): S^T = K Q^T leaves a row in lane % 16 with keys 4 (lane / 16) + i of every 16.
-// Probabilities in fp32, exponentials as exact as expf.  What binds is the time of a step, two barriers and products and maxima that wait for each other, where a
-// sample has few rows, and its vector and matrix instructions, one after the other, where it has many.
+// Probabilities in fp32, exponentials as exact as expf.  What binds is the time of a step, two barriers and products and maxima that wait for each other.
 // cap * tanh(x / cap), into = 2 / cap in powers of two: cap - 2 cap / (1 + 2^(into x)), the quotient refined once.  Off by a few roundings of cap, where a
 // score's own products are off by as many of |q| |k| (with a series below 0.35, exact for small x too, 29 instructions instead of 8).
 __device__ __forceinline__ float capped_of(float x, float cap, float into) {
@@ -758,20 +757,18 @@ __device__ __forceinline__ float capped_of(float x, float cap, float into) {
     return x != x ? x : y;
 }
 
-// APART: the workgroup takes 16 rows (of the block's 64, those of `part`), each wave a quarter of every tile's keys, and the waves' sums are united
-// behind the last key: where a sample has too few rows to fill the chip, a quarter of the steps behind each other.  (1000, 517 and 77 tokens,
-// 16 heads of 32, causal, capped, with a bias: 46 us before their order changed; with rows of their own for each wave 80.)
-template <int HD, bool APART>
+// A workgroup takes 16 rows (of the block's 64, those of `part`), each wave a quarter of every tile's keys, and the waves' sums are united behind the last key.
+// (1000, 517 and 77 tokens, 16 heads of 32, causal, capped, with a bias: 46 us, 38 since its parts lie side by side.  With rows of their own for each wave, and all
+// keys, 80; 4276 tokens, 30 heads of 64, 6068 us against 1898, of 16 1825 against 560, of 128 13240 against 4360.)
+template <int HD>
 __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave, int part) {
-    constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256, BQ = PACKED_BQ_F32, NG = APART ? 1 : 4;
-    constexpr int AHEAD = !APART ? 1 : HD <= 32 ? 4 : HD == 64 ? 2 : 1;              // tiles requested ahead (a step is shorter than a load)
-    const int l16 = lane & 15, kgrp = lane >> 4, g0 = APART ? wave : 0;              // g0: the wave's first 16 keys of a tile
+    constexpr int KT = 64, LD = HD + 4, NB = HD / 16, CH = HD / 4, LOADS = KT * CH / 256, BQ = PACKED_BQ_F32;
+    constexpr int AHEAD = HD <= 32 ? 4 : HD == 64 ? 2 : 1;           // tiles requested ahead (a step is shorter than a load)
+    const int l16 = lane & 15, kgrp = lane >> 4;
     const float *kb = (const float*)a.k + (long)it.k0 * a.k_tok + it.g * a.k_head, *vb = (const float*)a.v + (long)it.k0 * a.v_tok + it.g * a.v_head;
-    const int w0 = it.r0 + 16 * (APART ? part : wave), wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
-    const int bl = APART ? wl : min(it.r0 + BQ, it.rows) - 1;        // the workgroup's last row
-    const bool mine = w0 < it.rows;
-    const int least = mine ? it.reach(a, it.ahead + w0 / a.share) : 0, most = mine ? it.reach(a, it.ahead + wl / a.share) : 0;
-    const int tiles_all = (it.keys + KT - 1) / KT, tiles = (it.reach(a, it.ahead + bl / a.share) + KT - 1) / KT;
+    const int w0 = it.r0 + 16 * part, wl = min(w0 + 15, it.rows - 1), row = min(w0 + l16, it.rows - 1);
+    const int least = it.reach(a, it.ahead + w0 / a.share), most = it.reach(a, it.ahead + wl / a.share);
+    const int tiles_all = (it.keys + KT - 1) / KT, tiles = (most + KT - 1) / KT;
     const int j0 = (int)((long)tiles_all * it.piece / it.pieces), j1 = min(tiles, (int)((long)tiles_all * (it.piece + 1) / it.pieces));
     const PackedRow me = packed_query(a, it, row);
     const float into = a.cap > 0.f ? 2.0f * PACKED_LOG2E / a.cap : 0.f;
@@ -822,42 +819,35 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
         if (a.slopes && threadIdx.x < KT) Fs[threadIdx.x] = packed_frame(a, it, kv0 + (int)threadIdx.x);
         __syncthreads();
         if (j + AHEAD < j1) fetch(n, kv0 + AHEAD * KT);
-        const int k0 = kv0 + g0 * 16;                    // the wave's keys
+        const int k0 = kv0 + wave * 16;                  // the wave's keys
         if (k0 >= most) return;
-        const int blocks = min(NG, (most - k0 + 15) / 16);           // 16-key blocks that some row of the wave sees
-        const bool cut = k0 + 16 * NG > least;
+        const bool cut = k0 + 16 > least;
         const int left = me.reach - k0 - 4 * kgrp;
-        f32x4_t sc[NG];
+        f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
         float top = -INFINITY, low = INFINITY;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            sc[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (g < blocks) {
+        for (int d = 0; d < NB; ++d) {
+            const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + (wave * 16 + l16) * LD + d * 16 + kgrp * 4);
 #pragma unroll
-                for (int d = 0; d < NB; ++d) {
-                    const f32x4_t kf = *reinterpret_cast<const f32x4_t*>(Ks + ((g0 + g) * 16 + l16) * LD + d * 16 + kgrp * 4);
+            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[d][e], sc, 0, 0, 0);
+        }
+        if (a.cap > 0.f) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[d][e], sc[g], 0, 0, 0);
-                }
-            }
-            if (a.cap > 0.f) {
+            for (int i = 0; i < 4; ++i) sc[i] = capped_of(sc[i], a.cap, into);
+        }
+        if (a.slopes) {
+            const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + wave * 16 + kgrp * 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[g][i] = capped_of(sc[g][i], a.cap, into);
-            }
-            if (a.slopes) {
-                const f32x4_t f = *reinterpret_cast<const f32x4_t*>(Fs + (g0 + g) * 16 + kgrp * 4);
+            for (int i = 0; i < 4; ++i) sc[i] -= packed_bias(me, f[i]);
+        }
+        if (cut) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[g][i] -= packed_bias(me, f[i]);
-            }
-            if (cut) {
+            for (int i = 0; i < 4; ++i) sc[i] = i < left ? sc[i] : -INFINITY;
+        }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[g][i] = g * 16 + i < left ? sc[g][i] : -INFINITY;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                top = fmaxf(top, sc[g][i]);
-                low = fminf(low, sc[g][i]);
-            }
+        for (int i = 0; i < 4; ++i) {
+            top = fmaxf(top, sc[i]);
+            low = fminf(low, sc[i]);
         }
         const float mn = fmaxf(m, max_xor32(max_xor16(top))), ref = mn == -INFINITY ? 0.f : mn;
         if (__any(mn != m)) {
@@ -870,34 +860,30 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
         const bool near = __ballot(low - ref < EXP_NEAR) == 0;       // (of the whole wave; not with keys that a row does not see)
         bool odd = false;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            if (g >= blocks) continue;
+        for (int i = 0; i < 4; ++i) sc[i] = near ? exp_near(sc[i] - ref) : expf(sc[i] - ref);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[g][i] = near ? exp_near(sc[g][i] - ref) : expf(sc[g][i] - ref);
+        for (int i = 0; i < 4; ++i) l += sc[i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) l += sc[g][i];
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int d = 0; d < NB; ++d) {
-                    float x = Vs[((g0 + g) * 16 + kgrp * 4 + e) * LD + d * 16 + l16];
-                    if (cut) {                           // (as in the bf16 kernel)
-                        const bool o = !(fabsf(x) < INFINITY);
-                        odd = odd || o;
-                        x = o ? 0.f : x;
-                    }
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, sc[g][e], acc[d], 0, 0, 0);
+            for (int d = 0; d < NB; ++d) {
+                float x = Vs[(wave * 16 + kgrp * 4 + e) * LD + d * 16 + l16];
+                if (cut) {                               // (as in the bf16 kernel)
+                    const bool o = !(fabsf(x) < INFINITY);
+                    odd = odd || o;
+                    x = o ? 0.f : x;
                 }
-        }
+                acc[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, sc[e], acc[d], 0, 0, 0);
+            }
         if (cut && __any(odd)) {
 #pragma unroll 1
-            for (int key = 0; key < min(16 * NG, it.keys - k0); ++key) {
+            for (int key = 0; key < min(16, it.keys - k0); ++key) {
                 if (k0 + key >= me.reach) continue;
 #pragma unroll
                 for (int d = 0; d < NB; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = Vs[(g0 * 16 + key) * LD + d * 16 + 4 * kgrp + i];
+                        const float x = Vs[(wave * 16 + key) * LD + d * 16 + 4 * kgrp + i];
                         if (!(fabsf(x) < INFINITY)) acc[d][i] += x;
                     }
             }
@@ -909,39 +895,37 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
             if (j + n < j1) tile(j + n, n);
     }
     l = sum_xor32(sum_xor16(l));
-    if constexpr (APART) {
-        constexpr int N = NB * 4 + 2;                    // [wave - 1][value][lane]
-        static_assert(3 * N * 64 <= 2 * KT * LD, "scratch");
-        __syncthreads();
-        if (wave > 0) {
-            float* to = Ks + (wave - 1) * N * 64 + lane;
+    constexpr int N = NB * 4 + 2;                    // [wave - 1][value][lane]
+    static_assert(3 * N * 64 <= 2 * KT * LD, "scratch");
+    __syncthreads();
+    if (wave > 0) {
+        float* to = Ks + (wave - 1) * N * 64 + lane;
 #pragma unroll
-            for (int d = 0; d < NB; ++d)
+        for (int d = 0; d < NB; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) to[(d * 4 + i) * 64] = acc[d][i];
-            to[(N - 2) * 64] = l;
-            to[(N - 1) * 64] = m;
-        }
-        __syncthreads();
-        if (wave > 0) return;
-        float top = m;
+            for (int i = 0; i < 4; ++i) to[(d * 4 + i) * 64] = acc[d][i];
+        to[(N - 2) * 64] = l;
+        to[(N - 1) * 64] = m;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float top = m;
 #pragma unroll
-        for (int w = 0; w < 3; ++w) top = fmaxf(top, Ks[(w * N + N - 1) * 64 + lane]);
-        const float ref = top == -INFINITY ? 0.f : top, f0 = expf(m - ref);
-        m = top;
-        l *= f0;
+    for (int w = 0; w < 3; ++w) top = fmaxf(top, Ks[(w * N + N - 1) * 64 + lane]);
+    const float ref = top == -INFINITY ? 0.f : top, f0 = expf(m - ref);
+    m = top;
+    l *= f0;
 #pragma unroll
-        for (int d = 0; d < NB; ++d) acc[d] *= f0;
+    for (int d = 0; d < NB; ++d) acc[d] *= f0;
 #pragma unroll
-        for (int w = 0; w < 3; ++w) {
-            const float* from = Ks + w * N * 64 + lane;
-            const float f = expf(from[(N - 1) * 64] - ref);
-            l = __builtin_fmaf(from[(N - 2) * 64], f, l);
+    for (int w = 0; w < 3; ++w) {
+        const float* from = Ks + w * N * 64 + lane;
+        const float f = expf(from[(N - 1) * 64] - ref);
+        l = __builtin_fmaf(from[(N - 2) * 64], f, l);
 #pragma unroll
-            for (int d = 0; d < NB; ++d)
+        for (int d = 0; d < NB; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[d][i] = __builtin_fmaf(from[(d * 4 + i) * 64], f, acc[d][i]);
-        }
+            for (int i = 0; i < 4; ++i) acc[d][i] = __builtin_fmaf(from[(d * 4 + i) * 64], f, acc[d][i]);
     }
     if (w0 + l16 >= it.rows) return;
     if (it.pieces > 1) {
@@ -968,11 +952,7 @@ packed_f32_kernel(PackedArgs a) {
     const int part = at >> 3 & 3;
     const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane, at >> 5 << 3 | (at & 7));
     if (!it.any) return;                                 // (the whole workgroup)
-    if (packed_apart(it.rows, it.pieces, a.kv_heads)) {
-        if (it.r0 + 16 * part < it.rows) packed_f32_rows<HD, true>(a, it, lds, lds + KT * LD, Fs, lane, wave, part);
-    } else if (part == 0) {
-        packed_f32_rows<HD, false>(a, it, lds, lds + KT * LD, Fs, lane, wave, 0);
-    }
+    if (it.r0 + 16 * part < it.rows) packed_f32_rows<HD>(a, it, lds, lds + KT * LD, Fs, lane, wave, part);
 }
 
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup

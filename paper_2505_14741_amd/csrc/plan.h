@@ -431,6 +431,7 @@ constexpr CrossPlan cross_plan(bool bf16, int rows, int kv_len, int kv_heads, in
 // over all samples only.
 constexpr int PACKED_SEARCH = 64;                        // most samples that a workgroup looks through itself; more: a table
 constexpr int PACKED_KEYS = 1280;                        // least keys of a sample that is divided
+// (us with rows apart / keys apart: a token of 30 heads over 6, 17776 keys 22.3 / 21.7, 6 tokens, 1000 keys 19.6 / 14.7; 32 tokens of 30 heads, 17776 keys 41 / 37)
 constexpr int PACKED_FEW_ROWS = 32;                      // rows up to which a workgroup's waves take keys apart instead of rows
 constexpr int PACKED_FEW_KEYS = 1024;                    // least keys of a piece there
 constexpr int PACKED_FEW_MIN = 128;                      // keys from which they do
@@ -456,9 +457,8 @@ constexpr int packed_pieces(int rows, int keys, int kv_heads) {
     }
     return best;
 }
-// fp32: whether a sample's workgroups, up to four rounds of them, take 16 rows each and their waves keys apart
-constexpr bool packed_apart(int rows, int pieces, int kv_heads) { return (rows + 63L) / 64 * pieces * kv_heads <= 2 * PACKED_PIECES; }
-// block: rows of a workgroup (bf16, heads up to 64: 256 where that leaves two workgroups for each compute unit; a row's result does not depend on it); slots:
+// block: rows of a workgroup (bf16, heads up to 64: 256 where that leaves three workgroups for two compute units; a row's result does not depend on it; us at 128 / 256 rows,
+// one sample: 2926 tokens of 30 heads 102 / 112, 3400 155 / 134, 4276 218 / 225, 5600 325 / 291, 8326 640 / 557, 17776 of 6 heads 665 / 537); slots:
 // the most workgroups of a key head; scratch: a table of the slots, and a block of partial sums for each slot and key head
 struct PackedPlan { int block, slots, part_rows; size_t table_bytes, part_bytes; };
 constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int kv_heads, int block) {
@@ -473,7 +473,7 @@ constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int 
 constexpr long packed_workgroups(long slots, int kv_heads) { return (slots + 7) / 8 * 8 * kv_heads; }
 constexpr PackedPlan packed_plan(bool bf16, bool own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, int cus) {
     PackedPlan p{};
-    p.block = !bf16 ? 64 : head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 2L * cus ? 256 : 128;
+    p.block = !bf16 ? 64 : head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 3L * cus / 2 ? 256 : 128;
     p.slots = (int)packed_slots(own, samples, rows, kv_tokens, kv_heads, p.block);
     p.part_rows = rows < p.block ? rows : p.block;
     if (samples > PACKED_SEARCH) p.table_bytes = ((size_t)p.slots + 1) * 8 / 256 * 256 + 256;
