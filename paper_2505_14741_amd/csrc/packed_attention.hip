@@ -717,7 +717,7 @@ packed_bf16_kernel(PackedArgs a) {
             for (int d = 0; d < NB; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(t.acc[q][d][i], 0.f, zero);
-            zero += max_xor32(zero);
+            zero = sum_xor32(zero);                      // (both lanes of the row alike; a maximum would lose the NaN)
             redo[q] = redo[q] || (sum > PACKED_SUM_NEAR && zero != 0.f);
         }
         store(q, !redo[q]);
