@@ -213,9 +213,9 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 //
 // A row's exponents are relative to the largest score of its first 32 keys (without the distance bias, which is not positive where slopes are not
 // negative), instead of a maximum that moves: what the sums became is looked at behind the last key.  Rows whose sum is not within 2^-40 .. 2^32, or
-// above 2^14 with outputs that are not finite, or whose reference is beyond 2^10 (where the rounding of scale * score is 2^-14), are computed again by
-// tracked(): a reference that moves where a score exceeds it by 8 in powers of two, and is subtracted first where it is large.  The rows next to them keep
-// what they have, so a row's result depends neither on them nor on the block's size.
+// above 2^8 (which values may be multiplied with) with outputs that are not finite, or whose reference is beyond 2^10 (where the rounding of
+// scale * score is 2^-14), are computed again by tracked(): a reference that moves where a score exceeds it by 8 in powers of two, and is
+// subtracted first where it is large.  The rows next to them keep what they have, so a row's result depends neither on them nor on the block's size.
 //
 // Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 806 us, 0.94 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.45 ms, 0.90; the
 // simple kernel, one moving reference and a tile of 64 keys at a time, 1061 and 1810.  Vector instructions are at work 53 % of the time, the matrix unit 39 %, rarely
@@ -223,7 +223,7 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 // a manual order of the parts: as fast; items in the order of the offsets and over all XCDs instead of as packed_place() and packed_item() have them: 931 and 1766 us
 // (with them 847 and 1540, of that time's kernel).
 constexpr float PACKED_AHEAD = 8.0f, PACKED_FAR = 0x1p+10f;
-constexpr float PACKED_SUM_MIN = 0x1p-40f, PACKED_SUM_MAX = 0x1p+32f, PACKED_SUM_NEAR = 0x1p+14f;
+constexpr float PACKED_SUM_MIN = 0x1p-40f, PACKED_SUM_MAX = 0x1p+32f, PACKED_SUM_NEAR = 0x1p+8f;
 constexpr int PACKED_BQ_F32 = 64;
 
 __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {

@@ -37,3 +37,15 @@ def test_values_that_overflow_in_some_dimensions_under_divided_keys(dtype, d, di
     print(f"packed_attn {dtype} d={d} dims={dims} {nq}x{nk}x{heads}", flush=True)
     q, k, v = grown(dtype, d, nq, nk, heads, 16 * 16, 2.0 ** 108, list(dims))
     check_packed(q, k, v, SCALE, [0, nq], [0, nk])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [16, 64, 128])
+def test_values_that_overflow_under_moderate_sums(dtype, d):
+    """40 keys, the last 8 with the weight 1960: sums of 2^13.9, within 2^14, times 2^114.7 are no fp32 number."""
+    high = 2.0 ** 114 * 1.59375
+    assert high * 40 * 256 < torch.finfo(torch.float32).max
+    q, k, v = grown(dtype, d, 40, 40, 3, 175, high, [2, 5])
+    v[..., 2], v[..., 5] = high, -high
+    got = check_packed(q, k, v, SCALE, [0, 40])
+    assert bool(torch.isfinite(got).all())
