@@ -958,6 +958,11 @@ packed_f32_kernel(PackedArgs a) {
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
 // takes a block; HD / 4 lanes, a team, hold 4 adjacent values each.  Of many pieces a wave takes a row at a time and its 256 / HD teams a piece each in turn; of up
 // to four a team takes a row.
+// The sums l_i come first, and weights are divided by the power of two below their sum, which is exact: then no sum of values is more than twice the largest value.
+// (A bf16 piece's weights may sum to 2^32, and what each piece holds as a number the pieces together need not.)
+__device__ __forceinline__ float packed_unit(float l) {  // 2^-n for 2^n <= l < 2^(n + 1)
+    return l > 0.f && l < INFINITY ? __uint_as_float((254u << 23) - (__float_as_uint(l) & 0x7f800000u)) : 1.f;
+}
 template <typename T, int HD, int BQ>
 __global__ void __launch_bounds__(256)
 packed_join_kernel(PackedArgs a) {
@@ -989,14 +994,17 @@ packed_join_kernel(PackedArgs a) {
                 top = fmaxf(top, s[i][1]);
             }
             const float ref = top == -INFINITY ? 0.f : top;  // (then every weight is zero, and so are the sums)
+            float w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (i >= it.pieces) continue;
-                const float w = weight(s[i][1], ref);
-                acc += v[i] * w;
-                l = __builtin_fmaf(s[i][0], w, l);
+                w[i] = weight(s[i][1], ref);
+                if (i < it.pieces) l = __builtin_fmaf(s[i][0], w[i], l);
             }
-            result(r, acc, l);
+            const float f = packed_unit(l);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < it.pieces) acc += v[i] * (w[i] * f);
+            result(r, acc, l * f);
         }
         return;
     }
@@ -1007,23 +1015,24 @@ packed_join_kernel(PackedArgs a) {
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
         const float ref = top == -INFINITY ? 0.f : top;
-        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
+        for (int i = lane; i < it.pieces; i += 64) {
+            const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
+            l = __builtin_fmaf(s[0], weight(s[1], ref), l);
+        }
+        l = sum_of_64(l);
+        const float f = packed_unit(l);
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int i = team; i < it.pieces; i += TEAMS) {
-            const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-            const float w = weight(s[1], ref);
-            acc += v * w;
-            l = __builtin_fmaf(s[0], w, l);
+            acc += v * (weight(p[i * step + HD + 1], ref) * f);
         }
 #pragma unroll
-        for (int x = W; x < 64; x *= 2) {
-            l += __shfl_xor(l, x);
+        for (int x = W; x < 64; x *= 2)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], x);
-        }
-        if (team == 0) result(r, acc, l);
+        if (team == 0) result(r, acc, l * f);
     }
 }
 

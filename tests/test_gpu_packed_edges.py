@@ -49,3 +49,14 @@ def test_values_that_overflow_under_moderate_sums(dtype, d):
     v[..., 2], v[..., 5] = high, -high
     got = check_packed(q, k, v, SCALE, [0, 40])
     assert bool(torch.isfinite(got).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("nq,nk,heads,level,power", [(100, 3000, 1, 12, 108), (200, 1500, 60, 11, 109), (70, 20000, 2, 12, 105), (5, 3000, 2, 12, 108)])
+def test_pieces_whose_sums_overflow_only_together(dtype, d, nq, nk, heads, level, power):
+    """Each piece's sum of weights times values is below 2^128, the sum over the pieces is not."""
+    print(f"packed_attn {dtype} d={d} {nq}x{nk}x{heads}", flush=True)
+    assert 2.0 ** power * nk * 256 < torch.finfo(torch.float32).max
+    q, k, v = grown(dtype, d, nq, nk, heads, 16 * level, 2.0 ** power, [0, 3, 4])
+    check_packed(q, k, v, SCALE, [0, nq], [0, nk])
