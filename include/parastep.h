@@ -316,7 +316,7 @@ PS_API int qk_norm_rope(const void* q, const void* k, const float* table, const 
  * kv_tokens may be 0; samples and heads <= 65535, tokens <= 2^24, q_tokens * heads / kv_heads <= 2^30 and, divided by 64, plus samples, at most 2^23 / kv_heads, with own_offsets 2^19 / kv_heads.  frame >= 1; cap >= 0, and scale / cap must be finite.
  * Finite in fp32 must be, with what a query sees: scale * log2(e) (refused else), q . k and that times scale * log2(e); cap and slope * distance, times log2(e);
  * the largest |v| times the keys (in bf16 times 2^8 more).  bf16: products in bf16, probabilities rounded to bf16 for the second product, statistics and sums in fp32; fp32:
- * everything in fp32.  A sample's result does not depend on the others.
+ * everything in fp32.  A capped score is off by 2^-19 of the score at most (bf16, caps up to 256: 2^-21 of the cap).  A sample's result does not depend on the others.
  * workspace: DEVICE, 256-byte aligned, >= packed_attn_workspace_bytes(...) (may be NULL when that is 0): where a sample's queries do not fill the chip its keys, with
  * own_offsets, are divided among workgroups, and their partial sums pass through it; of more than 64 samples it holds a table. */
 typedef struct {

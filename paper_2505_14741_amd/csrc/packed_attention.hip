@@ -226,6 +226,17 @@ constexpr float PACKED_AHEAD = 8.0f, PACKED_FAR = 0x1p+10f;
 constexpr float PACKED_SUM_MIN = 0x1p-40f, PACKED_SUM_MAX = 0x1p+32f, PACKED_SUM_NEAR = 0x1p+8f;
 constexpr int PACKED_BQ_F32 = 64;
 
+// Largest cap that bf16 computes as cap - 2 cap / (1 + 2^(..)) alone, off by 2^-22 of the cap: 2^-14 here, where weights are rounded by 2^-8.
+constexpr float PACKED_CAP_NEAR = 256.0f;
+// Next to zero that form is off by more of x than its own roundings the larger the cap is; below a quarter of the cap the first terms of the series of cap * tanh(x / cap)
+// take its place.  w = 2 log2(e) x / cap; x + x (-t^2 / 3 + 2 t^4 / 15 - 17 t^6 / 315 + 62 t^8 / 2835) for t = x / cap, t^2 = w^2 ln(2)^2 / 4: off by 2^-23 of x at most.
+// Together with the other form: 2^-20 of x (its exponential and quotient, at a quarter of the cap).
+constexpr float PACKED_CAP_SERIES = 0.5203422f;              // (log2(e) / 2)^2
+__device__ __forceinline__ float packed_cap_series(float x, float w2) {
+    const float p = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(4.5520010e-6f, w2, -9.3521435e-5f), w2, 1.9236258e-3f), w2, -0.040037751f);
+    return __builtin_fmaf(x * w2, p, x);
+}
+
 __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
 }
@@ -233,10 +244,12 @@ __device__ __forceinline__ s16x4_t packed_read_tr16(const unsigned char* p) {
 enum PackedFrames { PACKED_ONE, PACKED_EACH, PACKED_ANY };
 enum PackedState { ROW_REACH, ROW_SLOPE, ROW_FRAME, ROW_M, ROW_MC, ROW_STATES };     // (ROW_MC: the reference in powers of two)
 
+// CAP: 0 none; 1 up to PACKED_CAP_NEAR; 2 above it (4276 tokens of 30 heads of 64: 220, 342 and 372 us; an exponential, a reciprocal and, of the last, the
+// series for each score).
 // BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  Two kernels, because the loops of both
 // in one leave it without registers.  (1350 rows of 30 heads against 17776 keys in frames of 1350: 316 us, with each
 // key's bias looked up 381; now, with its join, 275.)
-template <int HD, int QT, bool CAP, int BIAS>
+template <int HD, int QT, int CAP, int BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
     static constexpr int SLOTS = 3;                                  // tiles of K, and of V, in LDS (four, requested a tile earlier: as fast)
@@ -338,7 +351,8 @@ struct PackedBf16 {
         }
     }
     __device__ __forceinline__ float capped(float s) const {         // in powers of two
-        return __builtin_fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * into)), cap2);
+        const float w = s * into, y = __builtin_fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w)), cap2);
+        return CAP == 2 && w * w < PACKED_CAP_SERIES ? packed_cap_series(s * c0, w * w) : y;
     }
     // keys that the row does not see
     __device__ __forceinline__ void cut(f32x16_t& s, int q, int kv0) const {
@@ -558,7 +572,7 @@ struct PackedBf16 {
     }
 };
 
-template <int HD, int QT, bool CAP, int BIAS>
+template <int HD, int QT, int CAP, int BIAS>
 __global__ void __launch_bounds__(256, QT == 1 && HD <= 64 ? 3 : 2)
 packed_bf16_kernel(PackedArgs a) {
     typedef PackedBf16<HD, QT, CAP, BIAS> P;
@@ -749,12 +763,11 @@ packed_bf16_kernel(PackedArgs a) {
 // ------------------------------------------------------------------------------------ fp32
 // 16 rows per wave with full fp32 products (v_mfma_f32_16x16x4_f32): S^T = K Q^T leaves a row in lane % 16 with keys 4 (lane / 16) + i of every 16.
 // Probabilities in fp32, exponentials as exact as expf.  What binds is the time of a step, two barriers and products and maxima that wait for each other.
-// cap * tanh(x / cap), into = 2 / cap in powers of two: cap - 2 cap / (1 + 2^(into x)), the quotient refined once.  Off by a few roundings of cap, where a
-// score's own products are off by as many of |q| |k| (with a series below 0.35, exact for small x too, 29 instructions instead of 8).
+// cap * tanh(x / cap), into = 2 / cap in powers of two: cap - 2 cap / (1 + 2^(into x)), the quotient refined once; the series below a quarter of the cap.
 __device__ __forceinline__ float capped_of(float x, float cap, float into) {
-    const float d = 1.0f + fminf(__builtin_amdgcn_exp2f(x * into), 0x1p+100f), r = __builtin_amdgcn_rcpf(d);
+    const float w = x * into, d = 1.0f + fminf(__builtin_amdgcn_exp2f(w), 0x1p+100f), r = __builtin_amdgcn_rcpf(d);
     const float y = __builtin_fmaf(-2.0f * cap, __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r), cap);
-    return x != x ? x : y;
+    return w * w < PACKED_CAP_SERIES ? packed_cap_series(x, w * w) : x != x ? x : y;
 }
 
 // A workgroup takes 16 rows (of the block's 64, those of `part`), each wave a quarter of every tile's keys, and the waves' sums are united behind the last key.
@@ -1037,7 +1050,8 @@ packed_join_kernel(PackedArgs a) {
 }
 
 static PackedPlan packed_plan_of(int dtype, const PackedArgs& a) {
-    return packed_plan(dtype == PS_BF16, a.own_offsets, a.samples, a.q_tokens * a.share, a.kv_tokens, a.kv_heads, a.head_dim, compute_units());
+    return packed_plan(dtype == PS_BF16, a.own_offsets, a.samples, a.q_tokens * a.share, a.kv_tokens, a.kv_heads, a.head_dim, compute_units(),
+                       a.cap <= PACKED_CAP_NEAR ? 256 : 128);
 }
 size_t packed_workspace_bytes(int dtype, const PackedArgs& a) {
     const PackedPlan p = packed_plan_of(dtype, a);
@@ -1048,14 +1062,19 @@ template <int HD, int QT>
 static void launch_packed_bf16(const PackedArgs& a, unsigned grid, hipStream_t st) {
     if (a.samples > PACKED_SEARCH) packed_table_kernel<128 * QT><<<1, 1024, 0, st>>>(a);
     const int bias = !a.slopes ? 0 : a.frame >= 64 ? 1 : 2;
-    if (a.cap > 0.f) {
-        if (bias == 0) packed_bf16_kernel<HD, QT, true, 0><<<grid, 256, 0, st>>>(a);
-        else if (bias == 1) packed_bf16_kernel<HD, QT, true, 1><<<grid, 256, 0, st>>>(a);
-        else packed_bf16_kernel<HD, QT, true, 2><<<grid, 256, 0, st>>>(a);
+    if (a.cap > PACKED_CAP_NEAR) {                       // (hardly ever: blocks of 128 rows, one kernel for frames of every length)
+        if constexpr (QT == 1) {
+            if (bias == 0) packed_bf16_kernel<HD, 1, 2, 0><<<grid, 256, 0, st>>>(a);
+            else packed_bf16_kernel<HD, 1, 2, 2><<<grid, 256, 0, st>>>(a);
+        }
+    } else if (a.cap > 0.f) {
+        if (bias == 0) packed_bf16_kernel<HD, QT, 1, 0><<<grid, 256, 0, st>>>(a);
+        else if (bias == 1) packed_bf16_kernel<HD, QT, 1, 1><<<grid, 256, 0, st>>>(a);
+        else packed_bf16_kernel<HD, QT, 1, 2><<<grid, 256, 0, st>>>(a);
     } else {
-        if (bias == 0) packed_bf16_kernel<HD, QT, false, 0><<<grid, 256, 0, st>>>(a);
-        else if (bias == 1) packed_bf16_kernel<HD, QT, false, 1><<<grid, 256, 0, st>>>(a);
-        else packed_bf16_kernel<HD, QT, false, 2><<<grid, 256, 0, st>>>(a);
+        if (bias == 0) packed_bf16_kernel<HD, QT, 0, 0><<<grid, 256, 0, st>>>(a);
+        else if (bias == 1) packed_bf16_kernel<HD, QT, 0, 1><<<grid, 256, 0, st>>>(a);
+        else packed_bf16_kernel<HD, QT, 0, 2><<<grid, 256, 0, st>>>(a);
     }
     if (a.part) packed_join_kernel<bf16_t, HD, 128 * QT><<<grid, 256, 0, st>>>(a);
 }

@@ -471,9 +471,10 @@ constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int 
 }
 // a workgroup for each slot, up to a multiple of 8, and key head
 constexpr long packed_workgroups(long slots, int kv_heads) { return (slots + 7) / 8 * 8 * kv_heads; }
-constexpr PackedPlan packed_plan(bool bf16, bool own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, int cus) {
+// (most: 128 if there is no kernel for more)
+constexpr PackedPlan packed_plan(bool bf16, bool own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, int cus, int most = 256) {
     PackedPlan p{};
-    p.block = !bf16 ? 64 : head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 3L * cus / 2 ? 256 : 128;
+    p.block = !bf16 ? 64 : most >= 256 && head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 3L * cus / 2 ? 256 : 128;
     p.slots = (int)packed_slots(own, samples, rows, kv_tokens, kv_heads, p.block);
     p.part_rows = rows < p.block ? rows : p.block;
     if (samples > PACKED_SEARCH) p.table_bytes = ((size_t)p.slots + 1) * 8 / 256 * 256 + 256;
