@@ -17,9 +17,10 @@ struct PackedArgs {
     long q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
     bool own_offsets;             // whether kv_offsets are given, for the sizes
     void* scratch;                // packed_workspace_bytes()
-    int slots, part_rows;         // (set by the launcher)
-    int2* table;                  // (the same: which slot is whose, or NULL)
+    int slots;                    // (set by the launcher)
+    int2* table;                  // (the same: which slot is whose, and behind it the rows of partial sums in front of each sample, or NULL)
     float* part;                  // (the same: partial sums, or NULL)
+    unsigned part_rows;           // (the same: of a key head)
 };
 size_t packed_workspace_bytes(int dtype, const PackedArgs& a);
 hipError_t launch_packed_attention(int dtype, PackedArgs a, hipStream_t st);

@@ -11,6 +11,7 @@
 #include "lane_sums.h"
 #include "plan.h"
 #include "tile_ops.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace ps {
@@ -31,7 +32,8 @@ __device__ __forceinline__ unsigned frame_of(unsigned n, unsigned frame, float i
 
 // (wave-uniform)
 struct PackedItem {
-    int g, r0, rows, q0, k0, keys, ahead, prefix, piece, pieces, sample, slot;
+    int g, r0, rows, q0, k0, keys, ahead, prefix, piece, pieces, sample;
+    unsigned front;                                      // rows of partial sums of a key head in front of the sample's
     float inv_frame;
     bool any;
     // keys that a query sees, at `pos` of the sample's keys
@@ -72,36 +74,54 @@ __device__ __forceinline__ PackedCount packed_count(const PackedArgs& a, int s) 
     c.pieces = a.own_offsets ? packed_pieces(c.nq * a.share, c.keys, a.kv_heads) : 1;
     return c;
 }
-// More than PACKED_SEARCH samples: a table of (sample, slot of the sample) for every slot, table[0].x of them behind it; made by one workgroup.
+// Rows of a sample's partial sums (below 2^28; of all together below 2^30, but for offsets that fall, where sums of them may wrap around).
+__device__ __forceinline__ unsigned packed_rows(const PackedArgs& a, const PackedCount& c) { return c.pieces > 1 ? (unsigned)(c.nq * a.share * c.pieces) : 0; }
+// More than PACKED_SEARCH samples: a table of (sample, slot of the sample) for every slot, table[0].x of them behind it, and of the rows of partial sums in front of
+// every sample; made by one workgroup.
 template <int BQ>
 __global__ void __launch_bounds__(1024)
 packed_table_kernel(PackedArgs a) {
     __shared__ int sums[16];
+    __shared__ unsigned rows[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int2* const table = a.table;
+    unsigned* const fronts = reinterpret_cast<unsigned*>(table + 1 + a.slots);
     long base = 0;                                       // (offsets that fall could count far more than there are)
+    unsigned front_base = 0;
     for (int s0 = 0; s0 < a.samples; s0 += 1024) {
         const int s = s0 + (int)threadIdx.x;
         int n = 0;
+        unsigned own = 0;
         if (s < a.samples) {
             const PackedCount c = packed_count<BQ>(a, s);
             n = min(c.blocks * c.pieces, a.slots);
+            own = packed_rows(a, c);
         }
         int upto = n;                                    // inclusive sums
+        unsigned rows_upto = own;
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) {
             const int v = __shfl_up(upto, x);
+            const unsigned u = __shfl_up(rows_upto, x);
             upto += lane >= x ? v : 0;
+            rows_upto += lane >= x ? u : 0;
         }
         __syncthreads();
-        if (lane == 63) sums[wave] = upto;
+        if (lane == 63) {
+            sums[wave] = upto;
+            rows[wave] = rows_upto;
+        }
         __syncthreads();
         long at = base + upto - n;
+        unsigned front = front_base + rows_upto - own;
         for (int w = 0; w < 16; ++w) {
             at += w < wave ? sums[w] : 0;
             base += sums[w];
+            front += w < wave ? rows[w] : 0;
+            front_base += rows[w];
         }
         for (int i = 0; i < n && at + i < a.slots; ++i) table[1 + at + i] = make_int2(s, i);
+        if (s < a.samples) fronts[s] = front;
     }
     if (threadIdx.x == 0) table[0] = make_int2((int)min(base, (long)a.slots), 0);
 }
@@ -114,7 +134,7 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane,
     int slot, of_sample;                                 // of_sample: which of the sample's slots
     packed_place(id, a.kv_heads, t.g, slot);
     t.any = false;
-    t.slot = slot;
+    t.front = 0;
     if (slot >= a.slots) return t;
     PackedCount c;
     if (a.samples <= PACKED_SEARCH) {
@@ -129,6 +149,10 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane,
         if (here == 0) return t;
         t.sample = __builtin_ctzll(here);
         of_sample = slot - __builtin_amdgcn_readlane(before, t.sample);
+        if (__builtin_amdgcn_readlane(c.pieces, t.sample) > 1) {
+            const int rows = (int)packed_rows(a, c);
+            for (int i = 0; i < t.sample; ++i) t.front += (unsigned)__builtin_amdgcn_readlane(rows, i);
+        }
         c.q0 = __builtin_amdgcn_readlane(c.q0, t.sample);
         c.nq = __builtin_amdgcn_readlane(c.nq, t.sample);
         c.k0 = __builtin_amdgcn_readlane(c.k0, t.sample);
@@ -140,15 +164,17 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane,
         const int2 e = a.table[1 + slot];
         t.sample = uniform(e.x);
         of_sample = uniform(e.y);
+        t.front = (unsigned)uniform((int)reinterpret_cast<const unsigned*>(a.table + 1 + a.slots)[t.sample]);
         c = packed_count<BQ>(a, t.sample);
         c.q0 = uniform(c.q0); c.nq = uniform(c.nq); c.k0 = uniform(c.k0); c.keys = uniform(c.keys); c.blocks = uniform(c.blocks); c.pieces = uniform(c.pieces);
     }
     const int block = (int)((unsigned)of_sample / (unsigned)c.pieces);
     t.piece = of_sample - block * c.pieces;
     t.pieces = c.pieces;
-    if (slot - t.piece + t.pieces > a.slots) return t;   // (offsets that fall: the block's last pieces have no place)
-    t.q0 = c.q0;
     t.rows = c.nq * a.share;
+    // (offsets that fall: the block's last pieces have no slot, or the sample's rows no place)
+    if (t.pieces > 1 && (slot - t.piece + t.pieces > a.slots || t.front > a.part_rows || packed_rows(a, c) > a.part_rows - t.front)) return t;
+    t.q0 = c.q0;
     t.r0 = (c.blocks - 1 - block) * BQ;
     t.k0 = c.k0;
     t.keys = c.keys;
@@ -158,10 +184,10 @@ __device__ __forceinline__ PackedItem packed_item(const PackedArgs& a, int lane,
     t.any = true;
     return t;
 }
-// where the partial sums of a block's row lie: a block of rows for each slot and key head (slots of the block's pieces are neighbours)
-template <int BQ, int HD>
+// where a row's partial sums lie: [key head][row] of each of the sample's pieces
+template <int HD>
 __device__ __forceinline__ float* packed_part(const PackedArgs& a, const PackedItem& t, int piece, int row) {
-    return a.part + (((long)(t.slot - t.piece + piece) * a.kv_heads + t.g) * a.part_rows + (row - t.r0)) * (HD + 4);
+    return a.part + ((long)t.front * a.kv_heads + ((long)piece * a.kv_heads + t.g) * t.rows + row) * (HD + 4);
 }
 
 // offset of a row of the sample in q or o
@@ -600,7 +626,7 @@ packed_bf16_kernel(PackedArgs a) {
         const float sum = sum_xor32(t.l[q]);
         if (!in || row >= it.rows) return;
         if (it.pieces > 1) {
-            float* p = packed_part<BQ, HD>(a, it, it.piece, row);
+            float* p = packed_part<HD>(a, it, it.piece, row);
 #pragma unroll
             for (int d = 0; d < NB; ++d)
 #pragma unroll
@@ -942,7 +968,7 @@ __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const Packe
     }
     if (w0 + l16 >= it.rows) return;
     if (it.pieces > 1) {
-        float* p = packed_part<BQ, HD>(a, it, it.piece, row);
+        float* p = packed_part<HD>(a, it, it.piece, row);
 #pragma unroll
         for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(p + d * 16 + kgrp * 4) = acc[d];
         if (kgrp == 0) *reinterpret_cast<f32x2_t*>(p + HD) = f32x2_t{l, m};
@@ -968,6 +994,13 @@ packed_f32_kernel(PackedArgs a) {
     if (it.r0 + 16 * part < it.rows) packed_f32_rows<HD>(a, it, lds, lds + KT * LD, Fs, lane, wave, part);
 }
 
+__device__ __forceinline__ float max_of_64(float v) {    // in every lane (all lanes active)
+    v = max_xor16(max_xor32(v));
+    v = fmaxf(v, dpp<DPP_ROW_ROR_8>(v));
+    v = fmaxf(v, dpp<DPP_ROW_ROR_4>(v));
+    v = fmaxf(v, dpp<DPP_QUAD_XOR_2>(v));
+    return fmaxf(v, dpp<DPP_QUAD_XOR_1>(v));
+}
 // Adds the pieces of a row: o = sum_i w_i acc_i / sum_i w_i l_i, w_i = exp(ref_i - max), in powers of two times c for bf16.  A workgroup
 // takes a block; HD / 4 lanes, a team, hold 4 adjacent values each.  Of many pieces a wave takes a row at a time and its 256 / HD teams a piece each in turn; of up
 // to four a team takes a row.
@@ -985,7 +1018,7 @@ packed_join_kernel(PackedArgs a) {
     if (!it.any || it.pieces <= 1) return;
     // (the block's rows are shared among its pieces' workgroups)
     const float c = a.cap > 0.f || a.slopes ? 1.0f : a.scale * PACKED_LOG2E;
-    const long step = (long)a.kv_heads * a.part_rows * (HD + 4);
+    const long step = (long)a.kv_heads * it.rows * (HD + 4);     // from a piece to the next
     const auto weight = [c](float m, float ref) { return sizeof(T) == 2 ? exp2_between(m, ref, c) : expf(m - ref); };
     const auto result = [&](int r, f32x4_t acc, float l) {
         acc = l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / l;
@@ -995,7 +1028,7 @@ packed_join_kernel(PackedArgs a) {
     };
     if (it.pieces <= 4) {                                // a team takes a row, all of whose pieces are loaded together
         for (int r = (it.piece * 4 + wave) * TEAMS + team; r < min(BQ, it.rows - it.r0); r += 4 * it.pieces * TEAMS) {
-            const float* p = packed_part<BQ, HD>(a, it, 0, it.r0 + r);
+            const float* p = packed_part<HD>(a, it, 0, it.r0 + r);
             f32x4_t v[4], acc = {0.f, 0.f, 0.f, 0.f};
             f32x2_t s[4];
             float top = -INFINITY, l = 0.f;
@@ -1022,15 +1055,16 @@ packed_join_kernel(PackedArgs a) {
         return;
     }
     for (int r = wave + 4 * it.piece; r < min(BQ, it.rows - it.r0); r += 4 * it.pieces) {
-        const float* p = packed_part<BQ, HD>(a, it, 0, it.r0 + r);
-        float top = -INFINITY;
-        for (int i = lane; i < it.pieces; i += 64) top = fmaxf(top, p[i * step + HD + 1]);
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+        const float* p = packed_part<HD>(a, it, 0, it.r0 + r);
+        const auto state = [&](int i) { return *reinterpret_cast<const f32x2_t*>(p + i * step + HD); };
+        const f32x2_t mine = lane < it.pieces ? state(lane) : f32x2_t{0.f, -INFINITY};
+        float top = mine[1];
+        for (int i = lane + 64; i < it.pieces; i += 64) top = fmaxf(top, state(i)[1]);
+        top = max_of_64(top);
         const float ref = top == -INFINITY ? 0.f : top;
-        float l = 0.f;
-        for (int i = lane; i < it.pieces; i += 64) {
-            const f32x2_t s = *reinterpret_cast<const f32x2_t*>(p + i * step + HD);
+        float l = mine[0] * weight(mine[1], ref);
+        for (int i = lane + 64; i < it.pieces; i += 64) {
+            const f32x2_t s = state(i);
             l = __builtin_fmaf(s[0], weight(s[1], ref), l);
         }
         l = sum_of_64(l);
@@ -1039,7 +1073,7 @@ packed_join_kernel(PackedArgs a) {
 #pragma unroll 4
         for (int i = team; i < it.pieces; i += TEAMS) {
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + i * step + d);
-            acc += v * (weight(p[i * step + HD + 1], ref) * f);
+            acc += v * (weight(state(i)[1], ref) * f);
         }
 #pragma unroll
         for (int x = W; x < 64; x *= 2)
@@ -1053,9 +1087,14 @@ static PackedPlan packed_plan_of(int dtype, const PackedArgs& a) {
     return packed_plan(dtype == PS_BF16, a.own_offsets, a.samples, a.q_tokens * a.share, a.kv_tokens, a.kv_heads, a.head_dim, compute_units(),
                        a.cap <= PACKED_CAP_NEAR ? 256 : 128);
 }
+// Partial sums: what they take at most, by both bounds
+static size_t packed_part_bytes(const PackedPlan& p, const PackedArgs& a) {
+    const long rows = packed_part_rows(a.own_offsets, a.samples, a.q_tokens * a.share, a.kv_tokens, a.kv_heads);
+    return std::min(p.part_bytes, (size_t)rows * a.kv_heads * (a.head_dim + 4) * sizeof(float));
+}
 size_t packed_workspace_bytes(int dtype, const PackedArgs& a) {
     const PackedPlan p = packed_plan_of(dtype, a);
-    return p.table_bytes + p.part_bytes;
+    return p.table_bytes + packed_part_bytes(p, a);
 }
 
 template <int HD, int QT>
@@ -1083,9 +1122,10 @@ template <int HD>
 static hipError_t launch_packed_hd(int dtype, PackedArgs a, hipStream_t st) {
     const PackedPlan p = packed_plan_of(dtype, a);
     a.slots = p.slots;
-    a.part_rows = p.part_rows;
     a.table = p.table_bytes ? (int2*)a.scratch : nullptr;
-    a.part = p.part_bytes ? (float*)((char*)a.scratch + p.table_bytes) : nullptr;
+    const size_t part_bytes = packed_part_bytes(p, a);
+    a.part = part_bytes ? (float*)((char*)a.scratch + p.table_bytes) : nullptr;
+    a.part_rows = (unsigned)(part_bytes / ((size_t)a.kv_heads * (HD + 4) * sizeof(float)));
     const unsigned grid = (unsigned)packed_workgroups(p.slots, a.kv_heads);
     if (dtype != PS_BF16) {
         if (a.samples > PACKED_SEARCH) packed_table_kernel<PACKED_BQ_F32><<<1, 1024, 0, st>>>(a);

@@ -459,15 +459,55 @@ constexpr int packed_pieces(int rows, int keys, int kv_heads) {
 }
 // block: rows of a workgroup (bf16, heads up to 64: 256 where that leaves three workgroups for two compute units; a row's result does not depend on it; us at 128 / 256 rows,
 // one sample: 2926 tokens of 30 heads 102 / 112, 3400 155 / 134, 4276 218 / 225, 5600 325 / 291, 8326 640 / 557, 17776 of 6 heads 665 / 537); slots:
-// the most workgroups of a key head; scratch: a table of the slots, and a block of partial sums for each slot and key head
+// the most workgroups of a key head; table_bytes: the table of the slots and, for each sample, of the rows of partial sums in front of it; part_bytes: partial sums, a block
+// for each slot and key head
 struct PackedPlan { int block, slots, part_rows; size_t table_bytes, part_bytes; };
+// What the sums over all samples say of those that can be divided, by the three branches of packed_pieces(): few rows; up to a quarter of a round of items; up to two
+// rounds, in 4 pieces at most.
+struct PackedDivided {
+    int samples, round;                                  // that have PACKED_KEYS keys; most pieces of a unit of rows
+    int mid, mid_units, wide, wide_units;                // samples of the second and third branch, and the units of rows of one
+};
+constexpr PackedDivided packed_divided(int samples, int rows, int kv_tokens, int kv_heads) {
+    PackedDivided d{};
+    d.samples = samples < kv_tokens / PACKED_KEYS ? samples : kv_tokens / PACKED_KEYS;
+    d.round = PACKED_PIECES / kv_heads;
+    d.mid_units = PACKED_PIECES / 4 / kv_heads;
+    d.mid = d.mid_units < 1 ? 0 : rows / (PACKED_FEW_ROWS + 1);
+    if (d.mid > d.samples) d.mid = d.samples;
+    d.wide_units = (2 * PACKED_PIECES - 1) / kv_heads;
+    const int least = PACKED_UNIT * d.mid_units;         // such a sample has more rows
+    d.wide = d.wide_units < 1 ? 0 : rows / ((least > PACKED_FEW_ROWS ? least : PACKED_FEW_ROWS) + 1);
+    if (d.wide > d.samples) d.wide = d.samples;
+    return d;
+}
+constexpr long packed_least(long a, long b) { return a < b ? a : b; }
+constexpr long packed_most(long a, long b) { return a > b ? a : b; }
+// the most workgroups of a key head: a block each, and what pieces add
 constexpr long packed_slots(bool own, int samples, int rows, int kv_tokens, int kv_heads, int block) {
     const long blocks = rows / block + samples;
     if (!own || kv_tokens < PACKED_KEYS) return blocks;
-    const int divided = kv_tokens / PACKED_KEYS;         // samples that can be
-    const long more = (samples < divided ? samples : divided) * (long)(PACKED_PIECES / kv_heads) * (PACKED_UNIT > block ? PACKED_UNIT / block : 1);
-    const long each = ((rows < block ? rows : (long)PACKED_PIECES * block) + block - 1) / block * (kv_tokens / 256);     // blocks of a sample that has more than 4 pieces
-    return 4 * blocks + (more < each ? more : each);
+    const PackedDivided d = packed_divided(samples, rows, kv_tokens, kv_heads);
+    const long unit = PACKED_UNIT > block ? PACKED_UNIT / block : 1;                     // blocks of a unit of rows
+    const long mid_blocks = packed_least(((long)rows + block - 1) / block, ((long)d.mid_units * PACKED_UNIT + block - 1) / block);
+    const long wide_blocks = ((long)d.wide_units * PACKED_UNIT + block - 1) / block;
+    const long few = packed_least((long)d.samples * d.round, kv_tokens / PACKED_FEW_KEYS);
+    const long mid = packed_least(d.mid * d.round * unit, mid_blocks * (kv_tokens / 256));
+    const long wide = 3 * packed_least(d.wide ? rows / block + d.wide : 0, d.wide * wide_blocks);
+    const long more = packed_least(packed_least(few + mid, d.samples * d.round * unit) + wide, d.samples * packed_most(d.round * unit, 3 * wide_blocks));
+    return blocks + more;
+}
+// the most rows of partial sums of a key head: those of every divided sample, in each of its pieces.  (1024 samples of a token, 4096 keys each, 4 query heads to
+// each of 8 key heads: 262144, of which 16384 are used; a block for each slot would be 1.7 million.)
+constexpr long packed_part_rows(bool own, int samples, int rows, int kv_tokens, int kv_heads) {
+    if (!own || kv_tokens < PACKED_KEYS) return 0;
+    const PackedDivided d = packed_divided(samples, rows, kv_tokens, kv_heads);
+    const long few_rows = packed_least(rows, PACKED_FEW_ROWS), mid_rows = packed_least(rows, (long)d.mid_units * PACKED_UNIT);
+    const long few = few_rows * packed_least((long)d.samples * d.round, kv_tokens / PACKED_FEW_KEYS);
+    const long mid = packed_least((long)d.mid * d.round * PACKED_UNIT, mid_rows * (kv_tokens / 256));
+    const long wide = 4 * packed_least(d.wide ? rows : 0, (long)d.wide * d.wide_units * PACKED_UNIT);
+    const long each = packed_most(packed_most(few_rows * d.round, packed_least((long)d.round * PACKED_UNIT, mid_rows * (kv_tokens / 256))), 4 * packed_least(rows, (long)d.wide_units * PACKED_UNIT));
+    return packed_least(packed_least(few + mid + wide, rows * packed_most(d.round, 4)), d.samples * each);
 }
 // a workgroup for each slot, up to a multiple of 8, and key head
 constexpr long packed_workgroups(long slots, int kv_heads) { return (slots + 7) / 8 * 8 * kv_heads; }
@@ -477,7 +517,7 @@ constexpr PackedPlan packed_plan(bool bf16, bool own, int samples, int rows, int
     p.block = !bf16 ? 64 : most >= 256 && head_dim <= 64 && ((long)rows / 256 + samples) * kv_heads >= 3L * cus / 2 ? 256 : 128;
     p.slots = (int)packed_slots(own, samples, rows, kv_tokens, kv_heads, p.block);
     p.part_rows = rows < p.block ? rows : p.block;
-    if (samples > PACKED_SEARCH) p.table_bytes = ((size_t)p.slots + 1) * 8 / 256 * 256 + 256;
+    if (samples > PACKED_SEARCH) p.table_bytes = (((size_t)p.slots + 1) * 8 + (size_t)samples * 4) / 256 * 256 + 256;
     if (own && kv_tokens >= PACKED_KEYS) p.part_bytes = (size_t)p.slots * kv_heads * p.part_rows * (head_dim + 4) * sizeof(float);
     return p;
 }

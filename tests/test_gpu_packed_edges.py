@@ -1,5 +1,6 @@
 """Operators of self-attention on packed samples at the ends of their ranges: values as large as their type holds under scores that grow behind the first
 keys."""
+import ctypes as C
 import math
 
 import pytest
@@ -126,3 +127,33 @@ def test_large_caps_with_frames_prefixes_and_biases(dtype, d, frame, prefix):
         kk[300], vv[300] = float("nan"), float("inf")
         got = B.packed_attn(q, kk, vv, 0.2, ints(*offsets(lens)), causal=True, cap=300.0, **kw)
         assert torch.equal(got[:300], want[:300]) and torch.equal(got[531:], want[531:]) and bool(torch.isnan(got[300:531]).all())
+
+
+# ------------------------------------------------------------------------------------------------- many samples with kept keys
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("samples", [60, 64, 65, 150])
+def test_a_token_for_each_of_many_samples(dtype, samples):
+    """Keys of 0 to 4096, 16 heads over 4: divided and whole ones next to each other, the same bits as alone; nothing behind the workspace is written."""
+    g = gen(samples)
+    nks = [(0, 1, 1279, 1280, 2048, 4096, 700)[i % 7] for i in range(samples)]
+    nqs = [(1, 1, 2, 1, 0, 1, 9, 1)[i % 8] for i in range(samples)]
+    q, k, v = randn(g, sum(nqs), 16, 64).to(dtype), randn(g, sum(nks), 4, 64).to(dtype), randn(g, sum(nks), 4, 64).to(dtype)
+    qo, ko = offsets(nqs), offsets(nks)
+    whole = check_packed(q, k, v, 0.125, qo, ko, causal=True, prefix=[5] * samples)
+    for s in range(0, samples, 5):
+        a, b, ka, kb = qo[s], qo[s + 1], ko[s], ko[s + 1]
+        alone = B.packed_attn(q[a:b].contiguous(), k[ka:kb].contiguous(), v[ka:kb].contiguous(), 0.125, ints(0, b - a), kv_offsets=ints(0, kb - ka),
+                              prefix_lens=ints(5), causal=True)
+        assert torch.equal(whole[a:b], alone), s
+    shape = B._PackedShape(samples, sum(nqs), sum(nks), 16, 4, 64, B._CODE[dtype], 1, 1, 1, 0.125, 0.0, 1024, 64, 256, 64, 256, 64, 1024, 64)
+    n = B.lib().packed_attn_workspace_bytes(C.byref(shape))
+    ws = torch.full((n + 65536,), 77, dtype=torch.uint8, device=DEV)
+    prefix = ints(*[5] * samples)
+    fall = ints(*[0, sum(nqs)] * (samples // 2 + 1))[:samples + 1].contiguous(), ints(*[0, sum(nks)] * (samples // 2 + 1))[:samples + 1].contiguous()
+    for dq, dk in ((ints(*qo), ints(*ko)), fall):
+        out = torch.empty_like(q)
+        rc = B.lib().packed_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), dq.data_ptr(), dk.data_ptr(), prefix.data_ptr(), None, out.data_ptr(), C.byref(shape),
+                                 ws.data_ptr(), n, B._stream())
+        torch.cuda.synchronize()
+        assert rc == 0 and bool((ws[n:] == 77).all())
+        assert dq is fall[0] or torch.equal(out, whole)
