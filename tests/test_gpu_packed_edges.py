@@ -7,7 +7,8 @@ import pytest
 import torch
 
 from paper_2505_14741_amd import binding as B
-from test_gpu_packed_ops import DEV, U, check_packed, gen, ints, offsets, packed_ref, randn
+from test_gpu_packed_ops import DEV, U, check_packed, gen, ints, offsets, packed_ref, randn, widen
+from test_packed_edges_host import PRODUCTS, WIDE_HEADS, WIDE_KEYS, WIDE_LENS
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float32]
@@ -157,3 +158,101 @@ def test_a_token_for_each_of_many_samples(dtype, samples):
         torch.cuda.synchronize()
         assert rc == 0 and bool((ws[n:] == 77).all())
         assert dq is fall[0] or torch.equal(out, whole)
+
+
+# ------------------------------------------------------------------------------------------------- blocks of 256 rows
+def check_wide(q, k, v, scale, kv_lens, each=None, **kw):
+    """The call, in blocks of 256 rows, against 64 bits, and each sample's bits against those of a call of its own, in blocks of 128."""
+    qo, ko = offsets(WIDE_LENS), offsets(kv_lens or WIDE_LENS)
+    if each is None:
+        whole = check_packed(q, k, v, scale, qo, ko if kv_lens else None, **kw)
+    else:
+        whole = each
+    call = dict(kw)
+    prefix = call.pop("prefix", None)
+    for s in range(len(WIDE_LENS)):
+        a, b, ka, kb = qo[s], qo[s + 1], ko[s], ko[s + 1]
+        alone = B.packed_attn(q[a:b].contiguous(), k[ka:kb].contiguous(), v[ka:kb].contiguous(), scale, ints(0, b - a), kv_offsets=ints(0, kb - ka) if kv_lens else None,
+                              prefix_lens=None if prefix is None else ints(prefix[s]), **call)
+        assert torch.equal(whole[a:b].view(torch.int16), alone.view(torch.int16)), (s, kw)
+
+
+def wide_data(d, kv_lens, seed):
+    g = gen(seed + d)
+    n, m = sum(WIDE_LENS), sum(kv_lens or WIDE_LENS)
+    return g, randn(g, n, WIDE_HEADS, d).bfloat16(), randn(g, m, WIDE_HEADS, d).bfloat16(), randn(g, m, WIDE_HEADS, d).bfloat16()
+
+
+@pytest.mark.parametrize("d", [16, 32, 64])
+@pytest.mark.parametrize("kv_lens", [None, WIDE_KEYS])
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+def test_wide_blocks(d, kv_lens, cap):
+    """Masks, prefixes, frames shorter and longer than a tile, biases, capped scores, kept keys in pieces."""
+    _, q, k, v = wide_data(d, kv_lens, 1)
+    slopes = torch.linspace(-0.01, 0.4, WIDE_HEADS, device=DEV)
+    prefix = [i * 23 % 90 for i in range(len(WIDE_LENS))]
+    for kw in ({}, {"causal": True}, {"causal": True, "frame": 7, "prefix": prefix}, {"causal": True, "frame": 100, "prefix": prefix}, {"slopes": slopes},
+               {"slopes": slopes, "causal": True, "frame": 9, "prefix": prefix}, {"slopes": slopes, "causal": True, "frame": 130, "prefix": prefix}, {"slopes": slopes, "frame": 64}):
+        print(f"packed_attn wide d={d} own={kv_lens is not None} cap={cap} {sorted(kw)} frame={kw.get('frame')}", flush=True)
+        check_wide(q, k, v, 1.0 / math.sqrt(d), kv_lens, cap=cap, **kw)
+
+
+@pytest.mark.parametrize("d", [16, 32, 64])
+@pytest.mark.parametrize("kv_lens", [None, WIDE_KEYS])
+def test_wide_blocks_of_rows_that_are_computed_again(d, kv_lens):
+    """Scores of hundreds in some rows only, values that overflow under scores that grow, values and keys that are not finite."""
+    g, q, k, v = wide_data(d, kv_lens, 2)
+    loud = q.clone()
+    loud[::3] *= 60.0
+    check_wide(loud, k, v, 1.0 / math.sqrt(d), kv_lens)
+    check_wide(loud, k, v, 1.0 / math.sqrt(d), kv_lens, causal=True, frame=40)
+    qq, kk, vv = torch.zeros_like(q), torch.zeros_like(k), v.clone()
+    qq[..., 0] = 1.0
+    kk[torch.arange(k.shape[0], device=DEV) % 64 >= 32, :, 0] = 256.0
+    vv[..., [3, 6]] = (2.0 ** 107 * (0.5 + 0.5 * torch.rand(k.shape[0], WIDE_HEADS, 2, generator=g, device=DEV))).bfloat16()
+    check_wide(qq, kk, vv, SCALE, kv_lens)
+    qo, ko = offsets(WIDE_LENS), offsets(kv_lens or WIDE_LENS)
+    kk, vv = k.clone(), v.clone()
+    at = [ko[7] + 300, ko[2] + 40, ko[10] + 129]
+    kk[at[0]], vv[at[1], :, 2], vv[at[2], :, 1] = float("nan"), float("inf"), float("nan")
+    args = {"causal": True, "frame": 11}
+    dk = ints(*ko) if kv_lens else None
+    want = B.packed_attn(q, k, v, 0.2, ints(*qo), kv_offsets=dk, **args)
+    got = B.packed_attn(q, kk, vv, 0.2, ints(*qo), kv_offsets=dk, **args)
+    check_wide(q, kk, vv, 0.2, kv_lens, each=got, **args)
+    for s in range(len(WIDE_LENS)):
+        if s not in (7, 2, 10):
+            assert torch.equal(got[qo[s]:qo[s + 1]], want[qo[s]:qo[s + 1]])
+    exact, tol = packed_ref(q, k, v, 0.2, qo, ko, None, 11, True, 0.0, None)
+    for s, key, dim in ((7, 300, None), (2, 40, 2), (10, 129, 1)):
+        nq, nk = WIDE_LENS[s], (kv_lens or WIDE_LENS)[s]
+        pos = torch.arange(nk - nq, nk, device=DEV)
+        sees = torch.div(pos, 11, rounding_mode="floor") >= key // 11
+        part, ref = got[qo[s]:qo[s + 1]], want[qo[s]:qo[s + 1]]
+        assert torch.equal(part[~sees], ref[~sees])
+        assert not torch.isfinite(part[sees] if dim is None else part[sees][..., dim]).any()
+        if dim is not None:
+            # (a row whose sum is above 2^8 is computed again, so with another reference, as for values that overflow: other roundings of the same weights)
+            rest = [i for i in range(d) if i != dim]
+            far = (part.double() - exact[qo[s]:qo[s + 1]]).abs() <= tol[qo[s]:qo[s + 1]] * 1.001
+            assert bool(far[sees][..., rest].all())
+
+
+# ------------------------------------------------------------------------------------------------- 4-bit product
+# K products and a bias summed in fp32; GELU's slope is below 1.13, its own arithmetic good for 2^-20 of its argument
+@pytest.mark.parametrize("shape,tile", PRODUCTS)
+def test_product_of_4_bit_blocks_on_every_tile(shape, tile):
+    rows, n_out, k = shape
+    print(f"dit_linear_fp4 {rows}x{n_out}x{k} tile {tile}", flush=True)
+    g = gen(rows + n_out + k)
+    a = B.fp4_quantize(randn(g, rows, k) * torch.exp(2 * randn(g, rows, 1)) * torch.exp(randn(g, k)))
+    w = B.fp4_quantize(randn(g, n_out, k) / math.sqrt(k))
+    bias = randn(g, n_out)
+    A, W = widen(*a), widen(*w).t().contiguous()
+    y = A @ W + bias.double()
+    off = (k + 16) * 2.0 ** -24 * (A.abs() @ W.abs() + bias.double().abs())
+    for act in (0, 1):
+        ref = torch.nn.functional.gelu(y, approximate="tanh") if act else y
+        tol = 1.13 * off + U[torch.bfloat16] * ref.abs() + (2.0 ** -20 * (ref.abs() + 1.0) if act else 0.0) + 1e-30
+        err = (B.dit_linear_fp4(*a, *w, bias, act=act).double() - ref).abs()
+        assert bool((err <= tol).all()), (act, float((err / tol).max()))

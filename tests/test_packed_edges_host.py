@@ -9,10 +9,19 @@ import pytest
 from paper_2505_14741_amd import binding as B
 from paper_2505_14741_amd import build
 
+# 12 samples of 32 key heads: enough workgroups for blocks of 256 rows; each of them alone is not
+WIDE_HEADS = 32
+WIDE_LENS = [1, 5, 300, 64, 0, 257, 513, 700, 31, 255, 130, 66]
+WIDE_KEYS = [9, 1500, 2000, 64, 700, 1300, 513, 2500, 3000, 200, 5000, 1281]
+# rows, outputs, k: every tile of the 4-bit product (in the order of plan.h), an even and an odd number of blocks of 128, whole and ragged sizes
+PRODUCTS = [((2, 190, 1000), 0), ((190, 188, 300), 0), ((3585, 576, 2048), 1), ((3585, 578, 1900), 1), ((3601, 573, 2500), 1), ((3585, 1150, 1900), 2), ((3585, 1152, 2048), 2),
+            ((4516, 1920, 7680), 3), ((3585, 1150, 7780), 3), ((4500, 1906, 7800), 3), ((3585, 1150, 7600), 3), ((3585, 2304, 1900), 4), ((3585, 2303, 2048), 4), ((3585, 2304, 100), 4),
+            ((3585, 2304, 129), 4), ((3585, 2304, 300), 4)]
 RULES = """
 #include "plan.h"
 extern "C" int pieces(int rows, int keys, int kv_heads) { return ps::packed_pieces(rows, keys, kv_heads); }
 extern "C" long part_rows(int own, int samples, int rows, int kv_tokens, int kv_heads) { return ps::packed_part_rows(own != 0, samples, rows, kv_tokens, kv_heads); }
+extern "C" int product_tile(int m, int n, int blocks, int split) { return ps::fp4_plan(m, n, blocks, split != 0, 256).tile; }
 extern "C" void plan(int bf16, int own, int samples, int rows, int kv_tokens, int kv_heads, int head_dim, int most, long* out) {
     const ps::PackedPlan p = ps::packed_plan(bf16 != 0, own != 0, samples, rows, kv_tokens, kv_heads, head_dim, 256, most);
     out[0] = p.block; out[1] = p.slots; out[2] = p.part_rows; out[3] = (long)p.table_bytes; out[4] = (long)p.part_bytes; out[5] = ps::packed_workgroups(p.slots, kv_heads);
@@ -101,3 +110,25 @@ def test_the_largest_calls_count_below_31_bits(rules):
                 for bf16 in (0, 1):
                     rules.plan(bf16, 1, n, rows, 1 << 24, kv_heads, 16, 256, out)
                     assert out[5] < 1 << 24
+
+
+def test_blocks_of_256_rows_are_taken_where_their_tests_expect_them(rules):
+    out = (C.c_long * 6)()
+    for d in (16, 32, 64):
+        rules.plan(1, 0, 12, sum(WIDE_LENS), sum(WIDE_LENS), WIDE_HEADS, d, 256, out)
+        assert out[0] == 256
+        rules.plan(1, 1, 12, sum(WIDE_LENS), sum(WIDE_KEYS), WIDE_HEADS, d, 256, out)
+        assert out[0] == 256
+        for n in WIDE_LENS:
+            rules.plan(1, 1, 1, n, max(WIDE_KEYS), WIDE_HEADS, d, 256, out)
+            assert out[0] == 128
+    divided = {rules.pieces(a, b, WIDE_HEADS) for a, b in zip(WIDE_LENS, WIDE_KEYS)}
+    assert 1 in divided and divided & {2, 3, 4} and max(divided) > 4
+
+
+def test_products_take_the_tiles_their_tests_expect(rules):
+    for (m, n, k), tile in PRODUCTS:
+        for split in (0, 1):
+            assert rules.product_tile(m, n, (k + 127) // 128, split) == tile, (m, n, k)
+    for tile in range(5):
+        assert {(k + 127) // 128 % 2 for (_, _, k), t in PRODUCTS if t == tile} == {0, 1}
