@@ -291,7 +291,7 @@ PS_API int rope_table(const float* positions, int64_t position_row, int axes, co
  * projection; no other overlap.  kv_heads may be 0: then k, k_out and their norm are not looked at.  gamma, beta DEVICE fp32 [head_dim], each may be NULL (1, 0).
  * table DEVICE fp32 [tokens][rotated / 2][2], table_batch floats from one sample's to the next (0: one for all); may be NULL iff rotated is 0.
  * head_dim a multiple of 8, at most 256; rotated a multiple of 8 (halves: of 16), at most head_dim.  Statistics in fp32: the sum of a head's squares must be
- * finite there.  batch and tokens may be 0; tokens <= 2^24, batch and heads <= 65535, at most 2^25 tokens in all. */
+ * finite there and, if eps is 0, a normal number.  batch and tokens may be 0; tokens <= 2^24, batch and heads <= 65535, at most 2^25 tokens in all. */
 typedef struct {
     int batch, tokens, heads, kv_heads, head_dim, rotated, norm, halves, dtype;
     float eps;

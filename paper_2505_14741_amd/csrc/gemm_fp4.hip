@@ -15,7 +15,7 @@ namespace ps {
 // A block's scale is the least power of two 2^e, e >= -127, under which its largest value is at most 6, the largest of e2m1: with amax =
 // 1.f * 2^x, e = x - 2 where 1.f <= 1.5 and x - 1 above (6 = 1.5 * 2^2).  Multiplying by 2^-e is exact, so each value is rounded once, to the
 // nearest of 0 0.5 1 1.5 2 3 4 6, ties to the even code (what the conversion instruction does).  The format has no value that is not finite: a
-// block with one has the scale NaN, and zeros.  (17776 x 7680 in bf16, 346 MB: 74 us, 4.7 TB/s.)
+// block with one has the scale NaN, and zeros.  (17776 x 7680 in bf16, 346 MB: 88 us at the median, 3.9 TB/s, 73 at the best.)
 // Memory binds.  A workgroup takes 16 rows x 512 columns, 4 rows per wave, 8 adjacent values per lane (16 bytes of bf16, 4 lanes a
 // block): the 16 scales of a block lie side by side and are stored as 16 bytes, gathered in LDS.
 constexpr int FP4_ROWS = 16, FP4_COLS = 512;
@@ -126,7 +126,7 @@ template <int R> struct Fp4Strips {
     __device__ __forceinline__ static int at(int strip) { return strip / PER * 272 + strip % PER * R; }
 };
 
-// Measured: 17776 x 5760, k = 1920 147 to 160 us, 2.5 to 2.67 PFLOP/s; 4516 x 1920, k = 7680 39 to 42, 3.2 to 3.4.  No unit is busy for long (the first: matrix instructions 28 % of the
+// Measured: 17776 x 5760, k = 1920 147 to 178 us, 2.2 to 2.67 PFLOP/s; 4516 x 1920, k = 7680 39 to 44, 3.0 to 3.4.  No unit is busy for long (the first: matrix instructions 28 % of the
 // cycles, vector 32, LDS reads 18).  The loop alone reaches 4.6 PFLOP/s: a stage's 57 KB are read by 8 waves through 40 fragments and 40 scale bytes for
 // every 96 products of a SIMD.  The rest is the first stage's way and the results', 7 us for each of 9 rounds of workgroups.
 //

@@ -243,9 +243,9 @@ __device__ __forceinline__ float exp2_between(float a, float b, float c) {
 // scale * score is 2^-14), are computed again by tracked(): a reference that moves where a score exceeds it by 8 in powers of two, and is
 // subtracted first where it is large.  The rows next to them keep what they have, so a row's result depends neither on them nor on the block's size.
 //
-// Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 806 us, 0.94 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.45 ms, 0.90; the
-// simple kernel, one moving reference and a tile of 64 keys at a time, 1061 and 1810.  Vector instructions are at work 53 % of the time, the matrix unit 39 %, rarely
-// both: what a wave's three parts leave free the other wave of the SIMD hardly takes, and at the end of the launch 1.65 of 2 waves are there.  Four slots of keys and
+// Measured: five samples of 671 to 8326 tokens, 30 heads of 64 (761 GFLOP) 801 to 843 us, 0.90 to 0.95 PFLOP/s; 17776 tokens causal by frames (1305 GFLOP) 1.43 to
+// 1.50 ms, 0.87 to 0.91; the simple kernel, one moving reference and a tile of 64 keys at a time, 1061 and 1810.  Vector instructions are at work 64 % of the time, the
+// matrix unit 44 %, together less than half of it: what a wave's three parts leave free the other wave of the SIMD hardly takes, and at the end of the launch 1.65 of 2 waves are there.  Four slots of keys and
 // a manual order of the parts: as fast; items in the order of the offsets and over all XCDs instead of as packed_place() and packed_item() have them: 931 and 1766 us
 // (with them 847 and 1540, of that time's kernel).
 constexpr float PACKED_AHEAD = 8.0f, PACKED_FAR = 0x1p+10f;
@@ -274,7 +274,7 @@ enum PackedState { ROW_REACH, ROW_SLOPE, ROW_FRAME, ROW_M, ROW_MC, ROW_STATES };
 // series for each score).
 // BIAS: 0 none; 1 in frames of 64 keys and more, most tiles of which have one bias for each row; 2 in shorter ones.  Two kernels, because the loops of both
 // in one leave it without registers.  (1350 rows of 30 heads against 17776 keys in frames of 1350: 316 us, with each
-// key's bias looked up 381; now, with its join, 275.)
+// key's bias looked up 381; now, with its join, 265 to 286.)
 template <int HD, int QT, int CAP, int BIAS>
 struct PackedBf16 {
     static constexpr int U = HD > 64 ? 32 : 64, HALVES = U / 32;     // keys of a tile
@@ -518,8 +518,8 @@ struct PackedBf16 {
     }
 
     // Few rows (PACKED_FEW_ROWS): memory binds, and the waves take every fourth half of the keys each, through slots of their own and without a barrier; their
-    // sums are united behind the last key, in the first wave's registers.  (Single tokens of eight samples against 128 MB of keys and values: 30 us,
-    // 4.3 TB/s, and 7 for the join.)
+    // sums are united behind the last key, in the first wave's registers.  (Single tokens of eight samples against 128 MB of keys and values: 27 us,
+    // 4.7 TB/s, and 7 for the join.)
     static constexpr int FEW_UNITS = HD > 64 ? 2 : 3, FEW_LOADS = 32 * ROW / 1024, FEW_HALF = 32 * ROW, FEW_BYTES = 4 * FEW_UNITS * FEW_HALF;
     static constexpr int MOST = 2 * SLOTS * TILE > FEW_BYTES ? 2 * SLOTS * TILE : FEW_BYTES, SUMS = 3 * (NB * 16 + 2) * 256, LDS_BYTES = MOST > SUMS ? MOST : SUMS;
     __device__ __forceinline__ void request_half(int h, unsigned char* to, bool of_k) {
@@ -797,7 +797,7 @@ __device__ __forceinline__ float capped_of(float x, float cap, float into) {
 }
 
 // A workgroup takes 16 rows (of the block's 64, those of `part`), each wave a quarter of every tile's keys, and the waves' sums are united behind the last key.
-// (1000, 517 and 77 tokens, 16 heads of 32, causal, capped, with a bias: 46 us, 38 since its parts lie side by side.  With rows of their own for each wave, and all
+// (1000, 517 and 77 tokens, 16 heads of 32, causal, capped, with a bias: 46 us, 37 since its parts lie side by side.  With rows of their own for each wave, and all
 // keys, 80; 4276 tokens, 30 heads of 64, 6068 us against 1898, of 16 1825 against 560, of 128 13240 against 4360.)
 template <int HD>
 __device__ __forceinline__ void packed_f32_rows(const PackedArgs& a, const PackedItem& it, float* Ks, float* Vs, float* Fs, int lane, int wave, int part) {
@@ -986,7 +986,7 @@ packed_f32_kernel(PackedArgs a) {
     __shared__ __attribute__((aligned(16))) float lds[2 * KT * LD], Fs[KT];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     // four workgroups for each item, on one XCD and next to each other, so that what is long comes first for all of them (1000, 517 and 77 tokens, 16 heads of 32:
-    // 38 us, with the four parts one behind the other 46)
+    // 37 us, with the four parts one behind the other 46)
     const unsigned at = blockIdx.y * gridDim.x + blockIdx.x;
     const int part = at >> 3 & 3;
     const PackedItem it = packed_item<PACKED_BQ_F32>(a, lane, at >> 5 << 3 | (at & 7));
